@@ -1,0 +1,647 @@
+"""Work on caches held in 8 bits and on caches that forget, as a user's program
+calls it: a prompt's cache brought into 8 bits and back, attention of single
+tokens over such a cache, generation steps (append + attention) on it,
+attention that adds its weights up per cached row, and the eviction of the
+rows that gathered least.
+
+Shapes are those of the benchmark and the tests (32 query heads, 8 KV heads,
+head dimension 128; 4K to 1M tokens, full "adaptive" heads beside compact
+"consistent" ones); keys and values are N(0, 1) with 1% heavy-hitter keys
+scaled by 3.
+
+The 8-bit cache: of a view of L rows the first L // block * block are held as
+codes with one fp32 scale per block of rows (K and V each), the remaining
+L % block rows in the cache's own type in a tail buffer of one block.
+  int8  scale = fp32(max |x| * fp32(1 / 127)),  code = x / scale to nearest even
+  e4m3  scale = the least power of two with max |x| <= 448 scale, code = x / scale
+        to nearest even
+A block whose largest magnitude is below 2^-100 has scale and codes 0.
+"""
+import math
+import random
+from types import SimpleNamespace
+
+import numpy as np
+import torch
+
+own = False          # True: the framework's kernels instead of the plain forms
+
+DEV = "cuda:0"
+D = 128
+HEAVY_FRAC, HEAVY_SCALE = 0.01, 3.0
+TINY = 2.0 ** -100
+
+
+# ------------------------------------------------------------------ the cases
+
+def _case(op, n, **kw):
+    c = {"op": op, "dtype": "bf16", "fmt": "int8", "block": 64, "n": n, "n_min": n, "batch": 1, "len_seed": 1,
+         "hq": 32, "hkv": 8, "n_cons": 0, "rows_cons": 2112, "cs": 8, "recent": 64, "keep": 0, "weights": False}
+    c.update(kw)
+    return c
+
+
+def listed():
+    return [
+        # a short conversation of odd length parked in 8 bits and brought back, fp32
+        _case("quantize", 4099, name="quantize_4k_f32_int8", dtype="f32", block=32),
+        # a long prompt's cache: 0.5 GB of bf16 into 8 bits and back
+        _case("quantize", 131072, name="quantize_128k_bf16_e4m3", fmt="e4m3"),
+        # one token after a short prompt: the smallest call, latency and launches
+        _case("attend8", 1000, name="attend8_1k_int8", block=32),
+        # one token at 128K: 3 adaptive heads, 5 consistent heads of 2112 rows
+        _case("attend8", 131072, name="attend8_128k_e4m3", fmt="e4m3", n_cons=5),
+        # the largest: 2 adaptive heads over 1M tokens
+        _case("attend8", 1048576, name="attend8_1m_int8", n_cons=6, rows_cons=4160),
+        # a serving step: 16 sequences of 16K to 64K tokens, the new token appended, then attention
+        _case("step8", 65536, name="step8_batch16_e4m3", fmt="e4m3", n_min=16384, batch=16, n_cons=4, rows_cons=1088),
+        # a serving step on caches that are evicted now and then: append, attention, weights
+        _case("step8", 2304, name="step8_weights_batch16_int8", n_min=2050, batch=16, weights=True),
+        # attention with weights on a short fp32 cache
+        _case("weights", 4096, name="weights_4k_f32", dtype="f32", n_cons=4, rows_cons=288),
+        # attention with weights at 128K
+        _case("weights", 131072, name="weights_128k_bf16", n_cons=5),
+        # 16 sequences back from 2304 to 2048 rows: the eviction of a long generation
+        _case("evict", 2304, name="evict_batch16_bf16", batch=16, keep=1984),
+        # the first eviction after a 128K prompt: an eighth of the rows stays
+        _case("evict", 131072, name="evict_128k_bf16", keep=16384),
+        # the same on 8-bit caches of four 32K prompts, whole blocks at a time
+        _case("evict8", 32768, name="evict8_32k_e4m3", fmt="e4m3", batch=4, n_min=20000, cs=64, keep=4096),
+    ]
+
+
+def draw(rng):
+    """One more case of the listed ranges: 1 to 1M rows (odd ones among them), 1
+    to 16 sequences, every type, format, block and group size."""
+    op = rng.choice(["quantize", "attend8", "attend8", "step8", "step8", "weights", "evict", "evict8"])
+    dtype = rng.choice(["bf16", "bf16", "bf16", "f32"])
+    fmt, block = rng.choice(["int8", "e4m3"]), rng.choice([32, 64])
+    group, hkv = rng.choice([1, 2, 4, 4, 8]), rng.choice([1, 2, 4, 8, 8])
+    batch = rng.choice([1, 1, 2, 5, 8, 16])
+    low = 32 if op in ("attend8", "step8", "weights") else 1024
+    n = int(math.exp(rng.uniform(math.log(low), math.log(1048576))))
+    # at most so many rows in all (K and V): those of the largest listed case of the kind
+    most = {"quantize": 2 ** 20, "attend8": 2 ** 21, "step8": 2 ** 22, "weights": 2 ** 19, "evict": 2 ** 20,
+            "evict8": 2 ** 20}[op] // (2 if dtype == "f32" else 1)
+    cut = rng.uniform(0.5, 1.0)
+    n = max(low, min(n, int(cut * most / (batch * hkv))))
+    kw = {"dtype": dtype, "fmt": fmt, "block": block, "batch": batch, "hkv": hkv, "hq": hkv * group,
+          "n_min": max(1, n // rng.choice([1, 1, 2, 4])), "len_seed": rng.randint(1, 10 ** 6),
+          "weights": op == "weights" or rng.random() < 0.5}
+    if op in ("attend8", "step8", "weights"):
+        kw.update(n_cons=rng.randint(0, hkv - 1), rows_cons=rng.choice([288, 1088, 2112, 4160]))
+    if op in ("evict", "evict8"):
+        cs = rng.choice([1, 4, 8, 12, 16, 64]) if op == "evict" else block * rng.choice([1, 2])
+        kw.update(cs=cs, recent=rng.choice([0, 32, 64, 100, 256]), keep=int(n * rng.uniform(0.05, 0.95)))
+    return _case(op, n, **kw)
+
+
+def lengths(case):
+    """Rows of every sequence's full caches."""
+    if case["n_min"] >= case["n"]:
+        return [case["n"]] * case["batch"]
+    r = random.Random(case["len_seed"])
+    return [r.randint(case["n_min"], case["n"]) for _ in range(case["batch"])]
+
+
+def _dtype(case):
+    return torch.float32 if case["dtype"] == "f32" else torch.bfloat16
+
+
+def _groups(case):
+    """The views as (first head, heads, rows of each sequence, rows allocated): the
+    full caches of the adaptive heads, then the compact ones of the consistent heads."""
+    n, step = lengths(case), 1 if case["op"] == "step8" else 0
+    if step:    # the first sequence's new token completes a block
+        n[0] = max(n[0] // case["block"], 1) * case["block"] - 1
+    ad = case["hkv"] - case["n_cons"]
+    parts = [(0, ad, n)]
+    if case["n_cons"]:
+        parts.append((ad, case["n_cons"], [min(case["rows_cons"], m) for m in n]))
+    unit = 64
+    return [(h, m, r, -(-(max(r) + step) // unit) * unit) for h, m, r in parts]
+
+
+# ----------------------------------------------------------------- the inputs
+
+def _rng(seed, *key):
+    s = int(np.random.SeedSequence([int(seed), *key]).generate_state(1, np.uint64)[0] >> np.uint64(1))
+    return torch.Generator(device=DEV).manual_seed(s)
+
+
+def _rows(shape, g, heavy):
+    """[views, rows, D] in fp32, a few rows scaled up if `heavy`."""
+    x = torch.randn(shape, generator=g, device=DEV)
+    if heavy:
+        hot = torch.rand(shape[:-1], generator=g, device=DEV) < HEAVY_FRAC
+        x = torch.where(hot[..., None], x * HEAVY_SCALE, x)
+    return x
+
+
+def _codes_of(case, views, cap, g, heavy):
+    """Codes and scales as a program keeps them: rows brought into 8 bits, view by view."""
+    dt = torch.int8 if case["fmt"] == "int8" else torch.float8_e4m3fn
+    codes = torch.empty((views, cap, D), dtype=dt, device=DEV)
+    scale = torch.empty((views, cap // case["block"]), device=DEV)
+    for v in range(views):
+        x = _rows((cap // case["block"], case["block"], D), g, heavy)
+        s = x.abs().amax(dim=(1, 2)) / (127.0 if case["fmt"] == "int8" else 224.0)
+        if case["fmt"] == "e4m3":
+            s = _two(torch.frexp(s)[1] - 1).float()
+        y = x / s[:, None, None]
+        codes[v] = (y.round() if dt == torch.int8 else y).to(dt).view(cap, D)
+        scale[v] = s
+    return codes, scale
+
+
+def _group(case, seed, i, part):
+    op, dt = case["op"], _dtype(case)
+    h0, heads, rows, cap = part
+    B, V = case["batch"], case["batch"] * heads
+    g = _rng(seed, 1, i)
+    x = SimpleNamespace(h0=h0, heads=heads, rows=rows, cap=cap, block=case["block"])
+    x.lens = torch.tensor(rows, dtype=torch.int64, device=DEV)[:, None].expand(B, heads).reshape(V).contiguous()
+    if op in ("quantize", "weights", "evict"):
+        x.k, x.v = torch.empty((V, cap, D), dtype=dt, device=DEV), torch.empty((V, cap, D), dtype=dt, device=DEV)
+        for v in range(V):
+            x.k[v], x.v[v] = _rows((cap, D), g, True), _rows((cap, D), g, False)
+    if op in ("attend8", "step8", "evict8"):
+        x.kc, x.ks = _codes_of(case, V, cap, g, True)
+        x.vc, x.vs = _codes_of(case, V, cap, g, False)
+        x.kt, x.vt = _rows((V, x.block, D), g, True).to(dt), _rows((V, x.block, D), g, False).to(dt)
+    if op == "quantize":
+        f8 = torch.int8 if case["fmt"] == "int8" else torch.float8_e4m3fn
+        x.kc, x.vc = (torch.empty((V, cap, D), dtype=f8, device=DEV) for _ in "kv")
+        x.ks, x.vs = (torch.empty((V, cap // x.block), device=DEV) for _ in "kv")
+        x.kt, x.vt = (torch.zeros((V, x.block, D), dtype=dt, device=DEV) for _ in "kv")
+        x.k_out, x.v_out = torch.zeros_like(x.k), torch.zeros_like(x.v)
+    if op in ("evict", "evict8") or case["weights"] or op == "weights":
+        # weights gathered so far: a long tail, some rows that nothing attended to
+        w = torch.exp(2.0 * torch.randn((V, cap), generator=g, device=DEV) - 6.0)
+        w = w * (torch.rand((V, cap), generator=g, device=DEV) > 0.05)
+        x.acc = w * (torch.arange(cap, device=DEV) < x.lens[:, None])
+        x.acc_start = x.acc.clone()
+    if op == "step8":
+        x.k_new, x.v_new = _rows((V, D), g, False).to(dt), _rows((V, D), g, False).to(dt)
+    x.start = x.lens.clone()
+    return x
+
+
+def prepare(case, seed):
+    op = case["op"]
+    s = SimpleNamespace(case=case, groups=[_group(case, seed, i, p) for i, p in enumerate(_groups(case))])
+    if op in ("attend8", "step8", "weights"):
+        s.q = torch.randn((case["batch"], case["hq"], D), generator=_rng(seed, 2), device=DEV).to(_dtype(case))
+    if op in ("evict", "evict8"):
+        v = s.groups[0].lens.numel()
+        s.budget = torch.full((v,), max(case["keep"] // case["cs"], 0), dtype=torch.int32, device=DEV)
+    if own:
+        _plan(s)
+    return s
+
+
+# ---------------------------------------------------- the framework's own calls
+
+def _flat(s, name):
+    """One value per view, [batch][hkv] as the framework orders them."""
+    B = s.case["batch"]
+    return torch.cat([getattr(x, name).view(B, x.heads, *getattr(x, name).shape[1:]) for x in s.groups], dim=1)
+
+
+def _per_view(s, *names):
+    """Device addresses of the named tensors of every view, [batch][hkv]."""
+    got = []
+    for b in range(s.case["batch"]):
+        for x in s.groups:
+            for h in range(x.heads):
+                got.append(tuple(getattr(x, n)[b * x.heads + h].data_ptr() for n in names))
+    return got
+
+
+def _plan(s):
+    """Tables, lengths, plan and workspaces that a program keeps."""
+    import paper_2608_30295_amd as ck
+    case, op = s.case, s.case["op"]
+    s.lens = _flat(s, "lens").contiguous()
+    s.start = s.lens.clone()
+    s.max_rows = max(x.cap for x in s.groups)
+    if op in ("quantize", "weights", "evict"):
+        s.kv = ck.kv_table(_per_view(s, "k", "v"), DEV)
+    if op == "quantize":
+        s.kv_out = ck.kv_table(_per_view(s, "k_out", "v_out"), DEV)
+    if op in ("quantize", "attend8", "step8", "evict8"):
+        s.q8 = ck.q8_views(_per_view(s, "kc", "vc", "ks", "vs", "kt", "vt"), DEV, fmt=case["fmt"],
+                           block=case["block"], dtype=_dtype(case))
+    s.acc = ck.acc_table([p for p, in _per_view(s, "acc")], DEV) if hasattr(s.groups[0], "acc") else None
+    if op in ("attend8", "step8", "weights"):
+        room = 1 if op == "step8" else 0
+        most = s.lens.cpu().numpy() + room
+        s.plan = ck.decode_plan(most, case["hq"], case["hkv"], DEV)
+        s.ws = ck.workspace(ck.weights_workspace(most, case["hq"], case["hkv"]), DEV) if s.acc is not None else None
+    if op == "step8":
+        s.capacity = torch.tensor([[x.cap for x in s.groups for _ in range(x.heads)]] * case["batch"],
+                                  dtype=torch.int64, device=DEV)
+        s.k_new, s.v_new = _flat(s, "k_new").contiguous(), _flat(s, "v_new").contiguous()
+    if op in ("evict", "evict8"):
+        s.ws = ck.workspace(ck.evict_workspace(s.lens.numel(), s.max_rows, case["cs"]), DEV)
+
+
+def _run_own(s):
+    import paper_2608_30295_amd as ck
+    case, op = s.case, s.case["op"]
+    if op == "quantize":
+        ck.quantize_kv(s.kv, s.lens, s.q8, s.max_rows)
+        ck.dequantize_kv(s.q8, s.lens, s.kv_out, s.max_rows)
+        return [(x.k_out, x.v_out) for x in s.groups]
+    if op == "attend8":
+        return ck.decode_attn_q8(s.plan, s.q, s.q8, s.lens, acc=s.acc, ws=s.ws), _accs(s)
+    if op == "weights":
+        return ck.decode_attn_weights(s.plan, s.q, s.kv, s.lens, s.acc, ws=s.ws), _accs(s)
+    # bookkeeping rolled back to the pass's start, so that every pass is the same one
+    s.lens.copy_(s.start)
+    if op == "step8":
+        ck.append_kv_q8(s.q8, s.capacity, s.lens, s.k_new, s.v_new)
+        return ck.decode_attn_q8(s.plan, s.q, s.q8, s.lens, acc=s.acc, ws=s.ws), _cache(s), _accs(s), s.lens
+    x = s.groups[0]
+    x.acc.copy_(x.acc_start)
+    if op == "evict":
+        ck.evict_kv(s.kv, s.lens, s.acc, s.budget, cs=case["cs"], recent=case["recent"], max_rows=s.max_rows,
+                    dtype=x.k.dtype, ws=s.ws)
+        return x.k, x.v, x.acc, s.lens
+    ck.evict_kv_q8(s.q8, s.lens, s.acc, s.budget, cs=case["cs"], recent=case["recent"], max_rows=s.max_rows, ws=s.ws)
+    return _cache(s), x.acc, s.lens
+
+
+def _accs(s):
+    return [x.acc for x in s.groups if hasattr(x, "acc")]
+
+
+def _cache(s):
+    return [(x.kc, x.vc, x.ks, x.vs, x.kt, x.vt) for x in s.groups]
+
+
+# ------------------------------------------------------------- the plain forms
+
+def _two(e):
+    """2^e in 64 bits, exactly (a device's pow() may be off by a bit)."""
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
+def _quantize(x, fmt):
+    """Blocks [..., block, D] -> the codes' values and their scales [...]."""
+    big = x.float().abs().amax(dim=(-2, -1))
+    if fmt == "int8":
+        scale = big * (1.0 / 127.0)
+    else:       # big = m 2^e with m in [1/2, 1): 448 = 7/8 2^9
+        m, e = torch.frexp(big)
+        scale = _two(e - 9 + (m > 0.875).to(e.dtype)).float()
+    scale = torch.where(big < TINY, torch.zeros_like(scale), scale)
+    div = torch.where(scale > 0, scale, torch.ones_like(scale))
+    y = x.double() / div.double()[..., None, None]     # 64 bits: quotients next to a border
+    if fmt == "int8":
+        y = y.round().clamp(-127, 127)
+    else:       # 3 bits behind the leading one, from 2^-6 on; below, steps of 2^-9
+        _, e = torch.frexp(y)
+        step = _two((e - 1).clamp(min=-6) - 3)
+        y = (y / step).round() * step
+    return torch.where((scale > 0)[..., None, None], y, torch.zeros_like(y)).float(), scale
+
+
+def _values(codes, scale, block):
+    V, cap, _ = codes.shape
+    return (codes.float().view(V, cap // block, block, D) * scale[:, :, None, None]).view(V, cap, D)
+
+
+def _softmax(q, k, mask):
+    """q [V, G, D], k [V, R, D], mask [V, R] -> weights [V, G, R] and log-sum-exp."""
+    s = torch.bmm(q, k.transpose(1, 2)) * (1.0 / math.sqrt(D))
+    s = torch.where(mask[:, None, :], s, s.new_full((), -math.inf))
+    m = s.amax(dim=2, keepdim=True)
+    p = torch.exp(s - torch.where(torch.isinf(m), torch.zeros_like(m), m))
+    l = p.sum(dim=2, keepdim=True)
+    return p / torch.where(l > 0, l, torch.ones_like(l)), (m + torch.log(l))[:, :, 0]
+
+
+def _head_rows(s, x):
+    """The queries of a group's views, [views, G, D]."""
+    G = s.case["hq"] // s.case["hkv"]
+    q = s.q.float().view(s.case["batch"], s.case["hkv"], G, D)[:, x.h0:x.h0 + x.heads]
+    return q.reshape(-1, G, D)
+
+
+def _join(s, parts):
+    """[views, G, ...] of every group -> [batch, hq, ...]."""
+    B = s.case["batch"]
+    parts = [p.view(B, x.heads, *p.shape[1:]) for x, p in zip(s.groups, parts)]
+    return torch.cat(parts, dim=1).reshape(B, s.case["hq"], *parts[0].shape[3:])
+
+
+def _attend8(s, x):
+    """Attention of one group over its codes and its tail; the weights into x.acc."""
+    cap, block = x.cap, x.block
+    whole = x.lens // block * block
+    in_codes = torch.arange(cap, device=DEV) < whole[:, None]
+    in_tail = torch.arange(block, device=DEV) < (x.lens - whole)[:, None]
+    k = torch.cat([_values(x.kc, x.ks, block), x.kt.float()], dim=1)
+    p, lse = _softmax(_head_rows(s, x), k, torch.cat([in_codes, in_tail], dim=1))
+    del k
+    v = torch.cat([_values(x.vc, x.vs, block), torch.where(in_tail[..., None], x.vt.float(), 0.0)], dim=1)
+    out = torch.bmm(p, v)
+    if hasattr(x, "acc"):
+        w = p.mean(dim=1)
+        x.acc += w[:, :cap]
+        at = (whole[:, None] + torch.arange(block, device=DEV)).clamp(max=cap - 1)
+        x.acc.scatter_add_(1, at, torch.where(in_tail, w[:, cap:], 0.0))
+    return out, lse
+
+
+def _attend(s, x):
+    """The same over rows in the cache's own type."""
+    p, lse = _softmax(_head_rows(s, x), x.k.float(), torch.arange(x.cap, device=DEV) < x.lens[:, None])
+    x.acc += p.mean(dim=1)
+    return torch.bmm(p, x.v.float()), lse
+
+
+def _append(x, fmt):
+    """The new rows into the tails; a tail that is full becomes a block."""
+    views, at = torch.arange(x.lens.numel(), device=DEV), x.lens % x.block
+    x.kt[views, at], x.vt[views, at] = x.k_new, x.v_new
+    full, to = at == x.block - 1, x.lens // x.block
+    _close(x.kc, x.ks, x.kt, full, to, fmt)
+    _close(x.vc, x.vs, x.vt, full, to, fmt)
+    x.lens += 1
+
+
+def _close(codes, scale, tail, full, to, fmt):
+    V, block, _ = tail.shape
+    views, blocks = torch.arange(V, device=DEV), codes.view(torch.int8).view(V, -1, block, D)
+    y, s = _quantize(tail, fmt)
+    blocks[views, to] = torch.where(full[:, None, None], y.to(codes.dtype).view(torch.int8), blocks[views, to])
+    scale[views, to] = torch.where(full, s, scale[views, to])
+
+
+def _survivors(acc, lens, budget, cs, recent):
+    """Which row each row of a view takes its content from, and the new lengths.
+    The L rows are chunks of cs, as many as lie wholly before the last `recent`;
+    the `budget` of them with the largest weight (that of their best row; ties to
+    the lower chunk) stay.  Kept chunks below the count of kept ones do not move;
+    the others take, in order, the places of the chunks that go; the rows behind
+    the chunks follow."""
+    V, cap = acc.shape
+    N = cap // cs
+    nc = (lens - recent).clamp(min=0) // cs
+    k = torch.where(budget < 0, nc, torch.minimum(budget.long(), nc))
+    at = torch.arange(N, device=DEV).expand(V, N)
+    score = acc[:, :N * cs].reshape(V, N, cs).amax(dim=2)
+    score = torch.where(at < nc[:, None], score, score.new_full((), -math.inf))
+    order = torch.sort(score, dim=1, descending=True, stable=True).indices
+    keep = torch.empty_like(order).scatter_(1, order, at) < k[:, None]
+    hole, mover = ~keep & (at < k[:, None]), keep & (at >= k[:, None])
+    spare = torch.full_like(at, N)
+    by_rank = torch.zeros((V, N + 1), dtype=torch.int64, device=DEV)
+    by_rank.scatter_(1, torch.where(mover, mover.cumsum(1) - 1, spare), at)
+    source = torch.where(hole, by_rank.gather(1, (hole.cumsum(1) - 1).clamp(min=0)), at)
+    t = torch.arange(cap, device=DEV).expand(V, cap)
+    chunk = (t // cs).clamp(max=N - 1)
+    after = lens - (nc - k) * cs
+    row = torch.where(t < (k * cs)[:, None], source.gather(1, chunk) * cs + t % cs, t + ((nc - k) * cs)[:, None])
+    return torch.where(t < after[:, None], row, t), after
+
+
+def _evict(x, budget, case, eight):
+    row, after = _survivors(x.acc, x.lens, budget, case["cs"], case["recent"])
+    views, t = torch.arange(x.lens.numel(), device=DEV)[:, None], torch.arange(x.cap, device=DEV)
+    x.acc.copy_(torch.where((t >= after[:, None]) & (t < x.lens[:, None]), 0.0, x.acc[views, row]))
+    if eight:       # whole blocks with their scales; the tails stay
+        block = x.block
+        row = torch.where(t < (after // block * block)[:, None], row, t)
+        at = row[:, ::block] // block
+        x.kc.view(torch.int8).copy_(x.kc.view(torch.int8)[views, row])
+        x.vc.view(torch.int8).copy_(x.vc.view(torch.int8)[views, row])
+        x.ks.copy_(x.ks[views, at])
+        x.vs.copy_(x.vs[views, at])
+    else:
+        x.k.copy_(x.k[views, row])
+        x.v.copy_(x.v[views, row])
+    x.lens.copy_(after)
+
+
+def _round_trip(x, fmt):
+    """Whole blocks through the codes, the rest as it is; rows behind the length stay."""
+    V, cap, block = x.lens.numel(), x.cap, x.block
+    t = torch.arange(cap, device=DEV)[None, :, None]
+    whole, lens = (x.lens // block * block)[:, None, None], x.lens[:, None, None]
+    return [_restored(a, b, V, cap, block, t < whole, t < lens, fmt) for a, b in ((x.k, x.k_out), (x.v, x.v_out))]
+
+
+def _restored(a, b, V, cap, block, coded, valid, fmt):
+    y, s = _quantize(a.view(V, cap // block, block, D), fmt)
+    y = (y * s[..., None, None]).view(V, cap, D).to(a.dtype)
+    b.copy_(torch.where(coded, y, torch.where(valid, a, b)))
+    return b
+
+
+def _run_plain(s):
+    case, op = s.case, s.case["op"]
+    if op == "quantize":
+        return [tuple(_round_trip(x, case["fmt"])) for x in s.groups]
+    if op in ("attend8", "weights"):
+        got = [(_attend8 if op == "attend8" else _attend)(s, x) for x in s.groups]
+        return (_join(s, [o for o, _ in got]), _join(s, [l for _, l in got])), _accs(s)
+    _ = [x.lens.copy_(x.start) for x in s.groups]
+    if op == "step8":
+        _ = [_append(x, case["fmt"]) for x in s.groups]
+        got = [_attend8(s, x) for x in s.groups]
+        out = _join(s, [o for o, _ in got]), _join(s, [l for _, l in got])
+        return out, _cache(s), _accs(s), _flat(s, "lens")
+    x = s.groups[0]
+    x.acc.copy_(x.acc_start)
+    _evict(x, s.budget, case, op == "evict8")
+    lens = _flat(s, "lens")
+    return (x.k, x.v, x.acc, lens) if op == "evict" else (_cache(s), x.acc, lens)
+
+
+def run(s):
+    return _run_own(s) if own else _run_plain(s)
+
+
+# --------------------------------------------------------------- what it takes
+
+def work(case):
+    """Bytes and operations of one pass: every input that the result depends on
+    read once, every output written once."""
+    op, G, block, cs = case["op"], case["hq"] // case["hkv"], case["block"], case["cs"]
+    size = 4 if case["dtype"] == "f32" else 2
+    row, io = D * size, case["batch"] * case["hq"] * (D * size + D * 4 + 4)
+    total = sum(m * r for _, m, rows, _ in _groups(case) for r in rows)
+    views = case["batch"] * case["hkv"]
+    coded = sum(m * (r // block * block) for _, m, rows, _ in _groups(case) for r in rows)
+    eight = coded * (2 * D + 8 / block)
+    rest = (total - coded) * 2 * row
+    if op == "quantize":
+        return {"bytes": total * 4 * row + 2 * eight + 2 * rest, "flops": 6.0 * coded * D}
+    adds = total * 8 if case["weights"] or op == "weights" else 0
+    if op == "attend8":
+        return {"bytes": eight + rest + io + adds, "flops": 4.0 * total * G * D}
+    if op == "step8":
+        return {"bytes": eight + rest + io + adds + views * 4 * row, "flops": 4.0 * total * G * D}
+    if op == "weights":
+        return {"bytes": total * 2 * row + io + adds, "flops": 4.0 * total * G * D}
+    # every weight read; the chunks that change their place, with their weights, read and written
+    size = 2 * row + 4 if op == "evict" else 2 * D + 8 / block + 4
+    moved = 0.0
+    for _, m, rows, _ in _groups(case):
+        for r in rows:
+            nc = max(r - case["recent"], 0) // cs
+            k = min(case["keep"] // cs, nc)
+            moved += m * (k * (nc - k) / max(nc, 1) * cs + (r - nc * cs if k < nc else 0))
+    return {"bytes": total * 4 + 2 * moved * size + 16 * views, "flops": float(total)}
+
+
+# -------------------------------------------------------- the results, 64 bits
+
+E4M3 = sorted([m / 8 * 2.0 ** -6 for m in range(8)] + [(1 + m / 8) * 2.0 ** e for e in range(-6, 9) for m in range(8)
+                                                      if not (e == 8 and m == 7)])
+
+
+def _exact_block(x, fmt):
+    """One block's values in 64 bits (their codes times the scale), and the codes and scale."""
+    x = x.double()
+    big = float(x.abs().max())
+    if big < TINY:
+        return torch.zeros_like(x), torch.zeros_like(x), 0.0
+    if fmt == "int8":
+        scale = float(np.float32(big) * np.float32(1.0 / 127.0))
+        y = torch.round(x / scale).clamp(-127, 127)
+    else:
+        scale = 2.0 ** math.ceil(math.log2(big) - 1)
+        while big <= 448 * scale / 2:
+            scale /= 2
+        while big > 448 * scale:
+            scale *= 2
+        grid = torch.tensor(E4M3, dtype=torch.float64, device=x.device)
+        a = (x / scale).abs()
+        at = torch.searchsorted(grid, a.contiguous()).clamp(1, len(E4M3) - 1)
+        lo, hi = grid[at - 1], grid[at]
+        up = (a - lo > hi - a) | ((a - lo == hi - a) & (at % 2 == 0))
+        y = torch.where(up, hi, lo) * torch.sign(x)
+    return y * scale, y, scale
+
+
+def _exact_quantize(case, s):
+    got = []
+    for x in s.groups:
+        pair = []
+        for a in (x.k, x.v):
+            b = torch.zeros(a.shape, dtype=torch.float64, device=DEV)
+            for v, r in enumerate([r for r in x.rows for _ in range(x.heads)]):
+                whole = r // x.block * x.block
+                b[v, whole:r] = a[v, whole:r].double()
+                if not whole:
+                    continue
+                # all blocks of a view at once: rows of a block side by side
+                y = a[v, :whole].double().view(-1, x.block * D)
+                if case["fmt"] == "int8":
+                    big = y.abs().amax(dim=1)
+                    sc = torch.from_numpy(big.cpu().numpy().astype(np.float32) * np.float32(1.0 / 127.0))
+                    sc = sc.double().to(DEV)[:, None]
+                    y = torch.round(y / sc).clamp(-127, 127) * sc
+                else:
+                    big = y.abs().amax(dim=1).cpu().numpy()
+                    sc = np.exp2(np.round(np.log2(big / 448)))
+                    sc = np.where(448 * sc < big, 2 * sc, np.where(224 * sc >= big, sc / 2, sc))
+                    sc = torch.from_numpy(sc).to(DEV)[:, None]
+                    grid = torch.tensor(E4M3, dtype=torch.float64, device=DEV)
+                    w = (y / sc).abs()
+                    at = torch.searchsorted(grid, w).clamp(1, len(E4M3) - 1)
+                    lo, hi = grid[at - 1], grid[at]
+                    up = (w - lo > hi - w) | ((w - lo == hi - w) & (at % 2 == 0))
+                    y = torch.where(up, hi, lo) * torch.sign(y) * sc
+                b[v, :whole] = y.view(whole, D)
+            pair.append(b)
+        got.append(tuple(pair))
+    return got
+
+
+def _exact_view(q, k, v):
+    """Queries [G, D] over rows k, v in 64 bits: output, log-sum-exp and the rows' mean weight."""
+    if not len(k):
+        return q.new_zeros(q.shape), q.new_full((len(q),), -math.inf), q.new_zeros(0)
+    s = q @ k.t() / math.sqrt(D)
+    lse = torch.logsumexp(s, dim=1)
+    p = torch.exp(s - lse[:, None])
+    return p @ v, lse, p.mean(dim=0)
+
+
+def _exact_attention(case, s):
+    B, hq, G = case["batch"], case["hq"], case["hq"] // case["hkv"]
+    out = torch.zeros((B, hq, D), dtype=torch.float64, device=DEV)
+    lse = torch.zeros((B, hq), dtype=torch.float64, device=DEV)
+    accs, caches = [], []
+    lens = torch.zeros((B, case["hkv"]), dtype=torch.int64, device=DEV)
+    for x in s.groups:
+        acc = x.acc.double() if hasattr(x, "acc") else None
+        for b in range(B):
+            for h in range(x.heads):
+                i, r = b * x.heads + h, x.rows[b]
+                if case["op"] == "weights":
+                    k, v = x.k[i, :r].double(), x.v[i, :r].double()
+                else:
+                    if case["op"] == "step8":
+                        x.kt[i, r % x.block], x.vt[i, r % x.block] = x.k_new[i], x.v_new[i]
+                        if r % x.block == x.block - 1:
+                            j = r // x.block
+                            for c, sc, t in ((x.kc, x.ks, x.kt), (x.vc, x.vs, x.vt)):
+                                _, y, one = _exact_block(t[i], case["fmt"])
+                                c[i, j * x.block:(j + 1) * x.block] = y.float().to(c.dtype)
+                                sc[i, j] = one
+                        r += 1
+                    w = r // x.block * x.block
+                    k, v = ((c[i, :w].float().double().view(-1, x.block * D) * sc[i, :w // x.block, None].double())
+                            .view(w, D) for c, sc in ((x.kc, x.ks), (x.vc, x.vs)))
+                    k, v = torch.cat([k, x.kt[i, :r - w].double()]), torch.cat([v, x.vt[i, :r - w].double()])
+                at = slice((x.h0 + h) * G, (x.h0 + h + 1) * G)
+                out[b, at], lse[b, at], p = _exact_view(s.q[b, at].double(), k, v)
+                lens[b, x.h0 + h] = r
+                if acc is not None:
+                    acc[i, :r] += p
+        accs += [acc] if acc is not None else []
+        caches.append((x.kc, x.vc, x.ks, x.vs, x.kt, x.vt) if case["op"] == "step8" else ())
+    return ((out, lse), caches, accs, lens) if case["op"] == "step8" else ((out, lse), accs)
+
+
+def _exact_evict(case, s):
+    """Row by row lists on the host; the content is moved as it is."""
+    x, cs = s.groups[0], case["cs"]
+    acc, lens = x.acc.cpu().numpy().copy(), x.lens.cpu().numpy().copy()
+    for v in range(len(lens)):
+        L = int(lens[v])
+        nc = max(L - case["recent"], 0) // cs
+        k = min(int(s.budget[v]), nc)
+        best = acc[v, :nc * cs].reshape(nc, cs).max(axis=1) if nc else np.zeros(0, np.float32)
+        stay = np.sort(np.lexsort((np.arange(nc), -best))[:k])
+        source = np.arange(k)
+        source[np.setdiff1d(np.arange(k), stay)] = stay[stay >= k]
+        rows = np.concatenate([(source[:, None] * cs + np.arange(cs)).reshape(-1), np.arange(nc * cs, L)])
+        new = len(rows)
+        acc[v, :new], acc[v, new:L] = acc[v, rows], 0.0
+        if case["op"] == "evict":
+            at = torch.from_numpy(rows).to(DEV)
+            x.k[v, :new], x.v[v, :new] = x.k[v, at], x.v[v, at]
+        else:
+            whole = new // x.block
+            at = torch.from_numpy(rows[:whole * x.block:x.block] // x.block).to(DEV)
+            for c, sc in ((x.kc, x.ks), (x.vc, x.vs)):
+                b = c[v].view(torch.uint8).view(-1, x.block * D)
+                b[:whole], sc[v, :whole] = b[at], sc[v, at]
+        lens[v] = new
+    acc, lens = torch.from_numpy(acc).to(DEV), torch.from_numpy(lens).to(DEV).view(case["batch"], -1)
+    return (x.k, x.v, acc, lens) if case["op"] == "evict" else (_cache(s), acc, lens)
+
+
+def exact(case, seed):
+    """What run() returns for these inputs, from the definitions in 64 bits."""
+    s = prepare(case, seed)
+    if case["op"] == "quantize":
+        return _exact_quantize(case, s)
+    return (_exact_evict if case["op"] in ("evict", "evict8") else _exact_attention)(case, s)
