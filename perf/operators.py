@@ -237,7 +237,7 @@ def _plan(s):
         room = 1 if op == "step8" else 0
         most = s.lens.cpu().numpy() + room
         s.plan = ck.decode_plan(most, case["hq"], case["hkv"], DEV)
-        s.ws = ck.workspace(ck.weights_workspace(most, case["hq"], case["hkv"]), DEV) if s.acc is not None else None
+        s.ws = ck.workspace(ck.weights_workspace(s.plan), DEV) if s.acc is not None else None
     if op == "step8":
         s.capacity = torch.tensor([[x.cap for x in s.groups for _ in range(x.heads)]] * case["batch"],
                                   dtype=torch.int64, device=DEV)
