@@ -22,3 +22,18 @@ from .binding import (  # noqa: F401
     select_workspace,
     workspace,
 )
+from .cache import (  # noqa: F401
+    Q8Views,
+    acc_table,
+    append_kv_q8,
+    decode_attn_q8,
+    decode_attn_weights,
+    dequantize_kv,
+    evict_kv,
+    evict_kv_q8,
+    evict_workspace,
+    q8_alloc,
+    q8_views,
+    quantize_kv,
+    weights_workspace,
+)

@@ -70,6 +70,28 @@ SIGNATURES = {
     "catekv_version": (ctypes.c_char_p, []),
 }
 
+# include/catekv_cache.h
+CATEKV_I8 = 0
+CATEKV_E4M3 = 1
+CACHE_SIGNATURES = {
+    "catekv_q8_quantize": (c_int, [c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_int, c_i64, c_int, c_void_p]),
+    "catekv_q8_dequantize": (c_int, [c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_int, c_i64, c_int, c_void_p]),
+    "catekv_q8_append": (c_int, [c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int,
+                                 c_int, c_void_p, c_void_p]),
+    "catekv_weights_workspace": (c_size, [ctypes.POINTER(DecodePlanT)]),
+    "catekv_q8_decode_attn": (c_int, [c_int, c_int, c_int, ctypes.POINTER(DecodePlanT), c_void_p, c_void_p, c_void_p,
+                                      c_int, c_int, c_int, c_int, c_float, c_void_p, c_void_p, c_void_p, c_float,
+                                      c_void_p, c_size, c_void_p, c_size, c_void_p]),
+    "catekv_decode_attn_weights": (c_int, [c_int, ctypes.POINTER(DecodePlanT), c_void_p, c_void_p, c_void_p, c_int,
+                                           c_int, c_int, c_int, c_float, c_void_p, c_void_p, c_void_p, c_float,
+                                           c_void_p, c_size, c_void_p, c_size, c_void_p]),
+    "catekv_evict_workspace": (c_size, [c_int, c_i64, c_int]),
+    "catekv_evict_kv": (c_int, [c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_i64, c_int, c_int, c_int,
+                                c_void_p, c_size, c_void_p]),
+    "catekv_q8_evict": (c_int, [c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_i64, c_int, c_int, c_int,
+                                c_void_p, c_size, c_void_p]),
+}
+
 _lib = None
 
 
@@ -87,7 +109,7 @@ def lib() -> ctypes.CDLL:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing; build it with `python -m paper_2608_30295_amd.build`")
         L = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in SIGNATURES.items():
+        for name, (res, args) in {**SIGNATURES, **CACHE_SIGNATURES}.items():
             fn = getattr(L, name)
             fn.restype = res
             fn.argtypes = args

@@ -18,8 +18,9 @@ LIB = os.path.join(HERE, "libcatekv.so")
 ARCH = "gfx950"
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
-HIP_SOURCES = ["decode.hip", "prefill.hip", "retrieve.hip", "score_rowstats.hip", "score_colmass.hip", "score_obs.hip", "score_obsb.hip", "cv.hip"]
-HOST_SOURCES = ["api.cpp"]
+HIP_SOURCES = ["decode.hip", "prefill.hip", "retrieve.hip", "score_rowstats.hip", "score_colmass.hip", "score_obs.hip", "score_obsb.hip", "cv.hip",
+               "q8.hip", "attend_dense.hip", "attend_i8.hip", "attend_e4m3.hip", "evict.hip"]
+HOST_SOURCES = ["api.cpp", "cache_api.cpp"]
 
 # Packed fp32 ops are kept out of the device code: hipcc only emits them when
 # asked, and the build never asks.

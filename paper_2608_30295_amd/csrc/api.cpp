@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "catekv.h"
+#include "cache.h"
 #include "internal.h"
 
 namespace {
@@ -256,6 +257,32 @@ catekv::ScoreGeom score_geom(int hq, int hkv, int lq, int64_t n, int64_t l_init,
 }
 
 }  // namespace
+
+namespace catekv {
+
+int host_error(int code, const char* msg) { return fail(code, "%s", msg); }
+int host_ok() { return ok(); }
+int host_check_heads(int hq, int hkv, int d) { return check_heads(hq, hkv, d); }
+int host_check_ws(const void* ws, size_t ws_bytes, size_t need) { return check_ws(ws, ws_bytes, need); }
+bool host_plan_valid(const catekv_decode_plan_t* plan) { return plan && plan->magic == kPlanMagic; }
+
+DecodeArgs host_plan_args(const catekv_decode_plan_t* plan, void* ws) {
+  char* w = reinterpret_cast<char*>(ws);
+  DecodeArgs a{};
+  a.items = reinterpret_cast<const DecodeItem*>(w + plan->segs_off);
+  a.worker_seg = reinterpret_cast<const int32_t*>(w + plan->workers_off);
+  a.v2items = reinterpret_cast<const V2Item*>(w + v2_items_off(plan->segs_off, plan->n_segments));
+  a.views = reinterpret_cast<const ViewInfo*>(w + plan->views_off);
+  a.slots = reinterpret_cast<float*>(w + plan->slots_off);
+  a.n_workers = plan->n_workers;
+  a.n_multi = plan->n_multi;
+  a.n_views = plan->batch * plan->hkv;
+  a.hkv = plan->hkv;
+  a.variant = plan->variant;
+  return a;
+}
+
+}  // namespace catekv
 
 extern "C" {
 
@@ -527,21 +554,10 @@ int catekv_decode_attn(int dtype, const catekv_decode_plan_t* plan, const void* 
     return fail(CATEKV_ERR_INVALID_ARG, "scale=%g must be positive and finite", (double)scale);
   rc = check_ws(ws, ws_bytes, plan->ws_bytes);
   if (rc) return rc;
-  char* w = reinterpret_cast<char*>(ws);
-  catekv::DecodeArgs a{};
+  catekv::DecodeArgs a = catekv::host_plan_args(plan, ws);
   a.q = q;
   a.kv = kv;
   a.lens = lens;
-  a.items = reinterpret_cast<const catekv::DecodeItem*>(w + plan->segs_off);
-  a.worker_seg = reinterpret_cast<const int32_t*>(w + plan->workers_off);
-  a.v2items = reinterpret_cast<const catekv::V2Item*>(w + v2_items_off(plan->segs_off, plan->n_segments));
-  a.views = reinterpret_cast<const catekv::ViewInfo*>(w + plan->views_off);
-  a.slots = reinterpret_cast<float*>(w + plan->slots_off);
-  a.n_workers = plan->n_workers;
-  a.n_multi = plan->n_multi;
-  a.n_views = batch * hkv;
-  a.hkv = hkv;
-  a.variant = plan->variant;
   a.scale = scale;
   a.out = out;
   a.lse = lse;

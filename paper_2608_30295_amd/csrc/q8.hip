@@ -1,0 +1,294 @@
+// Caches in 8 bits: rows into codes with a scale per block of rows, back, and
+// the append of a step's token.
+//
+// All three move bytes and little else (quantize: 2 row bytes read and one
+// written per element pair), so a wave takes one block of K or of V whole: the
+// rows go through its registers once, the maximum is taken of the bit patterns
+// on the way, and the codes leave in 8-byte stores, eight elements per lane.
+#include "cache.h"
+#include "common.h"
+
+namespace catekv {
+
+constexpr float kTinyMax = 7.888609052210118e-31f;   // 2^-100
+constexpr int kQ8Waves = 4;
+
+typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
+
+// Eight consecutive elements as fp32.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<uint16_t> {
+  uint4 w;
+  __device__ __forceinline__ void load(const void* p) { w = ldg16(p); }
+  __device__ __forceinline__ void store(void* p) const { *reinterpret_cast<uint4*>(p) = w; }
+  __device__ __forceinline__ float get(int i) const {
+    const uint32_t x = i < 2 ? w.x : i < 4 ? w.y : i < 6 ? w.z : w.w;
+    return i & 1 ? bf16_hi(x) : bf16_lo(x);
+  }
+  __device__ __forceinline__ void set(const float (&f)[8]) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{f[0], f[1]}), b2));
+    w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{f[2], f[3]}), b2));
+    w.z = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{f[4], f[5]}), b2));
+    w.w = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{f[6], f[7]}), b2));
+  }
+};
+template <>
+struct Eight<float> {
+  uint4 w[2];
+  __device__ __forceinline__ void load(const void* p) {
+    w[0] = ldg16(p);
+    w[1] = ldg16(reinterpret_cast<const char*>(p) + 16);
+  }
+  __device__ __forceinline__ void store(void* p) const {
+    reinterpret_cast<uint4*>(p)[0] = w[0];
+    reinterpret_cast<uint4*>(p)[1] = w[1];
+  }
+  __device__ __forceinline__ float get(int i) const {
+    const uint4& q = w[i >> 2];
+    const int j = i & 3;
+    return __uint_as_float(j == 0 ? q.x : j == 1 ? q.y : j == 2 ? q.z : q.w);
+  }
+  __device__ __forceinline__ void set(const float (&f)[8]) {
+    w[0] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    w[1] = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
+  }
+};
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const uint32_t y = (uint32_t)__builtin_amdgcn_ds_bpermute(((int)__lane_id() ^ o) << 2, (int)x);
+    x = x > y ? x : y;
+  }
+  return x;
+}
+
+// Scale of a block whose largest |x| has these bits, and its reciprocal (0 for a
+// block that is all 0 or not finite: its codes are 0).
+template <int FMT>
+__device__ __forceinline__ void block_scale(uint32_t big, float& scale, float& inv) {
+  scale = inv = 0.f;
+  if (big >= 0x7f800000u) {
+    scale = __uint_as_float(0x7fc00000u);
+  } else if (__uint_as_float(big) >= kTinyMax) {
+    if constexpr (FMT == CATEKV_I8) {
+      scale = __uint_as_float(big) * (1.0f / 127.0f);
+      inv = 1.0f / scale;
+    } else {
+      // 448 = 1.75 * 2^8: m / 2^8, one power more if its fraction is above 1.75
+      const uint32_t e = (big >> 23) - 8 + ((big & 0x7fffffu) > 0x600000u ? 1 : 0);
+      scale = __uint_as_float(e << 23);
+      inv = __uint_as_float((254u - e) << 23);
+    }
+  }
+}
+
+// Codes of eight elements.  int8: x inv is within 2^-15 of the quotient x / scale,
+// which decides the rounding except next to a border between two codes; such
+// elements (1 in 10^4) are divided in fp64, whose quotient lies on a border only
+// if the exact one does.  e4m3: x inv is exact, the conversion rounds to nearest even.
+template <int FMT, typename T>
+__device__ __forceinline__ uint2 block_codes(const Eight<T>& x, float scale, float inv) {
+  if constexpr (FMT == CATEKV_I8) {
+    float r[8];
+    float off = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float y = x.get(i) * inv;
+      r[i] = __builtin_rintf(y);
+      off = fmaxf(off, fabsf(y - r[i]));
+    }
+    if (__builtin_amdgcn_ballot_w64(off > 0.4999f)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        r[i] = (float)__builtin_rint((double)x.get(i) / (double)scale);
+    }
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      w[h] = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[h] |= ((uint32_t)(int)r[4 * h + i] & 0xffu) << (8 * i);
+    }
+    return make_uint2(w[0], w[1]);
+  } else {
+    int w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(x.get(4 * h) * inv, x.get(4 * h + 1) * inv, 0, false);
+      w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(x.get(4 * h + 2) * inv, x.get(4 * h + 3) * inv, w[h], true);
+    }
+    return make_uint2((uint32_t)w[0], (uint32_t)w[1]);
+  }
+}
+
+// One block by one wave: lane takes dims 8 (lane % 16) .. of the rows lane / 16,
+// lane / 16 + 4, ...  `row(r)`: address of the block's row r.
+template <int FMT, typename T, int BLOCK, typename Row>
+__device__ __forceinline__ void quantize_block(Row row, uint8_t* codes, float* scale_out) {
+  const int lane = threadIdx.x & 63, d0 = (lane & 15) * 8, r0 = lane >> 4;
+  constexpr int N = BLOCK / 4;
+  Eight<T> x[N];
+  uint32_t big = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i].load(row(r0 + 4 * i) + d0 * sizeof(T));
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t b = __float_as_uint(x[i].get(j)) & 0x7fffffffu;
+      big = big > b ? big : b;
+    }
+  float scale, inv;
+  block_scale<FMT>(wave_max(big), scale, inv);
+  const bool zero = inv == 0.f;                    // 0 * inf is not 0
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    uint2 c = make_uint2(0, 0);
+    if (!zero) c = block_codes<FMT, T>(x[i], scale, inv);
+    *reinterpret_cast<uint2*>(codes + (r0 + 4 * i) * kD + d0) = c;
+  }
+  if (lane == 0) *scale_out = scale;
+}
+
+// grid: (groups of kQ8Waves blocks x views, views fastest; 1; K and V).  The wave
+// behind a view's last whole block copies the remaining rows into the tail.
+template <int FMT, typename T, int BLOCK>
+__global__ __launch_bounds__(kQ8Waves * 64) void q8_quantize_kernel(Q8Args a) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int group = blockIdx.x / a.n_views, bh = blockIdx.x - group * a.n_views;
+  const bool is_v = blockIdx.z;
+  const int64_t len = a.lens[bh];
+  if (len < 0 || len > a.max_rows) return;
+  const int64_t whole = len / BLOCK, blk = (int64_t)group * kQ8Waves + wave;
+  if (blk > whole) return;
+  const catekv_q8_view view = a.views[bh];
+  const catekv_kv_ptrs kv = a.kv[bh];
+  const char* src = reinterpret_cast<const char*>(is_v ? kv.v : kv.k) + (size_t)blk * BLOCK * kD * sizeof(T);
+  if (blk < whole) {
+    quantize_block<FMT, T, BLOCK>([&](int r) { return src + (size_t)r * kD * sizeof(T); },
+                                  reinterpret_cast<uint8_t*>(is_v ? view.v : view.k) + (size_t)blk * BLOCK * kD,
+                                  (is_v ? view.v_scale : view.k_scale) + blk);
+    return;
+  }
+  char* dst = reinterpret_cast<char*>(is_v ? view.v_tail : view.k_tail);
+  const int bytes = (int)(len - whole * BLOCK) * kD * (int)sizeof(T);
+  for (int i = lane * 16; i < bytes; i += 64 * 16) *reinterpret_cast<uint4*>(dst + i) = ldg16(src + i);
+}
+
+template <int FMT, typename T, int BLOCK>
+__global__ __launch_bounds__(kQ8Waves * 64) void q8_dequantize_kernel(Q8Args a) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int group = blockIdx.x / a.n_views, bh = blockIdx.x - group * a.n_views;
+  const bool is_v = blockIdx.z;
+  const int64_t len = a.lens[bh];
+  if (len < 0 || len > a.max_rows) return;
+  const int64_t whole = len / BLOCK, blk = (int64_t)group * kQ8Waves + wave;
+  if (blk > whole) return;
+  const catekv_q8_view view = a.views[bh];
+  const catekv_kv_ptrs kv = a.kv[bh];
+  char* dst = reinterpret_cast<char*>(const_cast<void*>(is_v ? kv.v : kv.k)) + (size_t)blk * BLOCK * kD * sizeof(T);
+  if (blk < whole) {
+    const char* src = reinterpret_cast<const char*>(is_v ? view.v : view.k) + (size_t)blk * BLOCK * kD;
+    const float scale = (is_v ? view.v_scale : view.k_scale)[blk];
+    constexpr int N = BLOCK * kD / 16 / 64;
+    uint4 w[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = ldg16(src + (i * 64 + lane) * 16);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t c[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t x = c[2 * h + (j >> 2)];
+          if constexpr (FMT == CATEKV_I8) {
+            f[j] = (float)(int8_t)(x >> (8 * (j & 3)));
+          } else {
+            f[j] = (j & 3) == 0   ? __builtin_amdgcn_cvt_f32_fp8(x, 0)
+                   : (j & 3) == 1 ? __builtin_amdgcn_cvt_f32_fp8(x, 1)
+                   : (j & 3) == 2 ? __builtin_amdgcn_cvt_f32_fp8(x, 2)
+                                  : __builtin_amdgcn_cvt_f32_fp8(x, 3);
+          }
+          f[j] *= scale;
+        }
+        Eight<T> o;
+        o.set(f);
+        o.store(dst + ((i * 64 + lane) * 16 + 8 * h) * sizeof(T));
+      }
+    }
+    return;
+  }
+  const char* src = reinterpret_cast<const char*>(is_v ? view.v_tail : view.k_tail);
+  const int bytes = (int)(len - whole * BLOCK) * kD * (int)sizeof(T);
+  for (int i = lane * 16; i < bytes; i += 64 * 16) *reinterpret_cast<uint4*>(dst + i) = ldg16(src + i);
+}
+
+// One workgroup per view: wave 0 K, wave 1 V.  The row that fills a block is
+// taken from the call's arguments, not from the tail it was just stored in.
+template <int FMT, typename T, int BLOCK>
+__global__ __launch_bounds__(128) void q8_append_kernel(Q8Args a) {
+  const int bh = blockIdx.x, lane = threadIdx.x & 63;
+  const bool is_v = threadIdx.x >= 64;
+  const int64_t len = a.lens_rw[bh];
+  if (len < 0 || len >= a.capacity[bh]) {
+    if (threadIdx.x == 0 && a.overflow) *a.overflow = 1;
+    return;
+  }
+  const catekv_q8_view view = a.views[bh];
+  const int64_t blk = len / BLOCK;
+  const int at = (int)(len - blk * BLOCK);
+  constexpr int kRow = kD * (int)sizeof(T);
+  const char* fresh = reinterpret_cast<const char*>(is_v ? a.v_new : a.k_new) + (size_t)bh * kRow;
+  char* tail = reinterpret_cast<char*>(is_v ? view.v_tail : view.k_tail);
+  if (lane < kRow / 16) *reinterpret_cast<uint4*>(tail + at * kRow + lane * 16) = ldg16(fresh + lane * 16);
+  if (at == BLOCK - 1)
+    quantize_block<FMT, T, BLOCK>([&](int r) { return r == BLOCK - 1 ? fresh : tail + r * kRow; },
+                                  reinterpret_cast<uint8_t*>(is_v ? view.v : view.k) + (size_t)blk * BLOCK * kD,
+                                  (is_v ? view.v_scale : view.k_scale) + blk);
+  __syncthreads();                                 // both waves have read the length
+  if (threadIdx.x == 0) a.lens_rw[bh] = len + 1;
+}
+
+int64_t q8_groups(int64_t max_rows, int block) {
+  return (max_rows / block + kQ8Waves) / kQ8Waves;   // one wave more than whole blocks, for the tail
+}
+
+enum Q8Op { kQuantize, kDequantize, kAppend };
+
+template <int FMT, typename T, int BLOCK>
+static hipError_t launch_q8_t(Q8Op op, const Q8Args& a, hipStream_t stream) {
+  const dim3 grid((unsigned)(q8_groups(a.max_rows, BLOCK) * a.n_views), 1, 2), block(kQ8Waves * 64);
+  if (op == kQuantize)
+    hipLaunchKernelGGL((q8_quantize_kernel<FMT, T, BLOCK>), grid, block, 0, stream, a);
+  else if (op == kDequantize)
+    hipLaunchKernelGGL((q8_dequantize_kernel<FMT, T, BLOCK>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((q8_append_kernel<FMT, T, BLOCK>), dim3(a.n_views), dim3(128), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <int FMT, typename T>
+static hipError_t launch_q8_b(Q8Op op, const Q8Args& a, hipStream_t stream) {
+  return a.block == 32 ? launch_q8_t<FMT, T, 32>(op, a, stream) : launch_q8_t<FMT, T, 64>(op, a, stream);
+}
+
+static hipError_t launch_q8(Q8Op op, int fmt, int dtype, const Q8Args& a, hipStream_t stream) {
+  if (fmt == CATEKV_I8)
+    return dtype == CATEKV_BF16 ? launch_q8_b<CATEKV_I8, uint16_t>(op, a, stream)
+                                : launch_q8_b<CATEKV_I8, float>(op, a, stream);
+  return dtype == CATEKV_BF16 ? launch_q8_b<CATEKV_E4M3, uint16_t>(op, a, stream)
+                              : launch_q8_b<CATEKV_E4M3, float>(op, a, stream);
+}
+
+hipError_t launch_q8_quantize(int fmt, int dtype, const Q8Args& a, hipStream_t s) { return launch_q8(kQuantize, fmt, dtype, a, s); }
+hipError_t launch_q8_dequantize(int fmt, int dtype, const Q8Args& a, hipStream_t s) { return launch_q8(kDequantize, fmt, dtype, a, s); }
+hipError_t launch_q8_append(int fmt, int dtype, const Q8Args& a, hipStream_t s) { return launch_q8(kAppend, fmt, dtype, a, s); }
+
+}  // namespace catekv
