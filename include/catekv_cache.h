@@ -136,9 +136,10 @@ size_t catekv_evict_workspace(int n_views, int64_t max_rows, int cs);
  * lens    [n_views] int64, device, read and written
  * acc     [n_views] device pointers to fp32 arrays of at least lens values
  * budget  [n_views] int32, device: chunks kept among those that compete
- * cs >= 1, recent >= 0
+ * max_rows  a bound on lens (sizes the launches and the workspace), at most 2^26
+ * cs in [1, 2^20], recent >= 0, n_views at most 2^16
  * Errors: INVALID_ARG for null pointers or bad sizes; UNSUPPORTED for an unknown
- * dtype, d != 128 or max_rows above 2^31 - 1; WORKSPACE for a ws too small. */
+ * dtype, d != 128 or sizes above these bounds; WORKSPACE for a ws too small. */
 int catekv_evict_kv(int dtype, const catekv_kv_ptrs* kv, int64_t* lens, float* const* acc, const int32_t* budget,
                     int n_views, int64_t max_rows, int cs, int recent, int d, void* ws, size_t ws_bytes,
                     void* stream);

@@ -72,6 +72,8 @@ struct EvictArgs {
   int64_t max_rows;
   void* ws;
 };
+// Sizes whose element numbers and launches fit 32 bits.
+bool evict_fits(int n_views, int64_t max_rows, int cs);
 size_t evict_workspace_bytes(int n_views, int64_t max_rows, int cs);
 hipError_t launch_evict(const EvictArgs& a, hipStream_t stream);
 

@@ -103,6 +103,9 @@ int check_evict(const void* views, const void* lens, const void* acc, const void
   int rc = check_rows(n_views, max_rows, d);
   if (rc) return rc;
   if (cs < 1) return fail(CATEKV_ERR_INVALID_ARG, "chunk size %d must be >= 1", cs);
+  if (!evict_fits(n_views, max_rows, cs))
+    return fail(CATEKV_ERR_UNSUPPORTED, "n_views=%d, max_rows=%lld, cs=%d: too large for one eviction", n_views,
+                (long long)max_rows, cs);
   if (recent < 0) return fail(CATEKV_ERR_INVALID_ARG, "recent=%d must be >= 0", recent);
   return host_check_ws(ws, ws_bytes, evict_workspace_bytes(n_views, max_rows, cs));
 }
@@ -213,7 +216,7 @@ int catekv_decode_attn_weights(int dtype, const catekv_decode_plan_t* plan, cons
 }
 
 size_t catekv_evict_workspace(int n_views, int64_t max_rows, int cs) {
-  if (n_views < 1 || max_rows < 1 || max_rows > INT32_MAX || cs < 1) return 0;
+  if (n_views < 1 || max_rows < 1 || cs < 1 || !evict_fits(n_views, max_rows, cs)) return 0;
   return evict_workspace_bytes(n_views, max_rows, cs);
 }
 

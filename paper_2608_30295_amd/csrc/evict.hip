@@ -1,14 +1,18 @@
 // Eviction by accumulated weight: which chunks of a view stay, and the moves.
 //
-// One launch selects (a workgroup per view): the chunks' largest weights as
-// ordered 32-bit keys, kept in LDS (or, for more than kLdsChunks, in the
-// workspace), a radix selection of the k-th largest key in three digits, and the
-// pairs (place that becomes free below k, kept chunk from k on) in ascending
-// order.  One launch moves: a workgroup per view and 64-byte strip of the rows of
-// K and of V (and one for the weights and scales) first fills the free places,
-// whose sources and destinations do not meet, then shifts the rows behind the
-// chunks down, a tile of rows read before any of it is written.  A strip belongs
-// to one workgroup, so in-place moves need no order between workgroups.
+// The chunks' largest weights become ordered 32-bit keys, in the selecting
+// workgroup itself or, for long views, in a launch of their own.  One workgroup
+// per view selects: few chunks by counting, for each, the better ones; more by a
+// radix selection of the k-th largest key in up to three digits, the keys in
+// registers (above 16384, read for every pass).  It lists the pairs (place that
+// becomes free below k, kept chunk from k on) in ascending order.
+//
+// One launch moves.  The pairs' sources lie from k on, their places below, so all
+// of them move at once, whole chunks at a time.  The rows behind the chunks
+// shift down over places that may still be sources: those pairs (the first of
+// the list, as sources ascend) belong to the workgroups that shift, one per strip
+// of the rows of K and of V, which read a turn's rows before they write any of
+// them.  No order between workgroups is needed.
 #include "cache.h"
 #include "common.h"
 
@@ -16,17 +20,24 @@ namespace catekv {
 
 constexpr int kEvictThreads = 1024;
 constexpr int kEvictWaves = kEvictThreads / 64;
-constexpr int kLdsChunks = 32768;       // 128 KB of keys
 constexpr int kBins = 2048;             // 11-bit digits: 11 + 11 + 10
-constexpr int kMoveThreads = 512;
+constexpr int kMoveThreads = 256;
+constexpr int64_t kMaxEvictRows = 1 << 26;   // 32 pieces a row, a workgroup per kKeyRows rows:
+constexpr int kMaxEvictChunk = 1 << 20;      // element, piece and workgroup numbers stay below 2^31
+constexpr int kMaxEvictViews = 1 << 16;
+constexpr int kRankChunks = 384;        // up to here a chunk's rank is counted
+constexpr int kOwnKeyRows = 16384;      // views up to here: keys by the selecting workgroup
+constexpr int kKeyRows = 4096;          // else by a workgroup per so many rows
 
 struct EvictInfo {
   int32_t moves;                        // pairs; the view is left alone if shift is 0
   int32_t nc, k, len;
   int32_t shift;                        // rows dropped
+  int32_t rest;                         // rows of K and V behind the chunks (8 bits: those in codes)
+  int32_t lead;                         // pairs whose source the shifted rows will cover
 };
 
-// Workspace: infos, then the pairs of every view, then (long views) its keys.
+// Workspace: infos, the pairs of every view, then (long views) their keys.
 static size_t info_bytes(int n_views) { return ((size_t)n_views * sizeof(EvictInfo) + 255) & ~(size_t)255; }
 static int64_t max_chunks_of(int64_t max_rows, int cs) { return max_rows / cs; }
 // at most half of the chunks can change places: min(k, nc - k)
@@ -36,8 +47,12 @@ static size_t pairs_bytes(int n_views, int64_t chunks) {
 }
 size_t evict_workspace_bytes(int n_views, int64_t max_rows, int cs) {
   const int64_t chunks = max_chunks_of(max_rows, cs);
-  const size_t keys = chunks > kLdsChunks ? (size_t)n_views * (size_t)chunks * sizeof(uint32_t) : 0;
+  const size_t keys = max_rows > kOwnKeyRows ? (size_t)n_views * (size_t)chunks * sizeof(uint32_t) : 0;
   return info_bytes(n_views) + pairs_bytes(n_views, chunks) + ((keys + 255) & ~(size_t)255);
+}
+
+bool evict_fits(int n_views, int64_t max_rows, int cs) {
+  return max_rows <= kMaxEvictRows && cs <= kMaxEvictChunk && n_views <= kMaxEvictViews;
 }
 
 // Larger key = larger weight; NaN above all, -0 as 0.
@@ -48,23 +63,76 @@ __device__ __forceinline__ uint32_t weight_key(float x) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __builtin_amdgcn_ds_bpermute(((int)__lane_id() ^ o) << 2, x);
+// Maximum over each aligned group of g lanes, g a power of two.
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_dpp(uint32_t x) {
+  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ uint32_t group_max(uint32_t x, int g) {
+  if (g >= 2) x = max_dpp<kDppXor1>(x);
+  if (g >= 4) x = max_dpp<kDppXor2>(x);
+  if (g >= 8) x = max_dpp<kDppHalfMirror>(x);
+  if (g >= 16) x = max_dpp<kDppMirror>(x);
+  if (g >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max(r[0], r[1]);
+  }
+  if (g >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    x = max(r[0], r[1]);
+  }
   return x;
+}
+
+// Keys of the chunks [c_lo, c_hi), by all threads of a workgroup: as many lanes to a
+// chunk as it has rows (a power of two, at most 64), so that a wave reads
+// consecutive weights; four groups of chunks per lane in flight.
+template <typename Put>
+__device__ __forceinline__ void chunk_keys(const float* acc, int cs, int c_lo, int c_hi, int threads, Put put) {
+  const int g = 1 << (31 - __builtin_clz(min(cs, 64))), log_g = 31 - __builtin_clz(g);
+  const int lane = threadIdx.x & (g - 1), per = threads >> log_g;
+  for (int c0 = c_lo + (int)(threadIdx.x >> log_g); c0 - (int)(threadIdx.x >> log_g) < c_hi; c0 += 4 * per) {
+    uint32_t x[4] = {0, 0, 0, 0};
+    for (int i = lane; i < cs; i += g) {
+      float w[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int c = min(c0 + u * per, c_hi - 1);
+        w[u] = acc[(size_t)c * cs + i];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[u] = max(x[u], weight_key(w[u]));
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const uint32_t m = group_max(x[u], g);
+      const int c = c0 + u * per;
+      if (lane == 0 && c < c_hi) put(c, m);
+    }
+  }
+}
+
+// What a view has to drop: nc competing chunks of which k stay; false: nothing.
+__device__ __forceinline__ bool evict_view(const EvictArgs& a, int bh, int64_t& len, int& nc, int& k) {
+  len = a.lens[bh];
+  k = a.budget[bh];
+  const int64_t eligible = len > a.recent ? len - a.recent : 0;
+  nc = (int)(eligible / a.cs);
+  return len >= 0 && len <= a.max_rows && k >= 0 && nc > k;
 }
 
 struct SelectShared {
   uint32_t hist[kBins];
   int part[kEvictWaves];
   int part2[kEvictWaves];
+  int lead;
   uint32_t digit;
-  int above;                            // keys above the chosen digit's bin
+  int above, inside;                    // keys above the chosen digit's bin, and in it
 };
 
-// The digit that holds the `want`-th largest of the histogram, and how many lie
-// above it.  Every thread calls it.
-__device__ __forceinline__ void find_digit(SelectShared& s, int want, uint32_t& digit, int& above) {
+// The digit that holds the `want`-th largest of the histogram; s.above and
+// s.inside: how many lie above its bin and in it.  Every thread calls it.
+__device__ __forceinline__ void find_digit(SelectShared& s, int want) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   // thread t owns bins 2047 - 2 t and 2046 - 2 t: sums from the top
   const int h0 = (int)s.hist[kBins - 1 - 2 * t], h1 = (int)s.hist[kBins - 2 - 2 * t];
@@ -82,248 +150,421 @@ __device__ __forceinline__ void find_digit(SelectShared& s, int want, uint32_t& 
   if (before < want && want <= before + h0) {
     s.digit = (uint32_t)(kBins - 1 - 2 * t);
     s.above = before;
+    s.inside = h0;
   } else if (before + h0 < want && want <= before + h0 + h1) {
     s.digit = (uint32_t)(kBins - 2 - 2 * t);
     s.above = before + h0;
+    s.inside = h1;
   }
   __syncthreads();
-  digit = s.digit;
-  above = s.above;
 }
 
-// Selection over nc keys of which k < nc stay; writes the pairs, returns their number.
-template <typename Keys>
-__device__ __forceinline__ int select_pairs(SelectShared& s, Keys key, int nc, int k, int32_t* pairs) {
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  uint32_t prefix = 0;
-  int want = k;
-  if (k > 0) {
-    const int shifts[3] = {21, 10, 0};
-#pragma unroll
-    for (int p = 0; p < 3; ++p) {
-      const int sh = shifts[p], bits = p == 2 ? 10 : 11;
-      __syncthreads();
-      s.hist[t] = 0;
-      s.hist[t + kEvictThreads] = 0;
-      __syncthreads();
-      for (int c = t; c < nc; c += kEvictThreads) {
-        const uint32_t x = key(c);
-        if (p == 0 || (x >> (sh + bits)) == (prefix >> (sh + bits)))
-          atomicAdd(&s.hist[(x >> sh) & ((1u << bits) - 1)], 1u);
-      }
-      __syncthreads();
-      uint32_t digit;
-      int above;
-      find_digit(s, want, digit, above);
-      prefix |= digit << sh;
-      want -= above;
-    }
-  } else {
-    prefix = 0xffffffffu;
-    want = 0;                            // nothing stays: no key above, no tie taken
-  }
-  // keys above prefix stay, and the first `want` equal ones.  Wave w owns a run of
-  // chunks, 64 at a time in order.
-  const int run = (nc + kEvictThreads - 1) / kEvictThreads * 64;
-  const int lo = wave * run, hi = min(nc, lo + run);
-  int ties = 0;
-  for (int c0 = lo; c0 < hi; c0 += 64) {
-    const int c = c0 + lane;
-    ties += __popcll(__builtin_amdgcn_ballot_w64(c < hi && key(c) == prefix));
-  }
-  __syncthreads();
-  if (lane == 0) s.part[wave] = ties;
-  __syncthreads();
-  int tie0 = 0;
-  for (int w = 0; w < wave; ++w) tie0 += s.part[w];
+// Where the wave's chunks lie: rows of 64 consecutive ones, [lo, hi).
+struct Run {
+  int lo, hi;
+};
+
+// The pairs of a view's chunks.  rows(f): f(row number, first chunk) for every row
+// of this wave; stays(row, c): whether c, a chunk of the wave, stays, asked in order
+// after each reset().  Returns the number of pairs; s.lead gets that of those whose
+// source lies below `covered`.
+template <typename Rows, typename Reset, typename Stays>
+__device__ __forceinline__ int list_pairs(SelectShared& s, Run run, int k, int covered, int32_t* pairs, Rows rows, Reset reset,
+                                          Stays stays) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint64_t below = lane ? ~0ull >> (64 - lane) : 0;
-  auto classify = [&](int c, int& tie, bool& stays) {
-    const uint32_t x = c < hi ? key(c) : 0;
-    const uint64_t eq = __builtin_amdgcn_ballot_w64(c < hi && x == prefix);
-    stays = c < hi && (x > prefix || (x == prefix && tie + __popcll(eq & below) < want));
-    tie += __popcll(eq);
-  };
-  int holes = 0, movers = 0, tie = tie0;
-  for (int c0 = lo; c0 < hi; c0 += 64) {
+  int holes = 0, movers = 0;
+  reset();
+  // a row below k holds places only, one from k on sources only
+  rows([&](int i, int c0) {
     const int c = c0 + lane;
-    bool stays;
-    classify(c, tie, stays);
-    holes += __popcll(__builtin_amdgcn_ballot_w64(c < hi && !stays && c < k));
-    movers += __popcll(__builtin_amdgcn_ballot_w64(stays && c >= k));
-  }
+    const bool st = stays(i, c);
+    if (c0 < k) holes += __popcll(__builtin_amdgcn_ballot_w64(!st && c < min(k, run.hi)));
+    if (c0 + 63 >= k) movers += __popcll(__builtin_amdgcn_ballot_w64(st && c >= k));
+  });
   __syncthreads();
   if (lane == 0) {
     s.part[wave] = holes;
     s.part2[wave] = movers;
   }
+  if (threadIdx.x == 0) s.lead = 0;
   __syncthreads();
   int total = 0, h = 0, m = 0;
+#pragma unroll
   for (int w = 0; w < kEvictWaves; ++w) {
-    if (w == wave) {
-      h = total;
-    }
+    h += w < wave ? s.part[w] : 0;
+    m += w < wave ? s.part2[w] : 0;
     total += s.part[w];
   }
-  for (int w = 0; w < wave; ++w) m += s.part2[w];
-  tie = tie0;
-  for (int c0 = lo; c0 < hi; c0 += 64) {
+  reset();
+  rows([&](int i, int c0) {
     const int c = c0 + lane;
-    bool stays;
-    classify(c, tie, stays);
-    const bool hole = c < hi && !stays && c < k, mover = stays && c >= k;
-    const uint64_t hm = __builtin_amdgcn_ballot_w64(hole), mm = __builtin_amdgcn_ballot_w64(mover);
-    if (hole) pairs[2 * (h + __popcll(hm & below))] = c;
-    if (mover) pairs[2 * (m + __popcll(mm & below)) + 1] = c;
-    h += __popcll(hm);
-    m += __popcll(mm);
-  }
+    const bool st = stays(i, c);
+    if (c0 < k) {
+      const bool hole = !st && c < min(k, run.hi);
+      const uint64_t hm = __builtin_amdgcn_ballot_w64(hole);
+      if (hole) pairs[2 * (h + __popcll(hm & below))] = c;
+      h += __popcll(hm);
+    }
+    if (c0 + 63 >= k) {
+      const bool mover = st && c >= k;
+      const uint64_t mm = __builtin_amdgcn_ballot_w64(mover);
+      if (mover) pairs[2 * (m + __popcll(mm & below)) + 1] = c;
+      m += __popcll(mm);
+      if (c0 < covered) {
+        const int lead = __popcll(__builtin_amdgcn_ballot_w64(mover && c < covered));
+        if (lane == 0 && lead) atomicAdd(&s.lead, lead);
+      }
+    }
+  });
+  __syncthreads();
   return total;
 }
 
+// Up to kRankChunks keys in LDS (padded to a multiple of four with zeros, which are
+// no chunk's key): chunk c stays if fewer than k are better (ties: the lower
+// chunk).  The better ones are counted by as many waves per chunk as there are;
+// against the chunks of another wave a tie always or never counts, so that two
+// instructions do.  s.hist holds the counts, zero on entry.
+__device__ __forceinline__ int rank_pairs(SelectShared& s, const uint32_t* keys, int nc, int k, int covered, int32_t* pairs) {
+  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
+  const int per = (nc + 63) / 64, parts = kEvictWaves / per;       // waves per part: one chunk per lane
+  const int part = wave / per, own = (wave - part * per) * 64, c = own + lane;
+  if (part < parts) {
+    const uint32_t x = keys[min(c, nc - 1)];
+    const int step = ((nc + 3) / 4 + parts - 1) / parts * 4, j0 = part * step, j1 = min(nc, j0 + step);
+    int rank = 0;
+    auto count = [&](int lo, int hi, uint32_t limit) {               // keys above limit
+#pragma unroll 4
+      for (int j = lo; j < hi; j += 4) {
+        const uint4 w = *reinterpret_cast<const uint4*>(keys + j);
+        rank += w.x > limit;
+        rank += w.y > limit;
+        rank += w.z > limit;
+        rank += w.w > limit;
+      }
+    };
+    count(j0, min(j1, own), x - 1);
+    for (int j = max(j0, own); j < min(j1, own + 64); j += 4) {
+      const uint4 w = *reinterpret_cast<const uint4*>(keys + j);
+      rank += w.x > (j < c ? x - 1 : x);
+      rank += w.y > (j + 1 < c ? x - 1 : x);
+      rank += w.z > (j + 2 < c ? x - 1 : x);
+      rank += w.w > (j + 3 < c ? x - 1 : x);
+    }
+    count(max(j0, own + 64), j1, x);
+    if (c < nc) atomicAdd(&s.hist[c], (uint32_t)rank);
+  }
+  __syncthreads();
+  const bool st = t < nc && (int)s.hist[min(t, nc - 1)] < k;
+  return list_pairs(s, Run{wave * 64, min(nc, wave * 64 + 64)}, k, covered, pairs,
+                    [&](auto f) { if (wave * 64 < nc) f(0, wave * 64); }, [] {}, [&](int, int) { return st; });
+}
+
+// Which of any number of keys stay, k < nc of them: those above `limit` and the
+// first `ties` equal ones.  key(row, c): the key of chunk c of this wave's row.
+template <typename Rows, typename Keys>
+__device__ __forceinline__ void radix_limit(SelectShared& s, Run run, Rows rows, Keys key, int k, uint32_t& limit, int& ties) {
+  const int t = threadIdx.x, lane = t & 63;
+  limit = 0xffffffffu;
+  ties = 0;
+  if (k == 0) return;
+  uint32_t prefix = 0;
+  ties = k;
+#pragma unroll 1
+  for (int p = 0; p < 3; ++p) {
+    const int sh = p == 0 ? 21 : p == 1 ? 10 : 0, bits = p == 2 ? 10 : 11;
+    const uint32_t mask = p == 0 ? 0u : 0xffffffffu << (sh + bits);
+    __syncthreads();
+    s.hist[t] = 0;
+    s.hist[t + kEvictThreads] = 0;
+    __syncthreads();
+    rows([&](int i, int c0) {
+      const int c = c0 + lane;
+      const uint32_t x = key(i, c);
+      if (c < run.hi && (x & mask) == prefix) atomicAdd(&s.hist[(x >> sh) & ((1u << bits) - 1)], 1u);
+    });
+    __syncthreads();
+    find_digit(s, ties);
+    prefix |= s.digit << sh;
+    ties -= s.above;
+    limit = prefix;
+    if (ties == s.inside && prefix != 0) {       // all of this bin stays: no ties to tell apart
+      limit = prefix - 1;
+      ties = 0;
+      return;
+    }
+  }
+}
+
+// Keys equal to limit in the waves before this one.
+template <typename Rows, typename Keys>
+__device__ __forceinline__ int ties_before(SelectShared& s, Run run, Rows rows, Keys key, uint32_t limit) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int n = 0;
+  rows([&](int i, int c0) {
+    const int c = c0 + lane;
+    n += __popcll(__builtin_amdgcn_ballot_w64(c < run.hi && key(i, c) == limit));
+  });
+  __syncthreads();
+  if (lane == 0) s.part[wave] = n;
+  __syncthreads();
+  n = 0;
+#pragma unroll
+  for (int w = 0; w < kEvictWaves; ++w) n += w < wave ? s.part[w] : 0;
+  return n;
+}
+
+// Whether chunk c stays; `tie`: equal keys before its row.
+__device__ __forceinline__ bool stays_at(uint32_t x, bool valid, uint32_t limit, int ties, int& tie) {
+  bool st = valid && x > limit;
+  if (ties > 0) {
+    const int lane = threadIdx.x & 63;
+    const uint64_t eq = __builtin_amdgcn_ballot_w64(valid && x == limit);
+    st = st || (valid && x == limit && tie + __popcll(eq & (lane ? ~0ull >> (64 - lane) : 0)) < ties);
+    tie += __popcll(eq);
+  }
+  return st;
+}
+
+// A lane's R keys in registers: nc <= 1024 R.
+template <int R, typename Load>
+__device__ __forceinline__ int register_pairs(SelectShared& s, Load load, int nc, int k, int covered, int32_t* pairs) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Run run{min(nc, wave * 64 * R), min(nc, (wave + 1) * 64 * R)};
+  uint32_t x[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) x[i] = load(min(run.lo + i * 64 + lane, nc - 1));
+  auto rows = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) f(i, run.lo + i * 64);
+  };
+  auto key = [&](int i, int) { return x[i]; };
+  uint32_t limit;
+  int ties;
+  radix_limit(s, run, rows, key, k, limit, ties);
+  int tie = ties > 0 ? ties_before(s, run, rows, key, limit) : 0;
+  uint32_t bits = 0;
+#pragma unroll
+  for (int i = 0; i < R; ++i) bits |= (uint32_t)stays_at(x[i], run.lo + i * 64 + lane < run.hi, limit, ties, tie) << i;
+  return list_pairs(s, run, k, covered, pairs, rows, [] {}, [&](int i, int) { return (bits >> i & 1) != 0; });
+}
+
+// Any number of keys, read for every pass.
+template <typename Load>
+__device__ __forceinline__ int memory_pairs(SelectShared& s, Load load, int nc, int k, int covered, int32_t* pairs) {
+  const int wave = threadIdx.x >> 6, size = (nc + kEvictThreads - 1) / kEvictThreads * 64;
+  const Run run{min(nc, wave * size), min(nc, (wave + 1) * size)};
+  auto rows = [&](auto f) {
+    for (int c0 = run.lo; c0 < run.hi; c0 += 64) f(0, c0);
+  };
+  auto key = [&](int, int c) { return load(min(c, nc - 1)); };
+  uint32_t limit;
+  int ties, tie = 0;
+  radix_limit(s, run, rows, key, k, limit, ties);
+  const int tie0 = ties > 0 ? ties_before(s, run, rows, key, limit) : 0;
+  return list_pairs(s, run, k, covered, pairs, rows, [&] { tie = tie0; },
+                    [&](int i, int c) { return stays_at(key(i, c), c < run.hi, limit, ties, tie); });
+}
+
+// Keys of long views: workgroups over kKeyRows rows each.
+__global__ __launch_bounds__(kEvictThreads) void evict_keys_kernel(EvictArgs a, uint32_t* keys, int64_t max_chunks, int per_wg) {
+  const int group = blockIdx.x / a.n_views, bh = blockIdx.x - group * a.n_views;
+  int64_t len;
+  int nc, k;
+  if (!evict_view(a, bh, len, nc, k)) return;
+  const int64_t c_lo = (int64_t)group * per_wg;
+  if (c_lo >= nc) return;
+  uint32_t* mine = keys + (size_t)bh * max_chunks;
+  chunk_keys(a.acc[bh], a.cs, (int)c_lo, (int)min((int64_t)nc, c_lo + per_wg), kEvictThreads,
+             [&](int c, uint32_t x) { mine[c] = x; });
+}
+
+// keys: null where this workgroup makes its own.
 __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a, EvictInfo* infos, int32_t* pairs,
-                                                                     uint32_t* keys, int64_t max_chunks,
+                                                                     const uint32_t* keys, int64_t max_chunks,
                                                                      int64_t max_moves) {
-  extern __shared__ uint32_t s_keys[];
+  extern __shared__ uint4 s_dyn[];
+  uint32_t* s_keys = reinterpret_cast<uint32_t*>(s_dyn);
   __shared__ SelectShared s;
   const int bh = blockIdx.x, t = threadIdx.x;
-  const int64_t len = a.lens[bh];
-  const int budget = a.budget[bh];
-  const int64_t eligible = len - a.recent > 0 ? len - a.recent : 0;
-  const int nc = (int)(eligible / a.cs);
-  const bool alone = len < 0 || len > a.max_rows || budget < 0 || nc <= budget;
+  int64_t len;
+  int nc, k;
+  const bool drops = evict_view(a, bh, len, nc, k);
   __syncthreads();                       // the length is read before it is replaced
-  if (alone) {
-    if (t == 0) infos[bh] = EvictInfo{0, 0, 0, 0, 0};
+  if (!drops) {
+    if (t == 0) infos[bh] = EvictInfo{};
     return;
   }
-  const int k = budget, cs = a.cs;
-  const float* acc = a.acc[bh];
-  const bool in_lds = nc <= kLdsChunks;
-  uint32_t* mine = in_lds ? nullptr : keys + (size_t)bh * max_chunks;
-  for (int c = t; c < nc; c += kEvictThreads) {
-    const float* p = acc + (size_t)c * cs;
-    uint32_t x = 0;
-    for (int i = 0; i < cs; ++i) x = max(x, weight_key(p[i]));
-    if (in_lds) s_keys[c] = x;
-    else mine[c] = x;
+  const uint32_t* mine = keys ? keys + (size_t)bh * max_chunks : s_keys;
+  if (!keys) {
+    chunk_keys(a.acc[bh], a.cs, 0, nc, kEvictThreads, [&](int c, uint32_t x) { s_keys[c] = x; });
+  } else if (nc <= kRankChunks) {
+    if (t < nc) s_keys[t] = mine[t];
+  }
+  if (nc <= kRankChunks) {
+    if (t < 4) s_keys[nc + t] = 0;       // rank_pairs reads four at a time
+    if (t < kRankChunks) s.hist[t] = 0;
   }
   __syncthreads();
   int32_t* out = pairs + (size_t)bh * max_moves * 2;
-  const int moves = in_lds ? select_pairs(s, [&](int c) { return s_keys[c]; }, nc, k, out)
-                           : select_pairs(s, [&](int c) { return mine[c]; }, nc, k, out);
+  const int64_t from = (int64_t)nc * a.cs;
+  const int rest = (int)((a.q8 ? len / a.block * a.block : len) - from);
+  const int covered = k + (rest + a.cs - 1) / a.cs;
+  // up to 16384 keys in the lanes' registers, more read again for every pass
+  int moves;
+  auto load = [&](int c) { return mine[c]; };
+  if (nc <= kRankChunks) {
+    moves = rank_pairs(s, s_keys, nc, k, covered, out);
+  } else if (nc <= 2 * kEvictThreads) {
+    moves = register_pairs<2>(s, load, nc, k, covered, out);
+  } else if (nc <= 16 * kEvictThreads) {
+    moves = register_pairs<16>(s, load, nc, k, covered, out);
+  } else {
+    moves = memory_pairs(s, load, nc, k, covered, out);
+  }
   if (t == 0) {
-    const int shift = (nc - k) * cs;
-    infos[bh] = EvictInfo{moves, nc, k, (int32_t)len, shift};
+    const int shift = (nc - k) * a.cs;
+    infos[bh] = EvictInfo{moves, nc, k, (int32_t)len, shift, rest, s.lead};
     a.lens[bh] = len - shift;
   }
 }
 
-// Rows [0, n) of a strip: row i from src(i) to dst(i), each row `pieces` 16-byte
-// pieces wide at a stride of `pitch` bytes.  All rows of a tile are read before
-// one is written; a tile's destinations lie below the sources of the next.
-constexpr int kMoveBatch = 8;
+constexpr int kMoveBatch = 8;           // loads of a thread in flight
 
-template <typename Src, typename Dst>
-__device__ __forceinline__ void move_rows(char* base, size_t pitch, int pieces_log, int64_t n, bool apart, Src src, Dst dst) {
-  const int piece = threadIdx.x & ((1 << pieces_log) - 1);
-  const int64_t row = threadIdx.x >> pieces_log, step = kMoveThreads >> pieces_log;
-  for (int64_t i0 = 0; i0 < n; i0 += step * kMoveBatch) {
-    uint4 w[kMoveBatch];
+// Three runs of elements of p in one sequence: n_fill from p[src(i)] to p[dst(i)],
+// n_shift from p[from + i] to p[to + i] (to < from), then n_zero zeros from p[end]
+// on.  A turn's elements are all read before one is written.  What a turn writes
+// no later turn reads: fills lie below all sources, shifted elements below the
+// sources of the shifts still to come, and zeros come last.
+template <typename E, typename Src, typename Dst, typename From, typename To>
+__device__ __forceinline__ void move_elements(E* p, int n_fill, Src src, Dst dst, int n_shift, From from, To to, int n_zero,
+                                              size_t end) {
+  const int n = n_fill + n_shift + n_zero;
+  for (int i0 = 0; i0 < n; i0 += kMoveThreads * kMoveBatch) {
+    E w[kMoveBatch];
 #pragma unroll
     for (int u = 0; u < kMoveBatch; ++u) {
-      const int64_t i = i0 + u * step + row;
-      if (i < n) w[u] = ldg16(base + (size_t)src(i) * pitch + piece * 16);
+      const int i = i0 + u * kMoveThreads + (int)threadIdx.x;
+      w[u] = E{};
+      if (i < n_fill) w[u] = p[src(i)];
+      else if (i < n_fill + n_shift) w[u] = p[from(i - n_fill)];
     }
-    if (!apart) {
-      __builtin_amdgcn_s_waitcnt(0);
-      __syncthreads();
-    }
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
 #pragma unroll
     for (int u = 0; u < kMoveBatch; ++u) {
-      const int64_t i = i0 + u * step + row;
-      if (i < n) *reinterpret_cast<uint4*>(base + (size_t)dst(i) * pitch + piece * 16) = w[u];
+      const int i = i0 + u * kMoveThreads + (int)threadIdx.x;
+      if (i < n_fill) p[dst(i)] = w[u];
+      else if (i < n_fill + n_shift) p[to(i - n_fill)] = w[u];
+      else if (i < n) p[end + (size_t)(i - n_fill - n_shift)] = w[u];
     }
   }
 }
 
-template <typename Src, typename Dst>
-__device__ __forceinline__ void move_floats(float* p, int64_t n, bool apart, Src src, Dst dst) {
-  for (int64_t i0 = 0; i0 < n; i0 += (int64_t)kMoveThreads * kMoveBatch) {
-    float w[kMoveBatch];
-#pragma unroll
-    for (int u = 0; u < kMoveBatch; ++u) {
-      const int64_t i = i0 + u * kMoveThreads + threadIdx.x;
-      w[u] = i < n ? p[src(i)] : 0.f;
-    }
-    if (!apart) {
-      __builtin_amdgcn_s_waitcnt(0);
-      __syncthreads();
-    }
-#pragma unroll
-    for (int u = 0; u < kMoveBatch; ++u) {
-      const int64_t i = i0 + u * kMoveThreads + threadIdx.x;
-      if (i < n) p[dst(i)] = w[u];
-    }
-  }
-}
-
-// blockIdx.x: view; blockIdx.y: strips of K, strips of V, then the weights (and scales).
+// blockIdx.x: view.  blockIdx.y: first the workgroups that shift: one for the weights
+// (and, for codes, one for the scales of K and one for those of V, which they move
+// whole), one per strip of K and of V (16 << strip_log bytes); then `fills` that fill
+// places in K, as many for V, and `acc_fills` for the weights.
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, const EvictInfo* infos,
-                                                                  const int32_t* pairs, int64_t max_moves) {
+                                                                  const int32_t* pairs, int64_t max_moves, int fills,
+                                                                  int acc_fills, int strip_log, bool zeros) {
   const int bh = blockIdx.x, cs = a.cs;
   const EvictInfo f = infos[bh];
   if (f.shift == 0) return;
-  const int32_t* pr = pairs + (size_t)bh * max_moves * 2;
-  const int64_t filled = (int64_t)f.moves * cs, at = (int64_t)f.k * cs, from = (int64_t)f.nc * cs;
-  const int strips = a.row_bytes / 64;
-  // row i of the fill: pair i / cs, row i % cs of its chunk
-  auto fill_src = [&](int64_t i) { const int p = (int)(i / cs); return (int64_t)pr[2 * p + 1] * cs + (i - (int64_t)p * cs); };
-  auto fill_dst = [&](int64_t i) { const int p = (int)(i / cs); return (int64_t)pr[2 * p] * cs + (i - (int64_t)p * cs); };
-  auto rest_src = [&](int64_t i) { return from + i; };
-  auto rest_dst = [&](int64_t i) { return at + i; };
-  if ((int)blockIdx.y < 2 * strips) {
-    const bool is_v = (int)blockIdx.y >= strips;
-    const int strip = is_v ? blockIdx.y - strips : blockIdx.y;
-    char* base;
-    int64_t rest;
-    if (a.q8) {
-      base = reinterpret_cast<char*>(is_v ? a.q8[bh].v : a.q8[bh].k);
-      rest = (int64_t)(f.len / a.block) * a.block - from;     // the codes behind the chunks
-    } else {
-      base = reinterpret_cast<char*>(const_cast<void*>(is_v ? a.kv[bh].v : a.kv[bh].k));
-      rest = f.len - from;
-    }
-    base += strip * 64;
-    move_rows(base, a.row_bytes, 2, filled, true, fill_src, fill_dst);
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    move_rows(base, a.row_bytes, 2, rest, false, rest_src, rest_dst);
+  const int2* pr = reinterpret_cast<const int2*>(pairs) + (size_t)bh * max_moves;
+  const int pieces = a.row_bytes / 16, strips = pieces >> strip_log, floats = a.q8 ? 3 : 1;
+  int y = blockIdx.y;
+  if (y < floats) {
+    // elements of a chunk: its rows' weights, or its blocks' scales
+    const int per = y == 0 ? cs : cs / a.block;
+    float* p = y == 0 ? a.acc[bh] : y == 1 ? a.q8[bh].k_scale : a.q8[bh].v_scale;
+    const int fill = y == 0 ? f.lead : f.moves;
+    const int behind = y == 0 ? (int)((int64_t)f.len - (int64_t)f.nc * cs) : f.rest / a.block;
+    move_elements(p, fill * per,
+                  [&](int i) { const int q = i / per; return (size_t)pr[q].y * per + (i - q * per); },
+                  [&](int i) { const int q = i / per; return (size_t)pr[q].x * per + (i - q * per); },
+                  behind, [&](int i) { return (size_t)f.nc * per + i; }, [&](int i) { return (size_t)f.k * per + i; },
+                  y == 0 && zeros ? f.shift : 0, (size_t)(f.len - f.shift));
     return;
   }
-  float* acc = a.acc[bh];
-  const int64_t rest = f.len - from;
-  move_floats(acc, filled, true, fill_src, fill_dst);
-  __builtin_amdgcn_s_waitcnt(0);
-  __syncthreads();
-  move_floats(acc, rest, false, rest_src, rest_dst);
-  __builtin_amdgcn_s_waitcnt(0);
-  __syncthreads();
-  for (int64_t i = f.len - f.shift + threadIdx.x; i < f.len; i += kMoveThreads) acc[i] = 0.f;
-  if (a.q8) {
-    const int per = cs / a.block;        // blocks of a chunk
-    auto src = [&](int64_t i) { const int p = (int)(i / per); return (int64_t)pr[2 * p + 1] * per + (i - (int64_t)p * per); };
-    auto dst = [&](int64_t i) { const int p = (int)(i / per); return (int64_t)pr[2 * p] * per + (i - (int64_t)p * per); };
-    const int64_t n = (int64_t)f.moves * per, left = f.len / a.block - (int64_t)f.nc * per;
-#pragma unroll 1
-    for (int v = 0; v < 2; ++v) {
-      float* p = v ? a.q8[bh].v_scale : a.q8[bh].k_scale;
-      move_floats(p, n, true, src, dst);
-      __builtin_amdgcn_s_waitcnt(0);
-      __syncthreads();
-      move_floats(p, left, false, [&](int64_t i) { return (int64_t)f.nc * per + i; },
-                  [&](int64_t i) { return (int64_t)f.k * per + i; });
+  y -= floats;
+  const bool shifting = y < 2 * strips;
+  if (!shifting) y -= 2 * strips;
+  if (!shifting && y >= 2 * fills) {
+    y -= 2 * fills;
+    float* p = a.acc[bh];
+    const int n = (f.moves - f.lead) * cs, step = kMoveThreads * kMoveBatch;
+    for (int i0 = y * step; i0 < n; i0 += acc_fills * step) {
+      int2 c[kMoveBatch];
+      int off[kMoveBatch];
+      float w[kMoveBatch];
+#pragma unroll
+      for (int u = 0; u < kMoveBatch; ++u) {
+        const int i = min(i0 + u * kMoveThreads + (int)threadIdx.x, n - 1), q = i / cs;
+        off[u] = i - q * cs;
+        c[u] = pr[f.lead + q];
+      }
+#pragma unroll
+      for (int u = 0; u < kMoveBatch; ++u) w[u] = p[(size_t)c[u].y * cs + off[u]];
+#pragma unroll
+      for (int u = 0; u < kMoveBatch; ++u) p[(size_t)c[u].x * cs + off[u]] = w[u];   // beyond n: the last one again
     }
+    return;
   }
+  const int of_k = shifting ? strips : fills;
+  const bool is_v = y >= of_k;
+  if (is_v) y -= of_k;
+  char* base = a.q8 ? reinterpret_cast<char*>(is_v ? a.q8[bh].v : a.q8[bh].k)
+                    : reinterpret_cast<char*>(const_cast<void*>(is_v ? a.kv[bh].v : a.kv[bh].k));
+  if (shifting) {
+    // element i: piece i % 2^strip_log of the strip's row i / 2^strip_log
+    const int64_t at = (int64_t)f.k * cs, from = (int64_t)f.nc * cs;
+    u32x4_t* p = reinterpret_cast<u32x4_t*>(base) + (y << strip_log);
+    const int in = (1 << strip_log) - 1;
+    move_elements(p, (f.lead * cs) << strip_log,
+                  [&](int i) { const int r = i >> strip_log, q = r / cs; return ((size_t)pr[q].y * cs + (r - q * cs)) * pieces + (i & in); },
+                  [&](int i) { const int r = i >> strip_log, q = r / cs; return ((size_t)pr[q].x * cs + (r - q * cs)) * pieces + (i & in); },
+                  f.rest << strip_log, [&](int i) { return (size_t)(from + (i >> strip_log)) * pieces + (i & in); },
+                  [&](int i) { return (size_t)(at + (i >> strip_log)) * pieces + (i & in); }, 0, 0);
+    return;
+  }
+  const int piece = cs * pieces;                     // 16-byte pieces of a chunk
+  const int64_t n = (int64_t)(f.moves - f.lead) * piece;
+  const size_t chunk_bytes = (size_t)cs * a.row_bytes;
+  for (int64_t i0 = (int64_t)y * (kMoveThreads * kMoveBatch); i0 < n; i0 += (int64_t)fills * (kMoveThreads * kMoveBatch)) {
+    // chunk and piece of the turn's first element, then 32-bit steps from there
+    const int64_t q0 = i0 / piece, first = f.lead + q0;
+    const uint32_t off0 = (uint32_t)(i0 - q0 * piece);
+    int2 c[kMoveBatch];
+    uint32_t off[kMoveBatch];
+    uint4 w[kMoveBatch];
+    bool mine[kMoveBatch];
+#pragma unroll
+    for (int u = 0; u < kMoveBatch; ++u) {
+      const uint32_t j = off0 + u * kMoveThreads + threadIdx.x, q = j / (uint32_t)piece;
+      const int64_t pi = first + q;
+      off[u] = (j - q * piece) * 16;
+      c[u] = pr[min(pi, (int64_t)f.moves - 1)];
+      mine[u] = pi < f.moves;
+    }
+#pragma unroll
+    for (int u = 0; u < kMoveBatch; ++u) w[u] = ldg16(base + (size_t)c[u].y * chunk_bytes + off[u]);
+#pragma unroll
+    for (int u = 0; u < kMoveBatch; ++u)
+      if (mine[u]) *reinterpret_cast<uint4*>(base + (size_t)c[u].x * chunk_bytes + off[u]) = w[u];
+  }
+}
+
+// Zeros behind the new lengths of long views (16 KB of weights per workgroup).
+__global__ __launch_bounds__(kMoveThreads) void evict_zero_kernel(EvictArgs a, const EvictInfo* infos) {
+  const int group = blockIdx.x / a.n_views, bh = blockIdx.x - group * a.n_views;
+  const EvictInfo f = infos[bh];
+  if (f.shift == 0) return;
+  float* acc = a.acc[bh];
+  const int64_t lo = (int64_t)(f.len - f.shift) + (int64_t)group * kKeyRows, hi = min((int64_t)f.len, lo + kKeyRows);
+#pragma unroll 4
+  for (int64_t i = lo + threadIdx.x; i < hi; i += kMoveThreads) acc[i] = 0.f;
 }
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
@@ -331,12 +572,36 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
   char* w = reinterpret_cast<char*>(a.ws);
   EvictInfo* infos = reinterpret_cast<EvictInfo*>(w);
   int32_t* pairs = reinterpret_cast<int32_t*>(w + info_bytes(a.n_views));
-  uint32_t* keys = reinterpret_cast<uint32_t*>(w + info_bytes(a.n_views) + pairs_bytes(a.n_views, chunks));
-  const size_t lds = (size_t)(chunks < kLdsChunks ? chunks : kLdsChunks) * sizeof(uint32_t);
-  hipLaunchKernelGGL(evict_select_kernel, dim3(a.n_views), dim3(kEvictThreads), lds, stream, a, infos, pairs, keys,
-                     chunks, moves);
-  hipLaunchKernelGGL(evict_move_kernel, dim3(a.n_views, 2 * (a.row_bytes / 64) + 1), dim3(kMoveThreads), 0, stream, a,
-                     infos, pairs, moves);
+  uint32_t* keys = nullptr;
+  if (a.max_rows > kOwnKeyRows) {
+    keys = reinterpret_cast<uint32_t*>(w + info_bytes(a.n_views) + pairs_bytes(a.n_views, chunks));
+    const int per_wg = kKeyRows / a.cs > 0 ? kKeyRows / a.cs : 1;
+    const int64_t groups = (chunks + per_wg - 1) / per_wg;
+    if (groups > 0)
+      hipLaunchKernelGGL(evict_keys_kernel, dim3((unsigned)(groups * a.n_views)), dim3(kEvictThreads), 0, stream, a, keys,
+                         chunks, per_wg);
+  }
+  const int64_t in_lds = keys ? kRankChunks : chunks;
+  hipLaunchKernelGGL(evict_select_kernel, dim3(a.n_views), dim3(kEvictThreads), (size_t)(in_lds + 4) * sizeof(uint32_t),
+                     stream, a, infos, pairs, keys, chunks, moves);
+  // A fill workgroup moves kTurn bytes per turn: as many as the most chunks that may
+  // move keep busy, but about four rounds of the device at most.  A strip is as wide
+  // as its workgroup moves in one turn, the rows behind the chunks being fewer than
+  // recent + cs and those filled first hardly more.
+  constexpr int64_t kTurn = kMoveThreads * kMoveBatch * 16;
+  const int64_t turns = (moves * a.cs * a.row_bytes + kTurn - 1) / kTurn;
+  const int64_t room = 2048 / a.n_views > 2 ? 2048 / a.n_views : 2;
+  const int fills = (int)(turns < room ? turns : room);
+  int strip_log = 2;
+  while ((16 << strip_log) < a.row_bytes && 2 * ((int64_t)a.recent + a.cs) * (32 << strip_log) <= kTurn) ++strip_log;
+  const int64_t acc_turns = (moves * a.cs + kMoveThreads * kMoveBatch - 1) / (kMoveThreads * kMoveBatch);
+  const int acc_fills = (int)(acc_turns < room / 4 + 1 ? acc_turns : room / 4 + 1);
+  const int shifts = (a.q8 ? 3 : 1) + 2 * ((a.row_bytes / 16) >> strip_log);
+  hipLaunchKernelGGL(evict_move_kernel, dim3(a.n_views, shifts + 2 * fills + acc_fills), dim3(kMoveThreads), 0, stream, a,
+                     infos, pairs, moves, fills, acc_fills, strip_log, keys == nullptr);
+  if (keys)
+    hipLaunchKernelGGL(evict_zero_kernel, dim3((unsigned)((a.max_rows + kKeyRows - 1) / kKeyRows * a.n_views)),
+                       dim3(kMoveThreads), 0, stream, a, infos);
   return hipGetLastError();
 }
 

@@ -428,8 +428,9 @@ def budgets(lens, cs, recent, rng):
 
 @pytest.mark.parametrize("kind", ["any", "ties", "equal", "special", "increasing", "decreasing"])
 @pytest.mark.parametrize("dtype,cs,recent", [("bf16", 1, 0), ("bf16", 8, 64), ("f32", 5, 33), ("bf16", 64, 1),
-                                             ("f32", 16, 0), ("bf16", 12, 3000)])
-def test_evict(kind, dtype, cs, recent):
+                                             ("f32", 16, 0), ("bf16", 12, 3000), ("bf16", 3, 1000)])
+@pytest.mark.parametrize("max_rows", [2304, 40000])
+def test_evict(kind, dtype, cs, recent, max_rows):
     rng = np.random.default_rng(31)
     lens = EVICT
     d = Dense(rng, lens, dtype)
@@ -438,7 +439,7 @@ def test_evict(kind, dtype, cs, recent):
     k0, v0, a0 = [x.clone() for x in d.k], [x.clone() for x in d.v], [x.clone() for x in a]
     new = d.lens.clone()
     ck.evict_kv(d.table, new, ck.acc_table([x.data_ptr() for x in a], DEV), torch.tensor(b, dtype=torch.int32, device=DEV),
-                cs=cs, recent=recent, max_rows=2304, dtype=DT[dtype])
+                cs=cs, recent=recent, max_rows=max_rows, dtype=DT[dtype])
     torch.cuda.synchronize()
     for i, n in enumerate(lens):
         rows = R.evict(a0[i][:n].cpu().numpy(), b[i], cs, recent)
