@@ -25,6 +25,7 @@ namespace catekv {
 constexpr int kAtWaves = 8;
 constexpr int kAtThreads = kAtWaves * 64;
 constexpr int kAtMaxSeg = kDecodeV2MaxSeg;   // segments described in LDS at a time
+constexpr int kRows8 = 32;                   // rows of an 8-bit tile
 constexpr float kShift = 11.f;
 constexpr float kSlack = 4.f;
 constexpr float kAtFloor = -1e30f;           // maximum of no row: 2^(floor - m) = 0, and no inf - inf
@@ -36,6 +37,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
@@ -179,10 +181,11 @@ struct Rows16 {
 // down to 2^-31 of the largest (below, off by at most 2^-39 of it); an fp32 row is
 // split into two fp16 rows (22 bits).  The block's K scale multiplies the scores
 // in fp32, its V scale the tile's P V sums.
-template <int FMT, typename QT>
+template <int FMT, typename QT, int ROWS>
 struct Kind8 {
-  static constexpr int TOK = 32;
+  static constexpr int TOK = ROWS, H = ROWS / 16;
   static constexpr bool kTail = true;
+  typedef catekv_q8_view View;
   typedef QT T;
   static constexpr int NQ = sizeof(QT) == 4 ? 2 : 1;
   struct Q {
@@ -190,8 +193,8 @@ struct Kind8 {
     float unscale;
   };
   struct Tile {
-    uint4 k[2][2];
-    uint2 v[8];
+    uint4 k[H][2];
+    uint2 v[4 * H];
     float ks, vs;
   };
   __device__ static __forceinline__ void load_q(Q& q, const uint4* row, bool head, int k4) {
@@ -232,18 +235,18 @@ struct Kind8 {
     const char* vp = uniform(sg.v) + (size_t)t * kD;
     const uint32_t ko = n16 * kD + k4 * 16, vo = 4 * k4 * kD + n16 * 8;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < H; ++h)
 #pragma unroll
       for (int j = 0; j < 2; ++j) b.k[h][j] = ldg16(kp + ko + h * 16 * kD + j * 64);
 #pragma unroll
-    for (int r = 0; r < 8; ++r) b.v[r] = ldg8(vp + vo + ((r >> 2) * 16 + (r & 3)) * kD);
+    for (int r = 0; r < 4 * H; ++r) b.v[r] = ldg8(vp + vo + ((r >> 2) * 16 + (r & 3)) * kD);
     b.ks = ldg4f(uniform(sg.ks) + t / block);
     b.vs = ldg4f(uniform(sg.vs) + t / block);
   }
   __device__ static __forceinline__ float factor(const Tile& b, const Q& q, float c) { return b.ks * (c * q.unscale); }
-  __device__ static __forceinline__ void scores(const Tile& b, const Q& q, f32x4 (&S)[2]) {
+  __device__ static __forceinline__ void scores(const Tile& b, const Q& q, f32x4 (&S)[H]) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < H; ++h) {
       f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
@@ -256,32 +259,35 @@ struct Kind8 {
     }
   }
   // P = hi + lo in fp16, 22 bits
-  __device__ static __forceinline__ void pv(const Tile& b, const float (&P)[8], f32x4 (&O)[8]) {
-    uint32_t hi[4], lo[4];
+  __device__ static __forceinline__ void pv(const Tile& b, const float (&P)[4 * H], f32x4 (&O)[8]) {
+    uint32_t hi[2 * H], lo[2 * H];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2 * H; ++i) {
       hi[i] = pack_f16(P[2 * i], P[2 * i + 1]);
       const f32x2 h = unpack_f16(hi[i]);
       lo[i] = pack_f16(P[2 * i] - h.x, P[2 * i + 1] - h.y);
     }
-    const f16x8 A_hi = __builtin_bit_cast(f16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-    const f16x8 A_lo = __builtin_bit_cast(f16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
 #pragma unroll
     for (int half = 0; half < 2; ++half) {      // dims 8 n16 + 4 half + e
-      uint32_t w0[4], w1[4];
-      if (half) {
-        transpose4(b.v[0].y, b.v[1].y, b.v[2].y, b.v[3].y, w0);
-        transpose4(b.v[4].y, b.v[5].y, b.v[6].y, b.v[7].y, w1);
-      } else {
-        transpose4(b.v[0].x, b.v[1].x, b.v[2].x, b.v[3].x, w0);
-        transpose4(b.v[4].x, b.v[5].x, b.v[6].x, b.v[7].x, w1);
+      uint32_t w[H][4];
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        const uint2* v = b.v + 4 * h;
+        if (half) transpose4(v[0].y, v[1].y, v[2].y, v[3].y, w[h]);
+        else transpose4(v[0].x, v[1].x, v[2].x, v[3].x, w[h]);
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const f16x8 B = codes8_to_f16<FMT>(w0[e], w1[e]);
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
-        o = __builtin_amdgcn_mfma_f32_16x16x32_f16(A_hi, B, o, 0, 0, 0);
-        o = __builtin_amdgcn_mfma_f32_16x16x32_f16(A_lo, B, o, 0, 0, 0);
+        if constexpr (H == 2) {
+          const f16x8 B = codes8_to_f16<FMT>(w[0][e], w[H - 1][e]);
+          o = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, make_uint4(hi[0], hi[1], hi[2 * H - 2], hi[2 * H - 1])), B, o, 0, 0, 0);
+          o = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, make_uint4(lo[0], lo[1], lo[2 * H - 2], lo[2 * H - 1])), B, o, 0, 0, 0);
+        } else {
+          const f16x4 B = __builtin_bit_cast(f16x4, codes_to_f16<FMT>(w[0][e]));
+          o = __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4, make_uint2(hi[0], hi[1])), B, o, 0, 0, 0);
+          o = __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4, make_uint2(lo[0], lo[1])), B, o, 0, 0, 0);
+        }
 #pragma unroll
         for (int r = 0; r < 4; ++r) O[4 * half + e][r] = __builtin_fmaf(b.vs, o[r], O[4 * half + e][r]);
       }
@@ -293,6 +299,7 @@ struct Kind8 {
 struct KindBf16 {
   static constexpr int TOK = 16;
   static constexpr bool kTail = false;
+  typedef catekv_kv_ptrs View;
   typedef uint16_t T;
   struct Q {
     uint4 w[4];
@@ -359,6 +366,7 @@ struct KindBf16 {
 struct KindF32 {
   static constexpr int TOK = 16;
   static constexpr bool kTail = false;
+  typedef catekv_kv_ptrs View;
   typedef float T;
   struct Q {
     const uint4* row;
@@ -400,44 +408,45 @@ void attend_stream_kernel(AttendArgs a) {
   __shared__ float s_o[2][WAVES][G][kD];
   __shared__ float s_ml[2][WAVES][2][G];
 
-  // A one-workgroup-per-CU plan lists a worker's segments with their count in one
-  // place; any other has them behind an index, sixteen of them taken at a time.
+  // A one-workgroup-per-CU plan lists a worker's segments in one place, each with
+  // their count; any other has them behind an index, sixteen of them taken at a time.
+  typedef typename K::View View;
+  const View* views = reinterpret_cast<const View*>(a.views);
   const bool v2 = a.variant == kDecodeStreamV2;
-  const V2Item* list = a.v2items + (size_t)blockIdx.x * kAtMaxSeg;
+  V2Item mine{};
+  if (v2) mine = a.v2items[(size_t)blockIdx.x * kAtMaxSeg + min((int)threadIdx.x, kAtMaxSeg - 1)];
   const int seg_lo = v2 ? 0 : a.worker_seg[blockIdx.x];
-  const int seg_hi = v2 ? (int)((uint32_t)list[0].bh_n >> 24) : a.worker_seg[blockIdx.x + 1];
+  const int seg_hi = v2 ? (int)((uint32_t)uniform(mine.bh_n) >> 24) : a.worker_seg[blockIdx.x + 1];
   int sbase = 0;                                 // the worker's score rows given out so far
 
   for (int s0 = seg_lo; s0 < seg_hi; s0 += kAtMaxSeg) {
     const int nseg = min(seg_hi - s0, kAtMaxSeg);
     if ((int)threadIdx.x < nseg) {
-      int bh, t0, t1, slot, part;
+      int bh, t0, t1, slot;
       if (v2) {
-        const V2Item it = list[threadIdx.x];
-        bh = it.bh_n & 0xFFFFFF;
-        t0 = it.t0;
-        t1 = it.t1;
-        slot = it.slot;
-        part = 0;
+        bh = mine.bh_n & 0xFFFFFF;
+        t0 = mine.t0;
+        t1 = mine.t1;
+        slot = mine.slot;
       } else {
         const DecodeItem it = a.items[s0 + threadIdx.x];
         const ViewInfo vi = a.infos[it.bh];
         bh = it.bh;
         t0 = it.t0;
         t1 = it.t1;
-        part = it.part;
-        slot = vi.n_parts > 1 ? vi.first_slot + part : -1;
+        slot = vi.n_parts > 1 ? vi.first_slot + it.part : -1;
       }
       int64_t len = a.lens[bh];
       len = len < 0 ? 0 : len;
+      const View view = views[bh];
       const int b = bh / hkv, h = bh - b * hkv;
       AtSeg sg{};
       sg.t0 = t0;
       const int end = (int)(len < (int64_t)t1 ? len : (int64_t)t1);     // rows [t0, end) of this segment
+      sg.k = reinterpret_cast<const char*>(view.k);
+      sg.v = reinterpret_cast<const char*>(view.v);
+      sg.t_end = end;
       if constexpr (K::kTail) {
-        const catekv_q8_view view = reinterpret_cast<const catekv_q8_view*>(a.views)[bh];
-        sg.k = reinterpret_cast<const char*>(view.k);
-        sg.v = reinterpret_cast<const char*>(view.v);
         sg.ks = view.k_scale;
         sg.vs = view.v_scale;
         sg.kt = reinterpret_cast<const char*>(view.k_tail);
@@ -447,11 +456,6 @@ void attend_stream_kernel(AttendArgs a) {
         const int64_t first = coded > (int64_t)t0 ? coded : (int64_t)t0;
         sg.tail0 = first < (int64_t)end ? (int)(first - coded) : 0;
         sg.tail_n = first < (int64_t)end ? (int)(end - first) : 0;
-      } else {
-        const catekv_kv_ptrs view = reinterpret_cast<const catekv_kv_ptrs*>(a.views)[bh];
-        sg.k = reinterpret_cast<const char*>(view.k);
-        sg.v = reinterpret_cast<const char*>(view.v);
-        sg.t_end = end;
       }
       sg.n_units = sg.t_end > t0 ? (sg.t_end - t0 + TOK - 1) / TOK : 0;
       sg.row0 = b * hq + h * G;
@@ -470,13 +474,16 @@ void attend_stream_kernel(AttendArgs a) {
       }
       for (int s = 0; s < nseg; ++s) sbase += s_seg[s].srows;
     }
-    // the query rows of every segment
-    for (int t = threadIdx.x; t < nseg * G * QW; t += NT) {
+
+    // The query rows of every segment, waited for before any tile is requested: behind
+    // the first tiles of all workgroups they would take 2 us longer.
+    const int nq = nseg * G * QW;
+    auto q_row = [&](int t) {
       const int s = t / (G * QW), r = t - s * (G * QW);
-      s_q[s][r / QW][r % QW] =
-          ldg16(reinterpret_cast<const char*>(a.q) + ((size_t)s_seg[s].row0 + r / QW) * (kD * sizeof(T)) + (r % QW) * 16);
-    }
-    __syncthreads();
+      return ldg16(reinterpret_cast<const char*>(a.q) + ((size_t)s_seg[s].row0 + r / QW) * (kD * sizeof(T)) + (r % QW) * 16);
+    };
+    const int tq = min((int)threadIdx.x, nq - 1);
+    const uint4 qv = q_row(tq);
 
     // ---- this wave's tiles ------------------------------------------------------
     int is = 0, iu = wave;                        // next tile: segment, tile of the segment
@@ -487,6 +494,21 @@ void attend_stream_kernel(AttendArgs a) {
       }
     };
     skip();
+    int n_my = 0;                                 // tiles left to use
+    for (int s = 0; s < nseg; ++s) {
+      const int u = s_seg[s].n_units;
+      n_my += u > wave ? (u - wave + WAVES - 1) / WAVES : 0;
+    }
+    n_my = uniform(n_my);
+    {
+      const int s = tq / (G * QW), r = tq - s * (G * QW);
+      s_q[s][r / QW][r % QW] = qv;
+    }
+    for (int t = threadIdx.x + NT; t < nq; t += NT) {
+      const int s = t / (G * QW), r = t - s * (G * QW);
+      s_q[s][r / QW][r % QW] = q_row(t);
+    }
+    __syncthreads();
     typename K::Tile tb[2];
     auto issue = [&](int buf) {                   // called only while the wave has tiles left
       const AtSeg& sg = s_seg[is];
@@ -629,11 +651,6 @@ void attend_stream_kernel(AttendArgs a) {
     // One tile is in flight while another is used, across segments too, and every
     // issue loads a real tile: the wave's very last tile is used without one.
     // `odd`: the tile to be used next is in buffer 1.
-    int n_my = 0;
-    for (int s = 0; s < nseg; ++s) {
-      const int u = s_seg[s].n_units;
-      n_my += u > wave ? (u - wave + WAVES - 1) / WAVES : 0;
-    }
     if (n_my > 0) issue(0);
     bool odd = false;
     for (int s = 0; s < nseg; ++s) {
@@ -762,28 +779,42 @@ __global__ __launch_bounds__(kAtThreads) void attend_join_kernel(AttendArgs a, i
     const bool v2 = a.variant == kDecodeStreamV2;
     const V2Item* list = a.v2items + (size_t)w * kAtMaxSeg;
     const int seg_lo = v2 ? 0 : a.worker_seg[w];
-    const int seg_hi = v2 ? (int)((uint32_t)list[0].bh_n >> 24) : a.worker_seg[w + 1];
+    int seg_hi = v2 ? 1 : a.worker_seg[w + 1];    // (v2: the first entry tells)
     int64_t soff = 0;
     for (int s = seg_lo; s < seg_hi; ++s) {
       int bh, t0, t1;
       if (v2) {
-        bh = list[s].bh_n & 0xFFFFFF;
-        t0 = list[s].t0;
-        t1 = list[s].t1;
+        const V2Item it = list[s];
+        bh = it.bh_n & 0xFFFFFF;
+        t0 = it.t0;
+        t1 = it.t1;
+        seg_hi = (int)((uint32_t)it.bh_n >> 24);
       } else {
-        bh = a.items[s].bh;
-        t0 = a.items[s].t0;
-        t1 = a.items[s].t1;
+        const DecodeItem it = a.items[s];
+        bh = it.bh;
+        t0 = it.t0;
+        t1 = it.t1;
       }
       const int srows = (t1 - t0 + 63) & ~63;
       const float* sc = a.scores + ((size_t)w * a.score_rows + soff) * G;
       soff += srows;
-      int64_t len = a.lens[bh];
-      const int end = (int)(len < (int64_t)t1 ? len : (int64_t)t1);
-      if (end <= t0) continue;
+      const int64_t len = a.lens[bh];
+      const ViewInfo vi = a.infos[bh];
+      float* acc = a.acc[bh] + t0;
+      const int n = (int)(len < (int64_t)t1 ? len : (int64_t)t1) - t0;
+      if (n <= 0) continue;
+      // the first rows' scores and weights, requested beside the parts
+      constexpr int AHEAD = 4;
+      float x[AHEAD][G], old[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int i = min(u * NT + t, n - 1);
+#pragma unroll
+        for (int g = 0; g < G; ++g) x[u][g] = sc[(size_t)g * srows + i];
+        old[u] = acc[i];
+      }
       // (M, L) of every head of the view, from all of its parts: thread t takes
       // head t % G of the parts t / G, t / G + NT / G, ...
-      const ViewInfo vi = a.infos[bh];
       const float* base = a.slots + (size_t)vi.first_slot * SF + G * kD + (t & (G - 1));
       float M = kAtFloor, L = 0.f;
       for (int p = t / G; p < vi.n_parts; p += NT / G) {
@@ -799,12 +830,12 @@ __global__ __launch_bounds__(kAtThreads) void attend_join_kernel(AttendArgs a, i
         L = L * fast_exp2(M - nm) + pl * fast_exp2(pm - nm);
         M = nm;
       }
-      __syncthreads();                            // the previous segment's values have been read
+      barrier_lds_only();                         // the previous segment's values have been read
       if (lane < G) {
         s_m[wave][lane] = M;
         s_s[wave][lane] = L;
       }
-      __syncthreads();
+      barrier_lds_only();
       float mg[G], ig[G];
 #pragma unroll
       for (int g = 0; g < G; ++g) {
@@ -817,8 +848,15 @@ __global__ __launch_bounds__(kAtThreads) void attend_join_kernel(AttendArgs a, i
         mg[g] = Mx;
         ig[g] = fast_exp2(kShift) / (Lx * (float)G);
       }
-      float* acc = a.acc[bh] + t0;
-      for (int i = t; i < end - t0; i += NT) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int i = u * NT + t;
+        float wsum = 0.f;
+#pragma unroll
+        for (int g = 0; g < G; ++g) wsum += fast_exp2(x[u][g] - mg[g]) * ig[g];
+        if (i < n) acc[i] = __builtin_fmaf(a.decay, old[u], wsum);
+      }
+      for (int i = AHEAD * NT + t; i < n; i += NT) {
         float wsum = 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) wsum += fast_exp2(sc[(size_t)g * srows + i] - mg[g]) * ig[g];

@@ -126,34 +126,41 @@ __device__ __forceinline__ uint2 block_codes(const Eight<T>& x, float scale, flo
   }
 }
 
-// One block by one wave: lane takes dims 8 (lane % 16) .. of the rows lane / 16,
-// lane / 16 + 4, ...  `row(r)`: address of the block's row r.
-template <int FMT, typename T, int BLOCK, typename Row>
-__device__ __forceinline__ void quantize_block(Row row, uint8_t* codes, float* scale_out) {
-  const int lane = threadIdx.x & 63, d0 = (lane & 15) * 8, r0 = lane >> 4;
-  constexpr int N = BLOCK / 4;
+// Rows first, first + 4, ... (N of them) of a block, in one wave: lane takes dims
+// 8 (lane % 16) .. of every fourth row.  `row(r)`: address of the block's row r.
+template <typename T, int N>
+struct BlockRows {
   Eight<T> x[N];
-  uint32_t big = 0;
+  template <typename Row>
+  __device__ __forceinline__ void load(Row row, int first) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int i = 0; i < N; ++i) x[i].load(row(r0 + 4 * i) + d0 * sizeof(T));
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t b = __float_as_uint(x[i].get(j)) & 0x7fffffffu;
-      big = big > b ? big : b;
-    }
-  float scale, inv;
-  block_scale<FMT>(wave_max(big), scale, inv);
-  const bool zero = inv == 0.f;                    // 0 * inf is not 0
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    uint2 c = make_uint2(0, 0);
-    if (!zero) c = block_codes<FMT, T>(x[i], scale, inv);
-    *reinterpret_cast<uint2*>(codes + (r0 + 4 * i) * kD + d0) = c;
+    for (int i = 0; i < N; ++i) x[i].load(row(first + (lane >> 4) + 4 * i) + (lane & 15) * 8 * sizeof(T));
   }
-  if (lane == 0) *scale_out = scale;
-}
+  // largest |x| of the wave's rows, as bits
+  __device__ __forceinline__ uint32_t largest() const {
+    uint32_t big = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t b = __float_as_uint(x[i].get(j)) & 0x7fffffffu;
+        big = big > b ? big : b;
+      }
+    return wave_max(big);
+  }
+  template <int FMT>
+  __device__ __forceinline__ void store(uint8_t* codes, int first, float scale, float inv) const {
+    const int lane = threadIdx.x & 63;
+    const bool zero = inv == 0.f;                  // 0 * inf is not 0
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      uint2 c = make_uint2(0, 0);
+      if (!zero) c = block_codes<FMT, T>(x[i], scale, inv);
+      *reinterpret_cast<uint2*>(codes + (first + (lane >> 4) + 4 * i) * kD + (lane & 15) * 8) = c;
+    }
+  }
+};
 
 // grid: (groups of kQ8Waves blocks x views, views fastest; 1; K and V).  The wave
 // behind a view's last whole block copies the remaining rows into the tail.
@@ -170,9 +177,12 @@ __global__ __launch_bounds__(kQ8Waves * 64) void q8_quantize_kernel(Q8Args a) {
   const catekv_kv_ptrs kv = a.kv[bh];
   const char* src = reinterpret_cast<const char*>(is_v ? kv.v : kv.k) + (size_t)blk * BLOCK * kD * sizeof(T);
   if (blk < whole) {
-    quantize_block<FMT, T, BLOCK>([&](int r) { return src + (size_t)r * kD * sizeof(T); },
-                                  reinterpret_cast<uint8_t*>(is_v ? view.v : view.k) + (size_t)blk * BLOCK * kD,
-                                  (is_v ? view.v_scale : view.k_scale) + blk);
+    BlockRows<T, BLOCK / 4> rows;
+    rows.load([&](int r) { return src + (size_t)r * kD * sizeof(T); }, 0);
+    float scale, inv;
+    block_scale<FMT>(rows.largest(), scale, inv);
+    rows.template store<FMT>(reinterpret_cast<uint8_t*>(is_v ? view.v : view.k) + (size_t)blk * BLOCK * kD, 0, scale, inv);
+    if (lane == 0) (is_v ? view.v_scale : view.k_scale)[blk] = scale;
     return;
   }
   char* dst = reinterpret_cast<char*>(is_v ? view.v_tail : view.k_tail);
@@ -230,29 +240,42 @@ __global__ __launch_bounds__(kQ8Waves * 64) void q8_dequantize_kernel(Q8Args a) 
   for (int i = lane * 16; i < bytes; i += 64 * 16) *reinterpret_cast<uint4*>(dst + i) = ldg16(src + i);
 }
 
-// One workgroup per view: wave 0 K, wave 1 V.  The row that fills a block is
-// taken from the call's arguments, not from the tail it was just stored in.
+// One workgroup per view: four waves for K, four for V, a quarter of a block each
+// when the new row fills it.  That row is taken from the call's arguments, not from
+// the tail it was just stored in.
+constexpr int kAppendThreads = 512;
 template <int FMT, typename T, int BLOCK>
-__global__ __launch_bounds__(128) void q8_append_kernel(Q8Args a) {
-  const int bh = blockIdx.x, lane = threadIdx.x & 63;
-  const bool is_v = threadIdx.x >= 64;
-  const int64_t len = a.lens_rw[bh];
-  if (len < 0 || len >= a.capacity[bh]) {
+__global__ __launch_bounds__(kAppendThreads) void q8_append_kernel(Q8Args a) {
+  const int bh = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = wave & 3;
+  const bool is_v = wave >= 4;
+  __shared__ uint32_t s_big[8];
+  const int64_t len = a.lens_rw[bh], cap = a.capacity[bh];
+  const catekv_q8_view view = a.views[bh];
+  if (len < 0 || len >= cap) {
     if (threadIdx.x == 0 && a.overflow) *a.overflow = 1;
     return;
   }
-  const catekv_q8_view view = a.views[bh];
   const int64_t blk = len / BLOCK;
   const int at = (int)(len - blk * BLOCK);
-  constexpr int kRow = kD * (int)sizeof(T);
+  constexpr int kRow = kD * (int)sizeof(T), kRows = BLOCK / 4;
   const char* fresh = reinterpret_cast<const char*>(is_v ? a.v_new : a.k_new) + (size_t)bh * kRow;
   char* tail = reinterpret_cast<char*>(is_v ? view.v_tail : view.k_tail);
-  if (lane < kRow / 16) *reinterpret_cast<uint4*>(tail + at * kRow + lane * 16) = ldg16(fresh + lane * 16);
-  if (at == BLOCK - 1)
-    quantize_block<FMT, T, BLOCK>([&](int r) { return r == BLOCK - 1 ? fresh : tail + r * kRow; },
-                                  reinterpret_cast<uint8_t*>(is_v ? view.v : view.k) + (size_t)blk * BLOCK * kD,
-                                  (is_v ? view.v_scale : view.k_scale) + blk);
-  __syncthreads();                                 // both waves have read the length
+  const bool full = at == BLOCK - 1;
+  BlockRows<T, kRows / 4> rows;
+  if (full) rows.load([&](int r) { return r == BLOCK - 1 ? fresh : tail + r * kRow; }, part * kRows);
+  if (part == 0 && lane < kRow / 16) *reinterpret_cast<uint4*>(tail + at * kRow + lane * 16) = ldg16(fresh + lane * 16);
+  if (full) {
+    const uint32_t big = rows.largest();
+    if (lane == 0) s_big[wave] = big;
+  }
+  __syncthreads();                                 // all waves have read the length, too
+  if (full) {
+    const uint32_t* b = s_big + (is_v ? 4 : 0);
+    float scale, inv;
+    block_scale<FMT>(max(max(b[0], b[1]), max(b[2], b[3])), scale, inv);
+    rows.template store<FMT>(reinterpret_cast<uint8_t*>(is_v ? view.v : view.k) + (size_t)blk * BLOCK * kD, part * kRows, scale, inv);
+    if (part == 0 && lane == 0) (is_v ? view.v_scale : view.k_scale)[blk] = scale;
+  }
   if (threadIdx.x == 0) a.lens_rw[bh] = len + 1;
 }
 
@@ -270,7 +293,7 @@ static hipError_t launch_q8_t(Q8Op op, const Q8Args& a, hipStream_t stream) {
   else if (op == kDequantize)
     hipLaunchKernelGGL((q8_dequantize_kernel<FMT, T, BLOCK>), grid, block, 0, stream, a);
   else
-    hipLaunchKernelGGL((q8_append_kernel<FMT, T, BLOCK>), dim3(a.n_views), dim3(128), 0, stream, a);
+    hipLaunchKernelGGL((q8_append_kernel<FMT, T, BLOCK>), dim3(a.n_views), dim3(kAppendThreads), 0, stream, a);
   return hipGetLastError();
 }
 
