@@ -410,7 +410,7 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
   int32_t* out = pairs + (size_t)bh * max_moves * 2;
   const int64_t from = (int64_t)nc * a.cs;
   const int rest = (int)((a.q8 ? len / a.block * a.block : len) - from);
-  const int covered = k + (rest + a.cs - 1) / a.cs;
+  const int covered = k + (int)((len - from + a.cs - 1) / a.cs);
   // up to 16384 keys in the lanes' registers, more read again for every pass
   int moves;
   auto load = [&](int c) { return mine[c]; };
@@ -465,7 +465,8 @@ __device__ __forceinline__ void move_elements(E* p, int n_fill, Src src, Dst dst
 // blockIdx.x: view.  blockIdx.y: first the workgroups that shift: one for the weights
 // (and, for codes, one for the scales of K and one for those of V, which they move
 // whole), one per strip of K and of V (16 << strip_log bytes); then `fills` that fill
-// places in K, as many for V, and `acc_fills` for the weights.
+// places in K, as many for V, and `acc_fills` for the weights (none where their
+// shifting workgroup writes the zeros behind them too).
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, const EvictInfo* infos,
                                                                   const int32_t* pairs, int64_t max_moves, int fills,
                                                                   int acc_fills, int strip_log, bool zeros) {
@@ -479,7 +480,8 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, c
     // elements of a chunk: its rows' weights, or its blocks' scales
     const int per = y == 0 ? cs : cs / a.block;
     float* p = y == 0 ? a.acc[bh] : y == 1 ? a.q8[bh].k_scale : a.q8[bh].v_scale;
-    const int fill = y == 0 ? f.lead : f.moves;
+    // with the zeros all of them: they may cover any source of a pair
+    const int fill = y == 0 && !zeros ? f.lead : f.moves;
     const int behind = y == 0 ? (int)((int64_t)f.len - (int64_t)f.nc * cs) : f.rest / a.block;
     move_elements(p, fill * per,
                   [&](int i) { const int q = i / per; return (size_t)pr[q].y * per + (i - q * per); },
@@ -595,7 +597,7 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
   int strip_log = 2;
   while ((16 << strip_log) < a.row_bytes && 2 * ((int64_t)a.recent + a.cs) * (32 << strip_log) <= kTurn) ++strip_log;
   const int64_t acc_turns = (moves * a.cs + kMoveThreads * kMoveBatch - 1) / (kMoveThreads * kMoveBatch);
-  const int acc_fills = (int)(acc_turns < room / 4 + 1 ? acc_turns : room / 4 + 1);
+  const int acc_fills = !keys ? 0 : (int)(acc_turns < room / 4 + 1 ? acc_turns : room / 4 + 1);
   const int shifts = (a.q8 ? 3 : 1) + 2 * ((a.row_bytes / 16) >> strip_log);
   hipLaunchKernelGGL(evict_move_kernel, dim3(a.n_views, shifts + 2 * fills + acc_fills), dim3(kMoveThreads), 0, stream, a,
                      infos, pairs, moves, fills, acc_fills, strip_log, keys == nullptr);

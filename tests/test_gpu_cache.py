@@ -479,6 +479,50 @@ def test_evict_8_bit(kind, fmt, dtype, block, cs, recent):
         assert same(a[i][:m], a0[i][torch.from_numpy(rows).to(DEV)]) and not a[i][m:n].any(), i
 
 
+@pytest.mark.parametrize("kind,n,cs,max_rows", [("dense", 2304, 8, 2304), ("dense", 2304, 8, 20000),
+                                                ("int8", 2335, 32, 2400), ("int8", 2335, 32, 20000),
+                                                ("e4m3", 3071, 64, 20000)])
+def test_evict_many_views(kind, n, cs, max_rows):
+    # many workgroups per view at work at once: what one of them writes, another may not have
+    # read yet
+    rng = np.random.default_rng(35)
+    V, recent = 160, 64
+    lens = [n - int(x) for x in rng.integers(0, 300, V)]
+    a = torch.from_numpy(np.exp(2 * rng.standard_normal((V, n))).astype(np.float32)).to(DEV)
+    a0, new = a.clone(), lens_of(*lens)
+    b = [int(x) for x in rng.integers(0, n // cs, V)]
+    budget, table = torch.tensor(b, dtype=torch.int32, device=DEV), ck.acc_table([x.data_ptr() for x in a], DEV)
+    if kind == "dense":
+        k = torch.randint(-30000, 30000, (V, n, D), dtype=torch.int16, device=DEV).view(torch.bfloat16)
+        v = torch.randint(-30000, 30000, (V, n, D), dtype=torch.int16, device=DEV).view(torch.bfloat16)
+        kv = ck.kv_table([(x.data_ptr(), y.data_ptr()) for x, y in zip(k, v)], DEV)
+        old = k.clone(), v.clone()
+        ck.evict_kv(kv, new, table, budget, cs=cs, recent=recent, max_rows=max_rows, dtype=torch.bfloat16)
+    else:
+        q8 = ck.q8_alloc([n] * V, DEV, fmt=kind, block=cs, dtype=torch.bfloat16)
+        for i in range(V):
+            for j in range(2):
+                q8.hold[6 * i + j].copy_(torch.randint(-100, 100, q8.hold[6 * i + j].shape, dtype=torch.int8))
+                q8.hold[6 * i + 2 + j].copy_(torch.rand(q8.hold[6 * i + 2 + j].shape))
+        old = [t.clone() for t in q8.hold]
+        ck.evict_kv_q8(q8, new, table, budget, cs=cs, recent=recent, max_rows=max_rows)
+    torch.cuda.synchronize()
+    for i, m in enumerate(lens):
+        rows = R.evict(a0[i, :m].cpu().numpy(), b[i], cs, recent)
+        at = torch.from_numpy(rows).to(DEV)
+        assert int(new[i]) == len(rows), i
+        assert same(a[i, :len(rows)], a0[i, at]) and not a[i, len(rows):m].any() and same(a[i, m:], a0[i, m:]), i
+        if kind == "dense":
+            assert same(k[i, :len(rows)], old[0][i, at]) and same(v[i, :len(rows)], old[1][i, at]), i
+            assert same(k[i, len(rows):], old[0][i, len(rows):]), i
+        else:
+            nb = len(rows) // cs
+            for j in range(2):
+                assert same(q8.hold[6 * i + j][:nb * cs], old[6 * i + j][at[:nb * cs]]), i
+                assert same(q8.hold[6 * i + 2 + j][:nb], old[6 * i + 2 + j][at[:nb * cs:cs] // cs]), i
+                assert same(q8.hold[6 * i + 4 + j], old[6 * i + 4 + j]), i
+
+
 @pytest.mark.parametrize("n,cs,budget", [(70001, 1, 20000), (70001, 1, 60000), (40000, 1, 32768), (300000, 8, 5000)])
 def test_evict_long_views(n, cs, budget):
     # more chunks than a workgroup keeps in LDS, beside a short view and one that stays
