@@ -407,6 +407,7 @@ void attend_stream_kernel(AttendArgs a) {
   __shared__ uint4 s_q[kAtMaxSeg][G][QW];
   __shared__ float s_o[2][WAVES][G][kD];
   __shared__ float s_ml[2][WAVES][2][G];
+  extern __shared__ float4 s_scores[];           // the worker's scores, where they fit (a.staged)
 
   // A one-workgroup-per-CU plan lists a worker's segments in one place, each with
   // their count; any other has them behind an index, sixteen of them taken at a time.
@@ -562,8 +563,10 @@ void attend_stream_kernel(AttendArgs a) {
     // x of 16 rows into the worker's scores, four rows of a head per lane
     auto keep_scores = [&](const AtSeg& sg, int t, f32x4 S, float kf) {
       if (head_lane) {
-        float* p = a.scores + ((size_t)blockIdx.x * a.score_rows + sg.soff) * G + (size_t)n16 * sg.srows + (t - sg.t0) + 4 * k4;
-        *reinterpret_cast<float4*>(p) = make_float4(S[0] * kf, S[1] * kf, S[2] * kf, S[3] * kf);
+        const size_t at = (size_t)sg.soff * G + (size_t)n16 * sg.srows + (t - sg.t0) + 4 * k4;
+        const float4 x = make_float4(S[0] * kf, S[1] * kf, S[2] * kf, S[3] * kf);
+        if (a.staged) s_scores[at >> 2] = x;
+        else *reinterpret_cast<float4*>(a.scores + (size_t)blockIdx.x * a.score_rows * G + at) = x;
       }
     };
 
@@ -693,6 +696,10 @@ void attend_stream_kernel(AttendArgs a) {
       merge(s);
     }
     __syncthreads();                              // the tables and the merge area are free
+    if (ACC && a.staged) {                        // (a plan of one batch of segments)
+      float4* to = reinterpret_cast<float4*>(a.scores + (size_t)blockIdx.x * a.score_rows * G);
+      for (int i = threadIdx.x; i < sbase * G / 4; i += NT) to[i] = s_scores[i];
+    }
   }
 }
 
@@ -866,9 +873,27 @@ __global__ __launch_bounds__(kAtThreads) void attend_join_kernel(AttendArgs a, i
   }
 }
 
+// Static LDS of the stream kernel, rounded up generously.
+constexpr size_t kAtMaxLds = 160 * 1024;
+constexpr int64_t kStagedRows = 1200;
+template <class K, int G>
+constexpr size_t attend_static_lds() {
+  return kAtMaxSeg * (sizeof(AtSeg) + G * kD * sizeof(typename K::T)) + 2 * kAtWaves * G * (kD + 2) * sizeof(float) + 1024;
+}
+
 template <class K, int G, bool ACC>
 static hipError_t launch_attend_t(const AttendArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((attend_stream_kernel<K, G, ACC>), dim3(a.n_workers), dim3(kAtThreads), 0, stream, a);
+  // The scores of a share of more than kStagedRows rows stay in LDS until its end, where
+  // they fit beside the rest (4 heads: 6000 rows): stored tile by tile among the
+  // loads they cost 5.8 us of a 128K bf16 step of 45, at the end 2.5.  us per step,
+  // tile by tile / staged, by rows of a share: bf16 620: 24.0 / 24.0, 1200: 43.1 /
+  // 41.0, 2050: 68.1 / 63.0; int8 830: 24.2 / 24.6, 1600: 35.4 / 34.2, 4700: 87.6 / 81.5.
+  const size_t lds = ACC && a.variant == kDecodeStreamV2 && a.score_rows > kStagedRows
+                         ? (size_t)a.score_rows * G * sizeof(float) : 0;
+  const bool staged = lds > 0 && lds + attend_static_lds<K, G>() <= kAtMaxLds;
+  AttendArgs b = a;
+  b.staged = staged;
+  hipLaunchKernelGGL((attend_stream_kernel<K, G, ACC>), dim3(a.n_workers), dim3(kAtThreads), staged ? lds : 0, stream, b);
   const int n_joins = a.n_multi > 0 ? a.n_views * G : 0;
   const int blocks = n_joins + (ACC ? a.n_workers : 0);
   if (blocks > 0)

@@ -51,6 +51,7 @@ struct AttendArgs {
   float* const* acc;               // one array per view; null without weights
   float decay;
   int n_workers, n_views, n_multi, hkv, variant, block;
+  bool staged;                     // the stream kernel keeps its scores in LDS until its end
   float scale;
   float* out;
   float* lse;

@@ -4,7 +4,7 @@
 // All three move bytes and little else (quantize: 2 row bytes read and one
 // written per element pair), so a wave takes one block of K or of V whole: the
 // rows go through its registers once, the maximum is taken of the bit patterns
-// on the way, and the codes leave in 8-byte stores, eight elements per lane.
+// on the way, and both sides are read and written in whole lines.
 #include "cache.h"
 #include "common.h"
 
@@ -13,16 +13,13 @@ namespace catekv {
 constexpr float kTinyMax = 7.888609052210118e-31f;   // 2^-100
 constexpr int kQ8Waves = 4;
 
-typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
-
-// Eight consecutive elements as fp32.
+// 16 bytes of a row: kN elements.
 template <typename T>
-struct Eight;
+struct Piece;
 template <>
-struct Eight<uint16_t> {
+struct Piece<uint16_t> {
+  static constexpr int kN = 8;
   uint4 w;
-  __device__ __forceinline__ void load(const void* p) { w = ldg16(p); }
-  __device__ __forceinline__ void store(void* p) const { *reinterpret_cast<uint4*>(p) = w; }
   __device__ __forceinline__ float get(int i) const {
     const uint32_t x = i < 2 ? w.x : i < 4 ? w.y : i < 6 ? w.z : w.w;
     return i & 1 ? bf16_hi(x) : bf16_lo(x);
@@ -37,24 +34,12 @@ struct Eight<uint16_t> {
   }
 };
 template <>
-struct Eight<float> {
-  uint4 w[2];
-  __device__ __forceinline__ void load(const void* p) {
-    w[0] = ldg16(p);
-    w[1] = ldg16(reinterpret_cast<const char*>(p) + 16);
-  }
-  __device__ __forceinline__ void store(void* p) const {
-    reinterpret_cast<uint4*>(p)[0] = w[0];
-    reinterpret_cast<uint4*>(p)[1] = w[1];
-  }
-  __device__ __forceinline__ float get(int i) const {
-    const uint4& q = w[i >> 2];
-    const int j = i & 3;
-    return __uint_as_float(j == 0 ? q.x : j == 1 ? q.y : j == 2 ? q.z : q.w);
-  }
-  __device__ __forceinline__ void set(const float (&f)[8]) {
-    w[0] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-    w[1] = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
+struct Piece<float> {
+  static constexpr int kN = 4;
+  uint4 w;
+  __device__ __forceinline__ float get(int i) const { return __uint_as_float(i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w); }
+  __device__ __forceinline__ void set(const float (&f)[4]) {
+    w = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
   }
 };
 
@@ -87,55 +72,63 @@ __device__ __forceinline__ void block_scale(uint32_t big, float& scale, float& i
   }
 }
 
-// Codes of eight elements.  int8: x inv is within 2^-15 of the quotient x / scale,
-// which decides the rounding except next to a border between two codes; such
-// elements (1 in 10^4) are divided in fp64, whose quotient lies on a border only
-// if the exact one does.  e4m3: x inv is exact, the conversion rounds to nearest even.
+// Codes of a piece, one word per four elements.  int8: x inv is within 2^-15 of the
+// quotient x / scale, which decides the rounding except next to a border between
+// two codes; such elements (1 in 10^4) are divided in fp64, whose quotient lies on
+// a border only if the exact one does.  e4m3: x inv is exact, the conversion
+// rounds to nearest even.
 template <int FMT, typename T>
-__device__ __forceinline__ uint2 block_codes(const Eight<T>& x, float scale, float inv) {
+__device__ __forceinline__ void piece_codes(const Piece<T>& x, float scale, float inv, uint32_t (&w)[Piece<T>::kN / 4]) {
+  constexpr int N = Piece<T>::kN;
   if constexpr (FMT == CATEKV_I8) {
-    float r[8];
+    float r[N];
     float off = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < N; ++i) {
       const float y = x.get(i) * inv;
       r[i] = __builtin_rintf(y);
       off = fmaxf(off, fabsf(y - r[i]));
     }
     if (__builtin_amdgcn_ballot_w64(off > 0.4999f)) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        r[i] = (float)__builtin_rint((double)x.get(i) / (double)scale);
+      for (int i = 0; i < N; ++i) r[i] = (float)__builtin_rint((double)x.get(i) / (double)scale);
     }
-    uint32_t w[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < N / 4; ++h) {
       w[h] = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[h] |= ((uint32_t)(int)r[4 * h + i] & 0xffu) << (8 * i);
     }
-    return make_uint2(w[0], w[1]);
   } else {
-    int w[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(x.get(4 * h) * inv, x.get(4 * h + 1) * inv, 0, false);
-      w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(x.get(4 * h + 2) * inv, x.get(4 * h + 3) * inv, w[h], true);
+    for (int h = 0; h < N / 4; ++h) {
+      int c = __builtin_amdgcn_cvt_pk_fp8_f32(x.get(4 * h) * inv, x.get(4 * h + 1) * inv, 0, false);
+      c = __builtin_amdgcn_cvt_pk_fp8_f32(x.get(4 * h + 2) * inv, x.get(4 * h + 3) * inv, c, true);
+      w[h] = (uint32_t)c;
     }
-    return make_uint2((uint32_t)w[0], (uint32_t)w[1]);
   }
 }
 
-// Rows first, first + 4, ... (N of them) of a block, in one wave: lane takes dims
-// 8 (lane % 16) .. of every fourth row.  `row(r)`: address of the block's row r.
-template <typename T, int N>
+template <int W>
+__device__ __forceinline__ void store_words(uint8_t* p, const uint32_t (&w)[W]) {
+  if constexpr (W == 2) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+  else *reinterpret_cast<uint32_t*>(p) = w[0];
+}
+
+// ROWS rows of a block in one wave, from row `first` on: a lane takes 16 bytes of
+// every 64-lane load, which covers two fp32 rows or four bf16 rows whole.
+// `row(r)`: address of the block's row r.
+template <typename T, int ROWS>
 struct BlockRows {
-  Eight<T> x[N];
+  static constexpr int kPer = kD / Piece<T>::kN;   // lanes of a row
+  static constexpr int kStep = 64 / kPer;          // rows of a load
+  static constexpr int N = ROWS / kStep;
+  Piece<T> x[N];
   template <typename Row>
   __device__ __forceinline__ void load(Row row, int first) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i].load(row(first + (lane >> 4) + 4 * i) + (lane & 15) * 8 * sizeof(T));
+    for (int i = 0; i < N; ++i) x[i].w = ldg16(row(first + lane / kPer + kStep * i) + (lane % kPer) * 16);
   }
   // largest |x| of the wave's rows, as bits
   __device__ __forceinline__ uint32_t largest() const {
@@ -143,7 +136,7 @@ struct BlockRows {
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < Piece<T>::kN; ++j) {
         const uint32_t b = __float_as_uint(x[i].get(j)) & 0x7fffffffu;
         big = big > b ? big : b;
       }
@@ -155,9 +148,9 @@ struct BlockRows {
     const bool zero = inv == 0.f;                  // 0 * inf is not 0
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      uint2 c = make_uint2(0, 0);
-      if (!zero) c = block_codes<FMT, T>(x[i], scale, inv);
-      *reinterpret_cast<uint2*>(codes + (first + (lane >> 4) + 4 * i) * kD + (lane & 15) * 8) = c;
+      uint32_t w[Piece<T>::kN / 4] = {};
+      if (!zero) piece_codes<FMT, T>(x[i], scale, inv, w);
+      store_words(codes + (first + lane / kPer + kStep * i) * kD + (lane % kPer) * Piece<T>::kN, w);
     }
   }
 };
@@ -177,7 +170,7 @@ __global__ __launch_bounds__(kQ8Waves * 64) void q8_quantize_kernel(Q8Args a) {
   const catekv_kv_ptrs kv = a.kv[bh];
   const char* src = reinterpret_cast<const char*>(is_v ? kv.v : kv.k) + (size_t)blk * BLOCK * kD * sizeof(T);
   if (blk < whole) {
-    BlockRows<T, BLOCK / 4> rows;
+    BlockRows<T, BLOCK> rows;
     rows.load([&](int r) { return src + (size_t)r * kD * sizeof(T); }, 0);
     float scale, inv;
     block_scale<FMT>(rows.largest(), scale, inv);
@@ -205,33 +198,34 @@ __global__ __launch_bounds__(kQ8Waves * 64) void q8_dequantize_kernel(Q8Args a) 
   if (blk < whole) {
     const char* src = reinterpret_cast<const char*>(is_v ? view.v : view.k) + (size_t)blk * BLOCK * kD;
     const float scale = (is_v ? view.v_scale : view.k_scale)[blk];
-    constexpr int N = BLOCK * kD / 16 / 64;
-    uint4 w[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = ldg16(src + (i * 64 + lane) * 16);
+    // a lane takes the codes of 16 bytes of every 64-lane store
+    constexpr int E = Piece<T>::kN, N = BLOCK * kD / E / 64;
+    uint32_t c[N][E / 4];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const uint32_t c[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+      const uint32_t* p = reinterpret_cast<const uint32_t*>(src + (i * 64 + lane) * E);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float f[8];
+      for (int h = 0; h < E / 4; ++h) c[i][h] = p[h];
+    }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint32_t x = c[2 * h + (j >> 2)];
-          if constexpr (FMT == CATEKV_I8) {
-            f[j] = (float)(int8_t)(x >> (8 * (j & 3)));
-          } else {
-            f[j] = (j & 3) == 0   ? __builtin_amdgcn_cvt_f32_fp8(x, 0)
-                   : (j & 3) == 1 ? __builtin_amdgcn_cvt_f32_fp8(x, 1)
-                   : (j & 3) == 2 ? __builtin_amdgcn_cvt_f32_fp8(x, 2)
-                                  : __builtin_amdgcn_cvt_f32_fp8(x, 3);
-          }
-          f[j] *= scale;
+    for (int i = 0; i < N; ++i) {
+      float f[E];
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        const uint32_t x = c[i][j >> 2];
+        if constexpr (FMT == CATEKV_I8) {
+          f[j] = (float)(int8_t)(x >> (8 * (j & 3)));
+        } else {
+          f[j] = (j & 3) == 0   ? __builtin_amdgcn_cvt_f32_fp8(x, 0)
+                 : (j & 3) == 1 ? __builtin_amdgcn_cvt_f32_fp8(x, 1)
+                 : (j & 3) == 2 ? __builtin_amdgcn_cvt_f32_fp8(x, 2)
+                                : __builtin_amdgcn_cvt_f32_fp8(x, 3);
         }
-        Eight<T> o;
-        o.set(f);
-        o.store(dst + ((i * 64 + lane) * 16 + 8 * h) * sizeof(T));
+        f[j] *= scale;
       }
+      Piece<T> o;
+      o.set(f);
+      *reinterpret_cast<uint4*>(dst + (size_t)(i * 64 + lane) * 16) = o.w;
     }
     return;
   }
@@ -261,7 +255,7 @@ __global__ __launch_bounds__(kAppendThreads) void q8_append_kernel(Q8Args a) {
   const char* fresh = reinterpret_cast<const char*>(is_v ? a.v_new : a.k_new) + (size_t)bh * kRow;
   char* tail = reinterpret_cast<char*>(is_v ? view.v_tail : view.k_tail);
   const bool full = at == BLOCK - 1;
-  BlockRows<T, kRows / 4> rows;
+  BlockRows<T, kRows> rows;
   if (full) rows.load([&](int r) { return r == BLOCK - 1 ? fresh : tail + r * kRow; }, part * kRows);
   if (part == 0 && lane < kRow / 16) *reinterpret_cast<uint4*>(tail + at * kRow + lane * 16) = ldg16(fresh + lane * 16);
   if (full) {
