@@ -1,11 +1,14 @@
 // Eviction by accumulated weight: which chunks of a view stay, and the moves.
 //
 // The chunks' largest weights become ordered 32-bit keys, in the selecting
-// workgroup itself or, for long views, in a launch of their own.  One workgroup
-// per view selects: few chunks by counting, for each, the better ones; more by a
-// radix selection of the k-th largest key in up to three digits, the keys in
-// registers (above 16384, read for every pass).  It lists the pairs (place that
-// becomes free below k, kept chunk from k on) in ascending order.
+// workgroup itself or, for long views, in a launch of their own.  Up to kOneChunks
+// chunks one workgroup per view selects: few chunks by counting, for each, the
+// better ones; more by a radix selection of the k-th largest key in up to three
+// digits, the keys in registers.  It lists the pairs (place that becomes free below
+// k, kept chunk from k on) in ascending order.  More chunks are counted by many
+// workgroups, a launch per digit, one for the counts that place their pairs and one
+// that lists them (73000 chunks of 8 views: 144 us per eviction with one workgroup
+// per view, of which 29 must move).
 //
 // One launch moves.  The pairs' sources lie from k on, their places below, so all
 // of them move at once, whole chunks at a time.  The rows behind the chunks
@@ -26,6 +29,8 @@ constexpr int64_t kMaxEvictRows = 1 << 26;   // 32 pieces a row, a workgroup per
 constexpr int kMaxEvictChunk = 1 << 20;      // element, piece and workgroup numbers stay below 2^31
 constexpr int kMaxEvictViews = 1 << 16;
 constexpr int kRankChunks = 384;        // up to here a chunk's rank is counted
+constexpr int kOneChunks = 16 * kEvictThreads;   // most chunks of a selecting workgroup
+constexpr int kGroupChunks = 4 * kEvictThreads;  // chunks of one of many
 constexpr int kOwnKeyRows = 16384;      // views up to here: keys by the selecting workgroup
 constexpr int kKeyRows = 4096;          // else by a workgroup per so many rows
 
@@ -35,9 +40,18 @@ struct EvictInfo {
   int32_t shift;                        // rows dropped
   int32_t rest;                         // rows of K and V behind the chunks (8 bits: those in codes)
   int32_t lead;                         // pairs whose source the shifted rows will cover
+  uint32_t limit;                       // keys above it stay, and the first `ties` equal ones
+  int32_t ties;
 };
 
-// Workspace: infos, the pairs of every view, then (long views) their keys.
+// What a group of kGroupChunks chunks holds: keys above the limit and equal to it,
+// below chunk k and from there on.
+struct GroupCount {
+  int32_t above_lo, equal_lo, above_hi, equal_hi;
+};
+
+// Workspace: infos, the pairs of every view, then (long views) their keys, and
+// (many chunks) the digits' histograms and the groups' counts.
 static size_t info_bytes(int n_views) { return ((size_t)n_views * sizeof(EvictInfo) + 255) & ~(size_t)255; }
 static int64_t max_chunks_of(int64_t max_rows, int cs) { return max_rows / cs; }
 // at most half of the chunks can change places: min(k, nc - k)
@@ -45,10 +59,15 @@ static int64_t max_moves_of(int64_t chunks) { return chunks / 2 + 1; }
 static size_t pairs_bytes(int n_views, int64_t chunks) {
   return ((size_t)n_views * (size_t)max_moves_of(chunks) * 2 * sizeof(int32_t) + 255) & ~(size_t)255;
 }
+static size_t key_bytes(int n_views, int64_t chunks) { return ((size_t)n_views * (size_t)chunks * sizeof(uint32_t) + 255) & ~(size_t)255; }
+static int64_t groups_of(int64_t chunks) { return (chunks + kGroupChunks - 1) / kGroupChunks; }
+static size_t hist_bytes(int n_views) { return (size_t)n_views * 3 * kBins * sizeof(uint32_t); }
 size_t evict_workspace_bytes(int n_views, int64_t max_rows, int cs) {
   const int64_t chunks = max_chunks_of(max_rows, cs);
-  const size_t keys = max_rows > kOwnKeyRows ? (size_t)n_views * (size_t)chunks * sizeof(uint32_t) : 0;
-  return info_bytes(n_views) + pairs_bytes(n_views, chunks) + ((keys + 255) & ~(size_t)255);
+  size_t bytes = info_bytes(n_views) + pairs_bytes(n_views, chunks);
+  if (max_rows > kOwnKeyRows) bytes += key_bytes(n_views, chunks);
+  if (chunks > kOneChunks) bytes += hist_bytes(n_views) + (size_t)n_views * groups_of(chunks) * sizeof(GroupCount);
+  return bytes;
 }
 
 bool evict_fits(int n_views, int64_t max_rows, int cs) {
@@ -166,11 +185,11 @@ struct Run {
 
 // The pairs of a view's chunks.  rows(f): f(row number, first chunk) for every row
 // of this wave; stays(row, c): whether c, a chunk of the wave, stays, asked in order
-// after each reset().  Returns the number of pairs; s.lead gets that of those whose
-// source lies below `covered`.
+// after each reset().  h, m: places and sources before this workgroup's chunks.
+// Returns the number of its places; s.lead gets that of its sources below `covered`.
 template <typename Rows, typename Reset, typename Stays>
 __device__ __forceinline__ int list_pairs(SelectShared& s, Run run, int k, int covered, int32_t* pairs, Rows rows, Reset reset,
-                                          Stays stays) {
+                                          Stays stays, int h = 0, int m = 0) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint64_t below = lane ? ~0ull >> (64 - lane) : 0;
   int holes = 0, movers = 0;
@@ -189,7 +208,7 @@ __device__ __forceinline__ int list_pairs(SelectShared& s, Run run, int k, int c
   }
   if (threadIdx.x == 0) s.lead = 0;
   __syncthreads();
-  int total = 0, h = 0, m = 0;
+  int total = 0;
 #pragma unroll
   for (int w = 0; w < kEvictWaves; ++w) {
     h += w < wave ? s.part[w] : 0;
@@ -350,25 +369,203 @@ __device__ __forceinline__ int register_pairs(SelectShared& s, Load load, int nc
   return list_pairs(s, run, k, covered, pairs, rows, [] {}, [&](int i, int) { return (bits >> i & 1) != 0; });
 }
 
-// Any number of keys, read for every pass.
-template <typename Load>
-__device__ __forceinline__ int memory_pairs(SelectShared& s, Load load, int nc, int k, int covered, int32_t* pairs) {
-  const int wave = threadIdx.x >> 6, size = (nc + kEvictThreads - 1) / kEvictThreads * 64;
-  const Run run{min(nc, wave * size), min(nc, (wave + 1) * size)};
-  auto rows = [&](auto f) {
-    for (int c0 = run.lo; c0 < run.hi; c0 += 64) f(0, c0);
-  };
-  auto key = [&](int, int c) { return load(min(c, nc - 1)); };
-  uint32_t limit;
-  int ties, tie = 0;
-  radix_limit(s, run, rows, key, k, limit, ties);
-  const int tie0 = ties > 0 ? ties_before(s, run, rows, key, limit) : 0;
-  return list_pairs(s, run, k, covered, pairs, rows, [&] { tie = tie0; },
-                    [&](int i, int c) { return stays_at(key(i, c), c < run.hi, limit, ties, tie); });
+// Rows behind the competing chunks: all of them (whose chunks' worth of places after
+// k the shift covers), and those of K and V that move (8 bits: the ones in codes).
+__device__ __forceinline__ EvictInfo evict_info(const EvictArgs& a, int64_t len, int nc, int k) {
+  const int64_t from = (int64_t)nc * a.cs;
+  EvictInfo f{};
+  f.nc = nc;
+  f.k = k;
+  f.len = (int32_t)len;
+  f.shift = (nc - k) * a.cs;
+  f.rest = (int)((a.q8 ? len / a.block * a.block : len) - from);
+  return f;
+}
+__device__ __forceinline__ int covered_below(const EvictInfo& f, int cs) {
+  return f.k + (int)(((int64_t)f.len - (int64_t)f.nc * cs + cs - 1) / cs);
 }
 
-// Keys of long views: workgroups over kKeyRows rows each.
-__global__ __launch_bounds__(kEvictThreads) void evict_keys_kernel(EvictArgs a, uint32_t* keys, int64_t max_chunks, int per_wg) {
+// ---- many chunks: a workgroup per group, a launch per step ----------------------
+__global__ __launch_bounds__(kEvictThreads) void evict_clear_kernel(uint32_t* hist, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * kEvictThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kEvictThreads) hist[i] = 0;
+}
+
+// A workgroup's histogram in LDS added to the view's.
+__device__ __forceinline__ void add_hist(const SelectShared& s, uint32_t* hist) {
+  __syncthreads();
+  for (int i = threadIdx.x; i < kBins; i += kEvictThreads)
+    if (s.hist[i]) atomicAdd(&hist[i], s.hist[i]);
+}
+
+// The digits decided by the first n of the view's histograms: limit so far (its lower
+// bits 0) and how many of its keys stay; false: all of a bin stays, nothing is open.
+__device__ __forceinline__ bool decide(SelectShared& s, const uint32_t* hist, int n, int k, uint32_t& limit, int& ties) {
+  const int t = threadIdx.x;
+  limit = 0xffffffffu;
+  ties = 0;
+  if (k == 0) return false;
+  uint32_t prefix = 0;
+  ties = k;
+#pragma unroll 1
+  for (int p = 0; p < n; ++p) {
+    __syncthreads();
+    s.hist[t] = hist[p * kBins + t];
+    s.hist[t + kEvictThreads] = hist[p * kBins + t + kEvictThreads];
+    __syncthreads();
+    find_digit(s, ties);
+    prefix |= s.digit << (p == 0 ? 21 : p == 1 ? 10 : 0);
+    ties -= s.above;
+    limit = prefix;
+    if (ties == s.inside && prefix != 0) {
+      limit = prefix - 1;
+      ties = 0;
+      return false;
+    }
+  }
+  return true;
+}
+
+// Digit P (1 or 2) of the keys that share the digits before it.
+template <int P>
+__global__ __launch_bounds__(kEvictThreads) void evict_digit_kernel(EvictArgs a, const uint32_t* keys, uint32_t* hist,
+                                                                    int64_t max_chunks) {
+  __shared__ SelectShared s;
+  const int group = blockIdx.x / a.n_views, bh = blockIdx.x - group * a.n_views, t = threadIdx.x;
+  int64_t len;
+  int nc, k;
+  if (!evict_view(a, bh, len, nc, k) || (int64_t)group * kGroupChunks >= nc) return;
+  uint32_t x[4];
+  const uint32_t* mine = keys + (size_t)bh * max_chunks;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) x[u] = mine[min(group * kGroupChunks + u * kEvictThreads + t, nc - 1)];
+  uint32_t* h = hist + (size_t)bh * 3 * kBins;
+  uint32_t limit;
+  int ties;
+  if (!decide(s, h, P, k, limit, ties)) return;
+  __syncthreads();
+  s.hist[t] = 0;
+  s.hist[t + kEvictThreads] = 0;
+  __syncthreads();
+  constexpr int sh = P == 1 ? 10 : 0, bits = P == 1 ? 11 : 10;
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+    if (group * kGroupChunks + u * kEvictThreads + t < nc && (x[u] >> (sh + bits)) == (limit >> (sh + bits)))
+      atomicAdd(&s.hist[(x[u] >> sh) & ((1u << bits) - 1)], 1u);
+  add_hist(s, h + P * kBins);
+}
+
+// The limit, and every group's counts.
+__global__ __launch_bounds__(kEvictThreads) void evict_count_kernel(EvictArgs a, EvictInfo* infos, const uint32_t* keys,
+                                                                    const uint32_t* hist, GroupCount* counts,
+                                                                    int64_t max_chunks, int groups) {
+  __shared__ SelectShared s;
+  __shared__ GroupCount total;
+  const int group = blockIdx.x / a.n_views, bh = blockIdx.x - group * a.n_views, t = threadIdx.x, lane = t & 63;
+  int64_t len;
+  int nc, k;
+  if (!evict_view(a, bh, len, nc, k)) {
+    if (group == 0 && t == 0) infos[bh] = EvictInfo{};
+    return;
+  }
+  if ((int64_t)group * kGroupChunks >= nc) return;
+  uint32_t x[4];
+  const uint32_t* mine = keys + (size_t)bh * max_chunks;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) x[u] = mine[min(group * kGroupChunks + u * kEvictThreads + t, nc - 1)];
+  if (t == 0) total = GroupCount{};
+  uint32_t limit;
+  int ties;
+  decide(s, hist + (size_t)bh * 3 * kBins, 3, k, limit, ties);
+  __syncthreads();
+  GroupCount n{};
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int c = group * kGroupChunks + u * kEvictThreads + t;
+    const bool above = c < nc && x[u] > limit, equal = c < nc && x[u] == limit;
+    n.above_lo += __popcll(__builtin_amdgcn_ballot_w64(above && c < k));
+    n.equal_lo += __popcll(__builtin_amdgcn_ballot_w64(equal && c < k));
+    n.above_hi += __popcll(__builtin_amdgcn_ballot_w64(above && c >= k));
+    n.equal_hi += __popcll(__builtin_amdgcn_ballot_w64(equal && c >= k));
+  }
+  if (lane == 0) {
+    atomicAdd(&total.above_lo, n.above_lo);
+    atomicAdd(&total.equal_lo, n.equal_lo);
+    atomicAdd(&total.above_hi, n.above_hi);
+    atomicAdd(&total.equal_hi, n.equal_hi);
+  }
+  __syncthreads();
+  if (t == 0) {
+    counts[(size_t)bh * groups + group] = total;
+    if (group == 0) {
+      EvictInfo f = evict_info(a, len, nc, k);
+      f.limit = limit;
+      f.ties = ties;
+      infos[bh] = f;
+    }
+  }
+}
+
+// Every group's pairs; the first group also writes their number and the new length
+// (no workgroup of this launch reads lens).
+__global__ __launch_bounds__(kEvictThreads) void evict_list_kernel(EvictArgs a, EvictInfo* infos, int32_t* pairs,
+                                                                   const uint32_t* keys, const GroupCount* counts,
+                                                                   int64_t max_chunks, int64_t max_moves, int groups) {
+  __shared__ SelectShared s;
+  __shared__ GroupCount before, total;
+  const int group = blockIdx.x / a.n_views, bh = blockIdx.x - group * a.n_views, t = threadIdx.x;
+  const int lane = t & 63, wave = t >> 6;
+  const EvictInfo f = infos[bh];
+  const int nc = f.nc, k = f.k, first = group * kGroupChunks;
+  if (f.shift == 0 || first >= nc) return;
+  const int n_groups = (nc + kGroupChunks - 1) / kGroupChunks;
+  const Run run{min(nc, first + wave * 256), min(nc, first + (wave + 1) * 256)};
+  const uint32_t* mine = keys + (size_t)bh * max_chunks;
+  uint32_t x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = mine[min(run.lo + i * 64 + lane, nc - 1)];
+  if (t == 0) before = total = GroupCount{};
+  __syncthreads();
+  for (int g = t; g < n_groups; g += kEvictThreads) {
+    const GroupCount c = counts[(size_t)bh * groups + g];
+    if (g < group) {
+      atomicAdd(&before.above_lo, c.above_lo);
+      atomicAdd(&before.equal_lo, c.equal_lo);
+      atomicAdd(&before.above_hi, c.above_hi);
+      atomicAdd(&before.equal_hi, c.equal_hi);
+    }
+    atomicAdd(&total.above_lo, c.above_lo);
+    atomicAdd(&total.equal_lo, c.equal_lo);
+  }
+  __syncthreads();
+  // equal keys stay in order: those below k first
+  const int holes = min(k, first) - before.above_lo - min(f.ties, before.equal_lo);
+  const int movers = before.above_hi + min(f.ties, total.equal_lo + before.equal_hi) - min(f.ties, total.equal_lo);
+  auto rows = [&](auto g) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) g(i, run.lo + i * 64);
+  };
+  auto key = [&](int i, int) { return x[i]; };
+  int tie = before.equal_lo + before.equal_hi;
+  if (f.ties > 0) tie += ties_before(s, run, rows, key, f.limit);
+  uint32_t bits = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bits |= (uint32_t)stays_at(x[i], run.lo + i * 64 + lane < run.hi, f.limit, f.ties, tie) << i;
+  list_pairs(s, run, k, covered_below(f, a.cs), pairs + (size_t)bh * max_moves * 2, rows, [] {},
+             [&](int i, int) { return (bits >> i & 1) != 0; }, holes, movers);
+  if (t == 0) {
+    if (s.lead) atomicAdd(&infos[bh].lead, s.lead);
+    if (group == 0) {
+      infos[bh].moves = k - total.above_lo - min(f.ties, total.equal_lo);
+      a.lens[bh] = (int64_t)f.len - f.shift;
+    }
+  }
+}
+
+// Keys of long views: workgroups over kKeyRows rows each; hist: the first digit's
+// histogram of every view (many chunks), or null.
+__global__ __launch_bounds__(kEvictThreads) void evict_keys_kernel(EvictArgs a, uint32_t* keys, uint32_t* hist,
+                                                                   int64_t max_chunks, int per_wg) {
+  __shared__ SelectShared s;
   const int group = blockIdx.x / a.n_views, bh = blockIdx.x - group * a.n_views;
   int64_t len;
   int nc, k;
@@ -376,8 +573,14 @@ __global__ __launch_bounds__(kEvictThreads) void evict_keys_kernel(EvictArgs a, 
   const int64_t c_lo = (int64_t)group * per_wg;
   if (c_lo >= nc) return;
   uint32_t* mine = keys + (size_t)bh * max_chunks;
-  chunk_keys(a.acc[bh], a.cs, (int)c_lo, (int)min((int64_t)nc, c_lo + per_wg), kEvictThreads,
-             [&](int c, uint32_t x) { mine[c] = x; });
+  s.hist[threadIdx.x] = 0;
+  s.hist[threadIdx.x + kEvictThreads] = 0;
+  __syncthreads();
+  chunk_keys(a.acc[bh], a.cs, (int)c_lo, (int)min((int64_t)nc, c_lo + per_wg), kEvictThreads, [&](int c, uint32_t x) {
+    mine[c] = x;
+    if (hist) atomicAdd(&s.hist[x >> 21], 1u);
+  });
+  if (hist) add_hist(s, hist + (size_t)bh * 3 * kBins);
 }
 
 // keys: null where this workgroup makes its own.
@@ -408,25 +611,16 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(EvictArgs a
   }
   __syncthreads();
   int32_t* out = pairs + (size_t)bh * max_moves * 2;
-  const int64_t from = (int64_t)nc * a.cs;
-  const int rest = (int)((a.q8 ? len / a.block * a.block : len) - from);
-  const int covered = k + (int)((len - from + a.cs - 1) / a.cs);
-  // up to 16384 keys in the lanes' registers, more read again for every pass
-  int moves;
+  EvictInfo f = evict_info(a, len, nc, k);
+  const int covered = covered_below(f, a.cs);
   auto load = [&](int c) { return mine[c]; };
-  if (nc <= kRankChunks) {
-    moves = rank_pairs(s, s_keys, nc, k, covered, out);
-  } else if (nc <= 2 * kEvictThreads) {
-    moves = register_pairs<2>(s, load, nc, k, covered, out);
-  } else if (nc <= 16 * kEvictThreads) {
-    moves = register_pairs<16>(s, load, nc, k, covered, out);
-  } else {
-    moves = memory_pairs(s, load, nc, k, covered, out);
-  }
+  f.moves = nc <= kRankChunks          ? rank_pairs(s, s_keys, nc, k, covered, out)
+            : nc <= 2 * kEvictThreads ? register_pairs<2>(s, load, nc, k, covered, out)
+                                      : register_pairs<16>(s, load, nc, k, covered, out);
   if (t == 0) {
-    const int shift = (nc - k) * a.cs;
-    infos[bh] = EvictInfo{moves, nc, k, (int32_t)len, shift, rest, s.lead};
-    a.lens[bh] = len - shift;
+    f.lead = s.lead;
+    infos[bh] = f;
+    a.lens[bh] = len - f.shift;
   }
 }
 
@@ -575,17 +769,34 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
   EvictInfo* infos = reinterpret_cast<EvictInfo*>(w);
   int32_t* pairs = reinterpret_cast<int32_t*>(w + info_bytes(a.n_views));
   uint32_t* keys = nullptr;
-  if (a.max_rows > kOwnKeyRows) {
-    keys = reinterpret_cast<uint32_t*>(w + info_bytes(a.n_views) + pairs_bytes(a.n_views, chunks));
+  const bool many = chunks > kOneChunks;
+  if (a.max_rows > kOwnKeyRows && chunks > 0) {
+    char* behind = w + info_bytes(a.n_views) + pairs_bytes(a.n_views, chunks);
+    keys = reinterpret_cast<uint32_t*>(behind);
+    uint32_t* hist = many ? reinterpret_cast<uint32_t*>(behind + key_bytes(a.n_views, chunks)) : nullptr;
+    if (many) {
+      const int64_t n = (int64_t)a.n_views * 3 * kBins;
+      hipLaunchKernelGGL(evict_clear_kernel, dim3((unsigned)(n / kEvictThreads < 1024 ? n / kEvictThreads : 1024)),
+                         dim3(kEvictThreads), 0, stream, hist, n);
+    }
     const int per_wg = kKeyRows / a.cs > 0 ? kKeyRows / a.cs : 1;
-    const int64_t groups = (chunks + per_wg - 1) / per_wg;
-    if (groups > 0)
-      hipLaunchKernelGGL(evict_keys_kernel, dim3((unsigned)(groups * a.n_views)), dim3(kEvictThreads), 0, stream, a, keys,
-                         chunks, per_wg);
+    hipLaunchKernelGGL(evict_keys_kernel, dim3((unsigned)((chunks + per_wg - 1) / per_wg * a.n_views)), dim3(kEvictThreads), 0,
+                       stream, a, keys, hist, chunks, per_wg);
+    if (many) {
+      GroupCount* counts = reinterpret_cast<GroupCount*>(behind + key_bytes(a.n_views, chunks) + hist_bytes(a.n_views));
+      const int groups = (int)groups_of(chunks);
+      const dim3 grid((unsigned)((int64_t)groups * a.n_views)), block(kEvictThreads);
+      hipLaunchKernelGGL(evict_digit_kernel<1>, grid, block, 0, stream, a, keys, hist, chunks);
+      hipLaunchKernelGGL(evict_digit_kernel<2>, grid, block, 0, stream, a, keys, hist, chunks);
+      hipLaunchKernelGGL(evict_count_kernel, grid, block, 0, stream, a, infos, keys, hist, counts, chunks, groups);
+      hipLaunchKernelGGL(evict_list_kernel, grid, block, 0, stream, a, infos, pairs, keys, counts, chunks, moves, groups);
+    }
   }
-  const int64_t in_lds = keys ? kRankChunks : chunks;
-  hipLaunchKernelGGL(evict_select_kernel, dim3(a.n_views), dim3(kEvictThreads), (size_t)(in_lds + 4) * sizeof(uint32_t),
-                     stream, a, infos, pairs, keys, chunks, moves);
+  if (!many) {
+    const int64_t in_lds = keys ? kRankChunks : chunks;
+    hipLaunchKernelGGL(evict_select_kernel, dim3(a.n_views), dim3(kEvictThreads), (size_t)(in_lds + 4) * sizeof(uint32_t),
+                       stream, a, infos, pairs, keys, chunks, moves);
+  }
   // A fill workgroup moves kTurn bytes per turn: as many as the most chunks that may
   // move keep busy, but about four rounds of the device at most.  A strip is as wide
   // as its workgroup moves in one turn, the rows behind the chunks being fewer than
