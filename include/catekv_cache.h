@@ -13,8 +13,9 @@
  * The conventions of catekv.h hold: caller-owned device pointers, checks before
  * any work is enqueued, caller-owned workspaces, d == 128, asynchronous work on
  * `stream`.  Every address below lies on a 16-byte border, except the scales,
- * the arrays of accumulated weights and the tables, which lie on a border of
- * their own type.  No two views share memory.
+ * the arrays of accumulated weights, lse and the tables, which lie on a border of
+ * their own type (q, out, k_new and v_new are checked: INVALID_ARG).  No two views
+ * that a call writes share memory, nor do two arrays of weights.
  *
  * An 8-bit view of L rows in blocks of `block` rows (32 or 64; K and V alike):
  *   rows [0, nb block), nb = L / block rounded down, as codes [row][d] with one
@@ -97,7 +98,8 @@ size_t catekv_weights_workspace(const catekv_decode_plan_t* plan);
  * out, lse  as in catekv_decode_attn
  * acc     [batch][hkv] device pointers to fp32 arrays of at least L values, in
  *         device memory, or NULL for no weights
- * decay   in [0, 1]; 1 sums all steps (ignored without acc)
+ * decay   in [0, 1]; 1 sums all steps, 0 leaves this step's weights alone
+ *         whatever acc held (ignored without acc)
  * ws      the plan's workspace
  * wws     catekv_weights_workspace() bytes (ignored without acc); calls that
  *         overlap in time must not share it

@@ -703,21 +703,51 @@ void attend_stream_kernel(AttendArgs a) {
   }
 }
 
+constexpr int kFewParts = 8;
+
 // ---- joining the partials, and the weights ----------------------------------------
-// Workgroups [0, n_views G): the partials of one view and head, when it has more
-// than one.  The workgroups behind them (with acc): worker w's rows, their
-// weights from the scores it kept and from all of the view's (m, l).
+// With acc, workgroup w < n_workers first: the weights of worker w's rows, from the
+// scores it kept (in the L2 of the same XCD) and from all of the view's (m, l); they
+// take longer than the rest.  Behind them, for every view and head: its partials,
+// when it has more than one.
 template <int G, bool ACC>
-__global__ __launch_bounds__(kAtThreads) void attend_join_kernel(AttendArgs a, int n_joins) {
+__global__ __launch_bounds__(kAtThreads) void attend_join_kernel(AttendArgs a) {
   constexpr int SF = G * kD + 2 * G;
   constexpr int NT = kAtThreads;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  if ((int)blockIdx.x < n_joins) {
+  if (!ACC || (int)blockIdx.x >= a.n_workers) {
     constexpr int LANES = NT / 32, BATCH = 16;    // parts side by side, parts per thread and round
-    const int bh = blockIdx.x / G, g = blockIdx.x - bh * G;
+    const int at = blockIdx.x - (ACC ? a.n_workers : 0), bh = at / G, g = at - bh * G;
     const ViewInfo vi = a.infos[bh];
     const int P = vi.n_parts;
     if (P <= 1) return;
+    if (P <= kFewParts) {
+      // few parts: the first head's workgroup joins all heads, one value per thread
+      if (g > 0) return;
+      const float* base = a.slots + (size_t)vi.first_slot * SF;
+      for (int i = t; i < G * kD; i += NT) {
+        const int gi = i / kD;
+        float ms[kFewParts], ls[kFewParts], os[kFewParts];
+        float M = kAtFloor, L = 0.f, O = 0.f;
+#pragma unroll
+        for (int p = 0; p < kFewParts; ++p) {
+          const float* sl = base + (size_t)min(p, P - 1) * SF;
+          ms[p] = p < P ? sl[G * kD + gi] : kAtFloor;
+          ls[p] = p < P ? sl[G * kD + G + gi] : 0.f;
+          os[p] = p < P ? sl[i] : 0.f;
+          M = fmaxf(M, ms[p]);
+        }
+#pragma unroll
+        for (int p = 0; p < kFewParts; ++p) {
+          const float w = fast_exp2(ms[p] - M);
+          L += w * ls[p];
+          O += w * os[p];
+        }
+        a.out[(size_t)bh * G * kD + i] = L == 0.f ? 0.f : O / L;
+        if (a.lse && i % kD == 0) a.lse[(size_t)bh * G + gi] = L == 0.f ? -INFINITY : kLn2 * M + logf(L * fast_exp2(-kShift));
+      }
+      return;
+    }
     __shared__ float s_red[NT / 64];
     __shared__ float4 s_acc[LANES][32];
     __shared__ float s_l[LANES];
@@ -782,7 +812,7 @@ __global__ __launch_bounds__(kAtThreads) void attend_join_kernel(AttendArgs a, i
   }
   if constexpr (ACC) {
     __shared__ float s_m[NT / 64][G], s_s[NT / 64][G];
-    const int w = blockIdx.x - n_joins;
+    const int w = blockIdx.x;
     const bool v2 = a.variant == kDecodeStreamV2;
     const V2Item* list = a.v2items + (size_t)w * kAtMaxSeg;
     const int seg_lo = v2 ? 0 : a.worker_seg[w];
@@ -861,13 +891,13 @@ __global__ __launch_bounds__(kAtThreads) void attend_join_kernel(AttendArgs a, i
         float wsum = 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) wsum += fast_exp2(x[u][g] - mg[g]) * ig[g];
-        if (i < n) acc[i] = __builtin_fmaf(a.decay, old[u], wsum);
+        if (i < n) acc[i] = a.decay > 0.f ? __builtin_fmaf(a.decay, old[u], wsum) : wsum;
       }
       for (int i = AHEAD * NT + t; i < n; i += NT) {
         float wsum = 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) wsum += fast_exp2(sc[(size_t)g * srows + i] - mg[g]) * ig[g];
-        acc[i] = __builtin_fmaf(a.decay, acc[i], wsum);
+        acc[i] = a.decay > 0.f ? __builtin_fmaf(a.decay, acc[i], wsum) : wsum;
       }
     }
   }
@@ -897,7 +927,7 @@ static hipError_t launch_attend_t(const AttendArgs& a, hipStream_t stream) {
   const int n_joins = a.n_multi > 0 ? a.n_views * G : 0;
   const int blocks = n_joins + (ACC ? a.n_workers : 0);
   if (blocks > 0)
-    hipLaunchKernelGGL((attend_join_kernel<G, ACC>), dim3(blocks), dim3(kAtThreads), 0, stream, a, n_joins);
+    hipLaunchKernelGGL((attend_join_kernel<G, ACC>), dim3(blocks), dim3(kAtThreads), 0, stream, a);
   return hipGetLastError();
 }
 

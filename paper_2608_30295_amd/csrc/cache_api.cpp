@@ -3,6 +3,7 @@
 
 #include <cmath>
 #include <cstdarg>
+#include <cstdint>
 #include <cstdio>
 
 #include "cache.h"
@@ -41,6 +42,12 @@ int check_rows(int n_views, int64_t max_rows, int d) {
   return CATEKV_OK;
 }
 
+// Addresses that the kernels read or write 16 bytes at a time.
+int check_aligned(const void* p, const char* name) {
+  if (reinterpret_cast<uintptr_t>(p) % 16) return fail(CATEKV_ERR_INVALID_ARG, "%s is not on a 16-byte border", name);
+  return CATEKV_OK;
+}
+
 // The checks of both conversions, and their launch sizes.
 int check_convert(int format, int dtype, int block, const void* kv, const void* lens, const void* views, int n_views,
                   int64_t max_rows, int d) {
@@ -59,7 +66,9 @@ int attend_args(const catekv_decode_plan_t* plan, const void* q, const void* vie
                 size_t ws_bytes, void* wws, size_t wws_bytes, AttendArgs& a) {
   if (!host_plan_valid(plan)) return fail(CATEKV_ERR_INVALID_ARG, "plan missing or not built by catekv_decode_plan");
   if (!q || !views || !lens || !out) return fail(CATEKV_ERR_INVALID_ARG, "null tensor pointer");
-  int rc = host_check_heads(hq, hkv, d);
+  int rc = check_aligned(q, "q");
+  if (!rc) rc = check_aligned(out, "out");
+  if (!rc) rc = host_check_heads(hq, hkv, d);
   if (rc) return rc;
   if (plan->batch != batch || plan->hq != hq || plan->hkv != hkv)
     return fail(CATEKV_ERR_INVALID_ARG, "shapes (batch=%d hq=%d hkv=%d) differ from the plan (%d, %d, %d)", batch, hq,
@@ -167,6 +176,9 @@ int catekv_q8_append(int format, int dtype, int block, const catekv_q8_view* vie
   if (batch < 1 || hkv < 1) return fail(CATEKV_ERR_INVALID_ARG, "batch=%d hkv=%d must be >= 1", batch, hkv);
   if (d != kD) return fail(CATEKV_ERR_UNSUPPORTED, "head dimension %d unsupported (only %d)", d, kD);
   if ((int64_t)batch * hkv > (int64_t)INT32_MAX) return fail(CATEKV_ERR_INVALID_ARG, "batch * hkv too large");
+  rc = check_aligned(k_new, "k_new");
+  if (!rc) rc = check_aligned(v_new, "v_new");
+  if (rc) return rc;
   Q8Args a{};
   a.block = block;
   a.views = views;

@@ -67,7 +67,7 @@ def test_conversions_refuse(change, status):
     (dict(format=7), UNSUPPORTED), (dict(dtype=7), UNSUPPORTED), (dict(block=8), INVALID),
     (dict(views=None), INVALID), (dict(capacity=None), INVALID), (dict(lens=None), INVALID), (dict(k=None), INVALID),
     (dict(v=None), INVALID), (dict(batch=0), INVALID), (dict(hkv=0), INVALID), (dict(d=256), UNSUPPORTED),
-    (dict(batch=1 << 20, hkv=1 << 20), INVALID),
+    (dict(batch=1 << 20, hkv=1 << 20), INVALID), (dict(k=FAKE + 8), INVALID), (dict(v=FAKE + 2), INVALID),
 ])
 def test_append_refuses(change, status):
     a = dict(format=1, dtype=0, block=32, views=FAKE, capacity=FAKE, lens=FAKE, k=FAKE, v=FAKE, batch=1, hkv=2, d=128)
@@ -85,7 +85,7 @@ def test_append_refuses(change, status):
     (dict(scale=float("inf")), INVALID), (dict(decay=-0.1), INVALID), (dict(decay=1.5), INVALID),
     (dict(decay=float("nan")), INVALID), (dict(ws=None), WORKSPACE), (dict(ws=FAKE + 8), WORKSPACE),
     (dict(ws_bytes=100), WORKSPACE), (dict(wws=None), WORKSPACE), (dict(wws=FAKE + 64), WORKSPACE),
-    (dict(wws_bytes=64), WORKSPACE),
+    (dict(wws_bytes=64), WORKSPACE), (dict(q=FAKE + 8), INVALID), (dict(out=FAKE + 4), INVALID),
 ])
 def test_attention_refuses(change, status):
     a = dict(dtype=1, plan=plan_of(), q=FAKE, views=FAKE, lens=FAKE, batch=1, hq=8, hkv=2, d=128, scale=0.1, out=FAKE,

@@ -317,6 +317,49 @@ def test_lengths_beyond_the_plan_are_cut(fmt):
     check_attention(q, cut, planned, 2, out, lse, a, a0, 1.0)
 
 
+@pytest.mark.parametrize("kind,group", [("int8", 4), ("e4m3", 8), ("bf16", 1), ("bf16", 4), ("bf16", 8), ("f32", 2),
+                                        ("f32", 8)])
+@pytest.mark.parametrize("split", [0, 640])
+def test_long_shares_with_weights(kind, group, split):
+    # shares of more than 1200 rows, whose scores are kept until the share's end where
+    # they fit, and shares of a given length
+    rng = np.random.default_rng(27)
+    dtype = kind if kind in DT else "bf16"
+    lens = [330_001, 70]
+    q = torch.randn((1, 2 * group, D), generator=torch.Generator().manual_seed(4)).to(DT[dtype]).to(DEV)
+    plan = ck.decode_plan(lens, 2 * group, 2, DEV, split_tokens=split)
+    a, a0, table = accs(rng, lens)
+    d = Dense(rng, lens, dtype)
+    if kind in DT:
+        out, lse = ck.decode_attn_weights(plan, q, d.table, d.lens, table)
+        host = d.host
+    else:
+        q8 = Eight([n + 64 for n in lens], kind, 64, dtype)
+        ck.quantize_kv(d.table, d.lens, q8.views, max(lens))
+        out, lse = ck.decode_attn_q8(plan, q, q8.views, d.lens, acc=table)
+        host = lambda i: q8.host(i, lens[i])
+    check_attention(q, host, lens, 2, out, lse, a, a0, 1.0)
+
+
+@pytest.mark.parametrize("kind", ["int8", "bf16"])
+def test_decay_zero_leaves_this_step_s_weights(kind):
+    rng = np.random.default_rng(28)
+    lens = [300, 3000, 0, 17]
+    d = Dense(rng, lens, "bf16")
+    q = torch.randn((2, 8, D), generator=torch.Generator().manual_seed(6)).bfloat16().to(DEV)
+    plan = ck.decode_plan(lens, 8, 2, DEV)
+    a = [torch.full((n + 3,), math.nan, device=DEV) for n in lens]
+    table = ck.acc_table([x.data_ptr() for x in a], DEV)
+    if kind == "bf16":
+        ck.decode_attn_weights(plan, q, d.table, d.lens, table, decay=0.0)
+    else:
+        q8 = Eight([n + 64 for n in lens], kind, 64, "bf16")
+        ck.quantize_kv(d.table, d.lens, q8.views, max(lens))
+        ck.decode_attn_q8(plan, q, q8.views, d.lens, acc=table, decay=0.0)
+    for x, n in zip(a, lens):
+        assert torch.isnan(x[n:]).all() and (n == 0 or abs(float(x[:n].double().sum()) - 1) < 1e-5)
+
+
 @pytest.mark.parametrize("kind", ["int8", "e4m3", "bf16", "f32"])
 def test_many_tiny_views(kind):
     # more segments per workgroup than its table holds at a time
