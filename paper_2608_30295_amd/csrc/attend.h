@@ -6,8 +6,14 @@
 //   x_t = c q . K_t,  c = scale log2(e);  m the running maximum of x, raised only
 //   when it would grow by more than kSlack;  P_t = 2^(x_t - m + kShift);
 //   l = sum P,  O = sum P V;  out = O / l,  lse = ln 2 (m + log2 l - kShift).
-// kShift lifts P so that its split into 16-bit floats keeps 22 bits down to
-// P = 2^-25 of the largest, and 2^(kShift + kSlack) still fits an fp16.
+// kShift lifts P so that two fp16 numbers hold it to 2^-22 of itself or 2^-36 of the
+// largest P, whichever is more, and 2^(kShift + kSlack) still fits an fp16.
+//
+// Bound by HBM: 4 FLOP per byte of bf16, 8 per byte of codes.  128K rows (3 full
+// views, 5 of 2112 rows) in e4m3: 103 MB in 24.2 us, 6 TB/s from the first tile's
+// request (2.6 us: three dependent loads, the query rows) to the end of the average
+// share, 3 us more to that of the slowest XCD; 1M rows (2 views) in int8: 544 MB in
+// 99 us (5.5 TB/s).  The join takes 4 us more, with weights 9.
 //
 // Work: the plan's shares (equal numbers of rows), one workgroup of 8 waves
 // each, tile u of a segment to wave u % 8, two tiles per wave in flight across
@@ -25,7 +31,6 @@ namespace catekv {
 constexpr int kAtWaves = 8;
 constexpr int kAtThreads = kAtWaves * 64;
 constexpr int kAtMaxSeg = kDecodeV2MaxSeg;   // segments described in LDS at a time
-constexpr int kRows8 = 32;                   // rows of an 8-bit tile
 constexpr float kShift = 11.f;
 constexpr float kSlack = 4.f;
 constexpr float kAtFloor = -1e30f;           // maximum of no row: 2^(floor - m) = 0, and no inf - inf
@@ -37,10 +42,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ uint2 ldg8(const void* p) {
   const u32x2 v = *(const __attribute__((address_space(1))) u32x2*)(p);
@@ -180,10 +183,13 @@ struct Rows16 {
 // two to a maximum in [2^14, 2^15), so that a bf16 element is an fp16 exactly
 // down to 2^-31 of the largest (below, off by at most 2^-39 of it); an fp32 row is
 // split into two fp16 rows (22 bits).  The block's K scale multiplies the scores
-// in fp32, its V scale the tile's P V sums.
-template <int FMT, typename QT, int ROWS>
+// in fp32, its V scale the tile's P V sums.  Converting costs 1.25 (int8) or 0.5
+// instructions per code of K and about twice that with the transpose of V: by
+// count a third of the issue slots while HBM delivers 6 TB/s.  Tiles of 16 rows: 27.2
+// against 26.8 us at 128K, 135.5 against 132.0 at 16 x 16K-64K (e4m3).
+template <int FMT, typename QT>
 struct Kind8 {
-  static constexpr int TOK = ROWS, H = ROWS / 16;
+  static constexpr int TOK = 32;
   static constexpr bool kTail = true;
   typedef catekv_q8_view View;
   typedef QT T;
@@ -193,8 +199,8 @@ struct Kind8 {
     float unscale;
   };
   struct Tile {
-    uint4 k[H][2];
-    uint2 v[4 * H];
+    uint4 k[2][2];
+    uint2 v[8];
     float ks, vs;
   };
   __device__ static __forceinline__ void load_q(Q& q, const uint4* row, bool head, int k4) {
@@ -235,18 +241,18 @@ struct Kind8 {
     const char* vp = uniform(sg.v) + (size_t)t * kD;
     const uint32_t ko = n16 * kD + k4 * 16, vo = 4 * k4 * kD + n16 * 8;
 #pragma unroll
-    for (int h = 0; h < H; ++h)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int j = 0; j < 2; ++j) b.k[h][j] = ldg16(kp + ko + h * 16 * kD + j * 64);
 #pragma unroll
-    for (int r = 0; r < 4 * H; ++r) b.v[r] = ldg8(vp + vo + ((r >> 2) * 16 + (r & 3)) * kD);
+    for (int r = 0; r < 8; ++r) b.v[r] = ldg8(vp + vo + ((r >> 2) * 16 + (r & 3)) * kD);
     b.ks = ldg4f(uniform(sg.ks) + t / block);
     b.vs = ldg4f(uniform(sg.vs) + t / block);
   }
   __device__ static __forceinline__ float factor(const Tile& b, const Q& q, float c) { return b.ks * (c * q.unscale); }
-  __device__ static __forceinline__ void scores(const Tile& b, const Q& q, f32x4 (&S)[H]) {
+  __device__ static __forceinline__ void scores(const Tile& b, const Q& q, f32x4 (&S)[2]) {
 #pragma unroll
-    for (int h = 0; h < H; ++h) {
+    for (int h = 0; h < 2; ++h) {
       f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
@@ -258,36 +264,34 @@ struct Kind8 {
       S[h] = s;
     }
   }
-  // P = hi + lo in fp16, 22 bits
-  __device__ static __forceinline__ void pv(const Tile& b, const float (&P)[4 * H], f32x4 (&O)[8]) {
-    uint32_t hi[2 * H], lo[2 * H];
+  // P = hi + lo in fp16, 22 bits.  Lane (n16, k4) holds P of the rows 4 k4 + r of both
+  // halves, eight of the 32 that a product sums over, and the codes of the same
+  // rows: dims 8 n16 .. + 8, one product each.
+  __device__ static __forceinline__ void pv(const Tile& b, const float (&P)[8], f32x4 (&O)[8]) {
+    uint32_t hi[4], lo[4];
 #pragma unroll
-    for (int i = 0; i < 2 * H; ++i) {
+    for (int i = 0; i < 4; ++i) {
       hi[i] = pack_f16(P[2 * i], P[2 * i + 1]);
       const f32x2 h = unpack_f16(hi[i]);
       lo[i] = pack_f16(P[2 * i] - h.x, P[2 * i + 1] - h.y);
     }
+    const f16x8 A_hi = __builtin_bit_cast(f16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+    const f16x8 A_lo = __builtin_bit_cast(f16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
 #pragma unroll
     for (int half = 0; half < 2; ++half) {      // dims 8 n16 + 4 half + e
-      uint32_t w[H][4];
+      uint32_t w[2][4];
 #pragma unroll
-      for (int h = 0; h < H; ++h) {
+      for (int h = 0; h < 2; ++h) {
         const uint2* v = b.v + 4 * h;
         if (half) transpose4(v[0].y, v[1].y, v[2].y, v[3].y, w[h]);
         else transpose4(v[0].x, v[1].x, v[2].x, v[3].x, w[h]);
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
+        const f16x8 B = codes8_to_f16<FMT>(w[0][e], w[1][e]);
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
-        if constexpr (H == 2) {
-          const f16x8 B = codes8_to_f16<FMT>(w[0][e], w[H - 1][e]);
-          o = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, make_uint4(hi[0], hi[1], hi[2 * H - 2], hi[2 * H - 1])), B, o, 0, 0, 0);
-          o = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, make_uint4(lo[0], lo[1], lo[2 * H - 2], lo[2 * H - 1])), B, o, 0, 0, 0);
-        } else {
-          const f16x4 B = __builtin_bit_cast(f16x4, codes_to_f16<FMT>(w[0][e]));
-          o = __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4, make_uint2(hi[0], hi[1])), B, o, 0, 0, 0);
-          o = __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4, make_uint2(lo[0], lo[1])), B, o, 0, 0, 0);
-        }
+        o = __builtin_amdgcn_mfma_f32_16x16x32_f16(A_hi, B, o, 0, 0, 0);
+        o = __builtin_amdgcn_mfma_f32_16x16x32_f16(A_lo, B, o, 0, 0, 0);
 #pragma unroll
         for (int r = 0; r < 4; ++r) O[4 * half + e][r] = __builtin_fmaf(b.vs, o[r], O[4 * half + e][r]);
       }

@@ -16,6 +16,10 @@
 // the list, as sources ascend) belong to the workgroups that shift, one per strip
 // of the rows of K and of V, which read a turn's rows before they write any of
 // them.  No order between workgroups is needed.
+//
+// Bound by latency where little moves (16 x 8 views of 2304 rows: 8.9 us select, of
+// it 5 in dependent loads and barriers, 10.4 move) and by HBM where much does (8
+// views of 131072 rows to 16384: 117 MB moved in 29 us, 4.0 TB/s in 2 KB chunks).
 #include "cache.h"
 #include "common.h"
 

@@ -4,7 +4,10 @@
 // All three move bytes and little else (quantize: 2 row bytes read and one
 // written per element pair), so a wave takes one block of K or of V whole: the
 // rows go through its registers once, the maximum is taken of the bit patterns
-// on the way, and both sides are read and written in whole lines.
+// on the way, and both sides are read and written in whole lines (lanes with 32
+// consecutive bytes of fp32, half a line per access: 4099 fp32 rows of 8 heads back
+// from int8 15.2 -> 8.4 us).  131072 bf16 rows of 8 heads: 805 MB in 166 us into
+// e4m3, in 137 us back (4.8 and 5.9 TB/s; a copy runs at 5.15).
 #include "cache.h"
 #include "common.h"
 
