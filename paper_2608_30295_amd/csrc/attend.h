@@ -841,7 +841,7 @@ __global__ __launch_bounds__(kAtThreads) void attend_join_kernel(AttendArgs a) {
       soff += srows;
       const int64_t len = a.lens[bh];
       const ViewInfo vi = a.infos[bh];
-      float* acc = a.acc[bh] + t0;
+      auto acc = (__attribute__((address_space(1))) float*)(a.acc[bh] + t0);
       const int n = (int)(len < (int64_t)t1 ? len : (int64_t)t1) - t0;
       if (n <= 0) continue;
       // the first rows' scores and weights, requested beside the parts

@@ -78,6 +78,13 @@ bool evict_fits(int n_views, int64_t max_rows, int cs) {
   return max_rows <= kMaxEvictRows && cs <= kMaxEvictChunk && n_views <= kMaxEvictViews;
 }
 
+// Pointers that come out of tables are global ones: without the cast their accesses
+// are flat, which wait for LDS as well.
+template <typename E>
+using Global = __attribute__((address_space(1))) E*;
+template <typename E>
+__device__ __forceinline__ Global<E> global(E* p) { return (Global<E>)p; }
+
 // Larger key = larger weight; NaN above all, -0 as 0.
 __device__ __forceinline__ uint32_t weight_key(float x) {
   uint32_t b = __float_as_uint(x);
@@ -121,7 +128,7 @@ __device__ __forceinline__ void chunk_keys(const float* acc, int cs, int c_lo, i
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const int c = min(c0 + u * per, c_hi - 1);
-        w[u] = acc[(size_t)c * cs + i];
+        w[u] = global(acc)[(size_t)c * cs + i];
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) x[u] = max(x[u], weight_key(w[u]));
@@ -636,8 +643,9 @@ constexpr int kMoveBatch = 8;           // loads of a thread in flight
 // no later turn reads: fills lie below all sources, shifted elements below the
 // sources of the shifts still to come, and zeros come last.
 template <typename E, typename Src, typename Dst, typename From, typename To>
-__device__ __forceinline__ void move_elements(E* p, int n_fill, Src src, Dst dst, int n_shift, From from, To to, int n_zero,
+__device__ __forceinline__ void move_elements(E* generic, int n_fill, Src src, Dst dst, int n_shift, From from, To to, int n_zero,
                                               size_t end) {
+  const Global<E> p = global(generic);
   const int n = n_fill + n_shift + n_zero;
   for (int i0 = 0; i0 < n; i0 += kMoveThreads * kMoveBatch) {
     E w[kMoveBatch];
@@ -693,7 +701,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, c
   if (!shifting) y -= 2 * strips;
   if (!shifting && y >= 2 * fills) {
     y -= 2 * fills;
-    float* p = a.acc[bh];
+    const Global<float> p = global(a.acc[bh]);
     const int n = (f.moves - f.lead) * cs, step = kMoveThreads * kMoveBatch;
     for (int i0 = y * step; i0 < n; i0 += acc_fills * step) {
       int2 c[kMoveBatch];
@@ -752,7 +760,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, c
     for (int u = 0; u < kMoveBatch; ++u) w[u] = ldg16(base + (size_t)c[u].y * chunk_bytes + off[u]);
 #pragma unroll
     for (int u = 0; u < kMoveBatch; ++u)
-      if (mine[u]) *reinterpret_cast<uint4*>(base + (size_t)c[u].x * chunk_bytes + off[u]) = w[u];
+      if (mine[u]) *global(reinterpret_cast<u32x4_t*>(base + (size_t)c[u].x * chunk_bytes + off[u])) = u32x4_t{w[u].x, w[u].y, w[u].z, w[u].w};
   }
 }
 
@@ -761,7 +769,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_zero_kernel(EvictArgs a, c
   const int group = blockIdx.x / a.n_views, bh = blockIdx.x - group * a.n_views;
   const EvictInfo f = infos[bh];
   if (f.shift == 0) return;
-  float* acc = a.acc[bh];
+  const Global<float> acc = global(a.acc[bh]);
   const int64_t lo = (int64_t)(f.len - f.shift) + (int64_t)group * kKeyRows, hi = min((int64_t)f.len, lo + kKeyRows);
 #pragma unroll 4
   for (int64_t i = lo + threadIdx.x; i < hi; i += kMoveThreads) acc[i] = 0.f;

@@ -566,7 +566,7 @@ def test_evict_many_views(kind, n, cs, max_rows):
                 assert same(q8.hold[6 * i + 4 + j], old[6 * i + 4 + j]), i
 
 
-@pytest.mark.parametrize("n,cs,budget", [(70001, 1, 20000), (70001, 1, 60000), (40000, 1, 32768), (300000, 8, 5000)])
+@pytest.mark.parametrize("n,cs,budget", [(16384, 1, 5000), (16385, 1, 5000), (16500, 1, 16400), (70001, 1, 20000), (70001, 1, 60000), (40000, 1, 32768), (300000, 8, 5000)])
 def test_evict_long_views(n, cs, budget):
     # more chunks than a workgroup keeps in LDS, beside a short view and one that stays
     rng = np.random.default_rng(33)
