@@ -275,6 +275,7 @@ __device__ __forceinline__ int rank_pairs(SelectShared& s, const uint32_t* keys,
       }
     };
     count(j0, min(j1, own), x - 1);
+#pragma unroll 4
     for (int j = max(j0, own); j < min(j1, own + 64); j += 4) {
       const uint4 w = *reinterpret_cast<const uint4*>(keys + j);
       rank += w.x > (j < c ? x - 1 : x);
@@ -815,7 +816,7 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
   // recent + cs and those filled first hardly more.
   constexpr int64_t kTurn = kMoveThreads * kMoveBatch * 16;
   const int64_t turns = (moves * a.cs * a.row_bytes + kTurn - 1) / kTurn;
-  const int64_t room = 2048 / a.n_views > 2 ? 2048 / a.n_views : 2;
+  const int64_t room = 512 / a.n_views > 4 ? 512 / a.n_views : 4;
   const int fills = (int)(turns < room ? turns : room);
   int strip_log = 2;
   while ((16 << strip_log) < a.row_bytes && 2 * ((int64_t)a.recent + a.cs) * (32 << strip_log) <= kTurn) ++strip_log;
