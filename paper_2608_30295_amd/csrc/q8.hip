@@ -6,8 +6,8 @@
 // rows go through its registers once, the maximum is taken of the bit patterns
 // on the way, and both sides are read and written in whole lines (lanes with 32
 // consecutive bytes of fp32, half a line per access: 4099 fp32 rows of 8 heads back
-// from int8 15.2 -> 8.4 us).  131072 bf16 rows of 8 heads: 805 MB in 166 us into
-// e4m3, in 137 us back (4.8 and 5.9 TB/s; a copy runs at 5.15).
+// from int8 15.2 -> 8.4 us).  131072 bf16 rows of 8 heads: 805 MB in 149 us into
+// e4m3, in 147 us back (5.4 and 5.5 TB/s; a copy runs at 5.15).
 #include "cache.h"
 #include "common.h"
 
@@ -15,6 +15,15 @@ namespace catekv {
 
 constexpr float kTinyMax = 7.888609052210118e-31f;   // 2^-100
 constexpr int kQ8Waves = 4;
+
+// 16 bytes that are read once: the rows on their way into codes.  They and the rows
+// written on the way back pass the caches by, which leaves these to the codes (8
+// heads of 131072 bf16 rows into e4m3 and back 306 -> 258 us, of 32768 87 -> 71; one
+// way alone 45 -> 39 and 47 -> 33 at 32768, 150 -> 149 and 155 -> 147 at 131072).
+__device__ __forceinline__ uint4 once16(const void* p) {
+  const u32x4_t v = __builtin_nontemporal_load((const __attribute__((address_space(1))) u32x4_t*)p);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
 
 // 16 bytes of a row: kN elements.
 template <typename T>
@@ -131,7 +140,7 @@ struct BlockRows {
   __device__ __forceinline__ void load(Row row, int first) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i].w = ldg16(row(first + lane / kPer + kStep * i) + (lane % kPer) * 16);
+    for (int i = 0; i < N; ++i) x[i].w = once16(row(first + lane / kPer + kStep * i) + (lane % kPer) * 16);
   }
   // largest |x| of the wave's rows, as bits
   __device__ __forceinline__ uint32_t largest() const {
@@ -228,7 +237,7 @@ __global__ __launch_bounds__(kQ8Waves * 64) void q8_dequantize_kernel(Q8Args a) 
       }
       Piece<T> o;
       o.set(f);
-      *reinterpret_cast<uint4*>(dst + (size_t)(i * 64 + lane) * 16) = o.w;
+      __builtin_nontemporal_store(u32x4_t{o.w.x, o.w.y, o.w.z, o.w.w}, reinterpret_cast<u32x4_t*>(dst + (size_t)(i * 64 + lane) * 16));
     }
     return;
   }
