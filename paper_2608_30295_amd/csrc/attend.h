@@ -45,8 +45,19 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
-__device__ __forceinline__ uint2 ldg8(const void* p) {
-  const u32x2 v = *(const __attribute__((address_space(1))) u32x2*)(p);
+// Rows of K and V, read once per step: their loads pass the caches by.  us per step,
+// cached / past the caches: int8 1M 100.4 / 95.4, e4m3 16 x 16K-64K with the append
+// 125.4 / 119.6, bf16 128K with weights 48.4 / 44.3; over the caches of 24 layers
+// in turn e4m3 128K 28.6 / 27.8, int8 16 x 2304 with append and weights 39.4 / 37.6.
+// Where the Infinity Cache would have kept rows from one step to the next it is
+// the other way round: the same two over 3 layers 26.2 / 27.1 and 36.0 / 36.7.
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 once16(const void* p) {
+  const u32x4 v = __builtin_nontemporal_load((const __attribute__((address_space(1))) u32x4*)(p));
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ uint2 once8(const void* p) {
+  const u32x2 v = __builtin_nontemporal_load((const __attribute__((address_space(1))) u32x2*)(p));
   return make_uint2(v.x, v.y);
 }
 __device__ __forceinline__ float ldg4f(const float* p) {
@@ -131,8 +142,10 @@ __device__ __forceinline__ float elem(const uint4& w, int i) {
 }
 
 // 16 rows on the fp32 matrix instruction: S^T (16 rows x 16 heads) += K Q^T, with
-// lane (n16, k4) holding dims [32 k4, 32 k4 + 32) of row n16 and of head n16; and
-// O += P V with the four rows 4 k4 + r of V.  Serves fp32 views and the tails
+// lane (n16, k4) holding the 16-byte pieces 4 i + k4 of row n16 and of head n16 (a
+// load covers 64 bytes of a row; the loads of a line find it in cache, so none passes
+// it by: 113 against 72 us for fp32 100K rows); and O += P V with the four rows
+// 4 k4 + r of V.  Serves fp32 views and the tails
 // of 8-bit views (exact products, fp32 sums).
 template <typename T>
 struct Rows16 {
@@ -141,9 +154,9 @@ struct Rows16 {
   uint4 v[4][NV];
   // rows kp, vp .. + last (uniform), a row behind them is the last one again
   __device__ __forceinline__ void load(const char* kp, const char* vp, int last, int n16, int k4) {
-    const uint32_t ko = (uint32_t)(min(n16, last) * kD + k4 * 32) * sizeof(T);
+    const uint32_t ko = (uint32_t)(min(n16, last) * kD) * sizeof(T) + k4 * 16;
 #pragma unroll
-    for (int i = 0; i < NK; ++i) k[i] = ldg16(kp + ko + 16 * i);
+    for (int i = 0; i < NK; ++i) k[i] = ldg16(kp + ko + 64 * i);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const uint32_t vo = (uint32_t)(min(4 * k4 + r, last) * kD + n16 * 8) * sizeof(T);
@@ -151,7 +164,7 @@ struct Rows16 {
       for (int i = 0; i < NV; ++i) v[r][i] = ldg16(vp + vo + 16 * i);
     }
   }
-  // q(i): 16 bytes of the head's 32 dims of this lane, in the storage type
+  // q(i): the 16 bytes 4 i + k4 of the head's query, in the storage type
   template <typename F>
   __device__ __forceinline__ f32x4 scores(F q) const {
     f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
@@ -243,9 +256,9 @@ struct Kind8 {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) b.k[h][j] = ldg16(kp + ko + h * 16 * kD + j * 64);
+      for (int j = 0; j < 2; ++j) b.k[h][j] = once16(kp + ko + h * 16 * kD + j * 64);
 #pragma unroll
-    for (int r = 0; r < 8; ++r) b.v[r] = ldg8(vp + vo + ((r >> 2) * 16 + (r & 3)) * kD);
+    for (int r = 0; r < 8; ++r) b.v[r] = once8(vp + vo + ((r >> 2) * 16 + (r & 3)) * kD);
     b.ks = ldg4f(uniform(sg.ks) + t / block);
     b.vs = ldg4f(uniform(sg.vs) + t / block);
   }
@@ -324,9 +337,9 @@ struct KindBf16 {
     const char* vp = uniform(sg.v) + (size_t)t * (kD * 2);
     const uint32_t ko = min(n16, last) * (kD * 2) + k4 * 16;
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) b.k[ks] = ldg16(kp + ko + ks * 64);
+    for (int ks = 0; ks < 4; ++ks) b.k[ks] = once16(kp + ko + ks * 64);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) b.v[r] = ldg16(vp + (uint32_t)(min(4 * k4 + r, last) * (kD * 2) + n16 * 16));
+    for (int r = 0; r < 4; ++r) b.v[r] = once16(vp + (uint32_t)(min(4 * k4 + r, last) * (kD * 2) + n16 * 16));
   }
   __device__ static __forceinline__ float factor(const Tile&, const Q&, float c) { return c; }
   __device__ static __forceinline__ void scores(const Tile& b, const Q& q, f32x4 (&S)[1]) {
@@ -378,7 +391,7 @@ struct KindF32 {
   };
   typedef Rows16<float> Tile;
   __device__ static __forceinline__ void load_q(Q& q, const uint4* row, bool head, int k4) {
-    q.row = row + 8 * k4;
+    q.row = row + k4;
     q.head = head;
   }
   __device__ static __forceinline__ void load(Tile& b, const AtSeg& sg, int t, int, int n16, int k4) {
@@ -387,7 +400,7 @@ struct KindF32 {
   }
   __device__ static __forceinline__ float factor(const Tile&, const Q&, float c) { return c; }
   __device__ static __forceinline__ void scores(const Tile& b, const Q& q, f32x4 (&S)[1]) {
-    S[0] = b.scores([&](int i) { return q.head ? q.row[i] : make_uint4(0, 0, 0, 0); });
+    S[0] = b.scores([&](int i) { return q.head ? q.row[4 * i] : make_uint4(0, 0, 0, 0); });
   }
   __device__ static __forceinline__ void pv(const Tile& b, const float (&P)[4], f32x4 (&O)[8]) { b.pv(P, O); }
 };
@@ -584,7 +597,7 @@ void attend_stream_kernel(AttendArgs a) {
           const size_t at = (size_t)uniform(sg.tail0 + 16 * i) * (kD * sizeof(T));
           rows.load(uniform(sg.kt) + at, uniform(sg.vt) + at, uniform(sg.tail_n) - 16 * i - 1, n16, k4);
           const f32x4 S[1] = {rows.scores([&](int j) {
-            const uint4 w = s_q[s][head_lane ? n16 : 0][k4 * Rows16<T>::NK + j];
+            const uint4 w = s_q[s][head_lane ? n16 : 0][4 * j + k4];
             return head_lane ? w : make_uint4(0, 0, 0, 0);
           })};
           float P[4];
