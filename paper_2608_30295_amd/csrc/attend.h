@@ -10,10 +10,11 @@
 // largest P, whichever is more, and 2^(kShift + kSlack) still fits an fp16.
 //
 // Bound by HBM: 4 FLOP per byte of bf16, 8 per byte of codes.  128K rows (3 full
-// views, 5 of 2112 rows) in e4m3: 103 MB in 24.2 us, 6 TB/s from the first tile's
+// views, 5 of 2112 rows) in e4m3: 103 MB in 24 us, 6 TB/s from the first tile's
 // request (2.6 us: three dependent loads, the query rows) to the end of the average
-// share, 3 us more to that of the slowest XCD; 1M rows (2 views) in int8: 544 MB in
-// 99 us (5.5 TB/s).  The join takes 4 us more, with weights 9.
+// share, 3 us more to that of the slowest XCD; the same in bf16 with weights: 206 MB
+// in 36 us; 1M rows (2 views) in int8: 544 MB in 97 us (5.6 TB/s).  The join takes
+// 4 to 5 us more, with weights 7.
 //
 // Work: the plan's shares (equal numbers of rows), one workgroup of 8 waves
 // each, tile u of a segment to wave u % 8, two tiles per wave in flight across
@@ -932,7 +933,7 @@ template <class K, int G, bool ACC>
 static hipError_t launch_attend_t(const AttendArgs& a, hipStream_t stream) {
   // The scores of a share of more than kStagedRows rows stay in LDS until its end, where
   // they fit beside the rest (4 heads: 6000 rows): stored tile by tile among the
-  // loads they cost 5.8 us of a 128K bf16 step of 45, at the end 2.5.  us per step,
+  // loads they cost 5.8 us of a 128K bf16 step of 53, at the end 2.5.  us per step,
   // tile by tile / staged, by rows of a share: bf16 620: 24.0 / 24.0, 1200: 43.1 /
   // 41.0, 2050: 68.1 / 63.0; int8 830: 24.2 / 24.6, 1600: 35.4 / 34.2, 4700: 87.6 / 81.5.
   const size_t lds = ACC && a.variant == kDecodeStreamV2 && a.score_rows > kStagedRows

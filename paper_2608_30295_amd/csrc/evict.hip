@@ -17,9 +17,10 @@
 // of the rows of K and of V, which read a turn's rows before they write any of
 // them.  No order between workgroups is needed.
 //
-// Bound by latency where little moves (16 x 8 views of 2304 rows: 8.9 us select, of
-// it 5 in dependent loads and barriers, 10.4 move) and by HBM where much does (8
-// views of 131072 rows to 16384: 117 MB moved in 29 us, 4.0 TB/s in 2 KB chunks).
+// Bound by latency where little moves (16 x 8 views of 2304 rows: 9 us select, of
+// it 5 in dependent loads and barriers, 9 move) and by HBM where much does (8 views
+// of 131072 rows to 16384: 117 MB moved in 28 us, 4.2 TB/s in 2 KB chunks; loads
+// past the caches 24 us there, but 9.7 -> 11.8 for the short views).
 #include "cache.h"
 #include "common.h"
 
