@@ -117,7 +117,9 @@ int catekv_decode_attn_weights(int dtype, const catekv_decode_plan_t* plan, cons
                                float scale, float* out, float* lse, float* const* acc, float decay, void* ws,
                                size_t ws_bytes, void* wws, size_t wws_bytes, void* stream);
 
-/* Workspace bytes of the eviction calls; 0 for sizes they refuse. */
+/* Workspace bytes of the eviction calls; 0 for sizes they refuse.  Beside the
+ * bounds below these are sizes that would take a launch of 2^32 threads: none with
+ * max_rows up to 16384 or n_views * max_rows up to 2^32, all from 2^36 on. */
 size_t catekv_evict_workspace(int n_views, int64_t max_rows, int cs);
 
 /* Drops rows of every view by accumulated weight, in place.  Of the L = lens[bh]
@@ -141,7 +143,8 @@ size_t catekv_evict_workspace(int n_views, int64_t max_rows, int cs);
  * max_rows  a bound on lens (sizes the launches and the workspace), at most 2^26
  * cs in [1, 2^20], recent >= 0, n_views at most 2^16
  * Errors: INVALID_ARG for null pointers or bad sizes; UNSUPPORTED for an unknown
- * dtype, d != 128 or sizes above these bounds; WORKSPACE for a ws too small. */
+ * dtype, d != 128 or sizes above these bounds or for which
+ * catekv_evict_workspace() is 0; WORKSPACE for a ws too small. */
 int catekv_evict_kv(int dtype, const catekv_kv_ptrs* kv, int64_t* lens, float* const* acc, const int32_t* budget,
                     int n_views, int64_t max_rows, int cs, int recent, int d, void* ws, size_t ws_bytes,
                     void* stream);

@@ -16,6 +16,9 @@ bool host_plan_valid(const catekv_decode_plan_t* plan);
 // The plan's tables in its workspace; the other fields are the caller's.
 DecodeArgs host_plan_args(const catekv_decode_plan_t* plan, void* ws);
 
+// HIP takes launches of less than 2^32 threads.
+inline bool launch_fits(int64_t workgroups, int threads) { return workgroups * threads < (int64_t)1 << 32; }
+
 // ---- 8-bit caches ------------------------------------------------------------
 struct Q8Args {
   int block;                       // rows of a block: 32 or 64
@@ -73,7 +76,7 @@ struct EvictArgs {
   int64_t max_rows;
   void* ws;
 };
-// Sizes whose element numbers and launches fit 32 bits.
+// Sizes whose element numbers fit 32 bits and whose launches HIP takes.
 bool evict_fits(int n_views, int64_t max_rows, int cs);
 size_t evict_workspace_bytes(int n_views, int64_t max_rows, int cs);
 hipError_t launch_evict(const EvictArgs& a, hipStream_t stream);

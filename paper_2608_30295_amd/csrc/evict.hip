@@ -75,8 +75,18 @@ size_t evict_workspace_bytes(int n_views, int64_t max_rows, int cs) {
   return bytes;
 }
 
+// Chunks of a workgroup of evict_keys_kernel, and the workgroups per view of the
+// launches whose grid grows with the rows.
+static int key_chunks(int cs) { return kKeyRows / cs > 0 ? kKeyRows / cs : 1; }
+static int64_t key_groups(int64_t chunks, int cs) { return (chunks + key_chunks(cs) - 1) / key_chunks(cs); }
+static int64_t zero_groups(int64_t max_rows) { return (max_rows + kKeyRows - 1) / kKeyRows; }
+
 bool evict_fits(int n_views, int64_t max_rows, int cs) {
-  return max_rows <= kMaxEvictRows && cs <= kMaxEvictChunk && n_views <= kMaxEvictViews;
+  if (max_rows > kMaxEvictRows || cs > kMaxEvictChunk || n_views > kMaxEvictViews) return false;
+  if (max_rows <= kOwnKeyRows) return true;             // a workgroup or a few per view
+  const int64_t chunks = max_chunks_of(max_rows, cs);
+  return launch_fits(key_groups(chunks, cs) * n_views, kEvictThreads) && launch_fits(groups_of(chunks) * n_views, kEvictThreads) &&
+         launch_fits(zero_groups(max_rows) * n_views, kMoveThreads);
 }
 
 // Pointers that come out of tables are global ones: without the cast their accesses
@@ -777,7 +787,10 @@ __global__ __launch_bounds__(kMoveThreads) void evict_zero_kernel(EvictArgs a, c
   for (int64_t i = lo + threadIdx.x; i < hi; i += kMoveThreads) acc[i] = 0.f;
 }
 
+// Every launch is followed by a look at its status: none may run on what a refused one
+// before it has not written.
 hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
+  hipError_t e;
   const int64_t chunks = max_chunks_of(a.max_rows, a.cs), moves = max_moves_of(chunks);
   char* w = reinterpret_cast<char*>(a.ws);
   EvictInfo* infos = reinterpret_cast<EvictInfo*>(w);
@@ -792,24 +805,30 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
       const int64_t n = (int64_t)a.n_views * 3 * kBins;
       hipLaunchKernelGGL(evict_clear_kernel, dim3((unsigned)(n / kEvictThreads < 1024 ? n / kEvictThreads : 1024)),
                          dim3(kEvictThreads), 0, stream, hist, n);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    const int per_wg = kKeyRows / a.cs > 0 ? kKeyRows / a.cs : 1;
-    hipLaunchKernelGGL(evict_keys_kernel, dim3((unsigned)((chunks + per_wg - 1) / per_wg * a.n_views)), dim3(kEvictThreads), 0,
-                       stream, a, keys, hist, chunks, per_wg);
+    hipLaunchKernelGGL(evict_keys_kernel, dim3((unsigned)(key_groups(chunks, a.cs) * a.n_views)), dim3(kEvictThreads), 0, stream,
+                       a, keys, hist, chunks, key_chunks(a.cs));
+    if ((e = hipGetLastError()) != hipSuccess) return e;
     if (many) {
       GroupCount* counts = reinterpret_cast<GroupCount*>(behind + key_bytes(a.n_views, chunks) + hist_bytes(a.n_views));
       const int groups = (int)groups_of(chunks);
       const dim3 grid((unsigned)((int64_t)groups * a.n_views)), block(kEvictThreads);
       hipLaunchKernelGGL(evict_digit_kernel<1>, grid, block, 0, stream, a, keys, hist, chunks);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
       hipLaunchKernelGGL(evict_digit_kernel<2>, grid, block, 0, stream, a, keys, hist, chunks);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
       hipLaunchKernelGGL(evict_count_kernel, grid, block, 0, stream, a, infos, keys, hist, counts, chunks, groups);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
       hipLaunchKernelGGL(evict_list_kernel, grid, block, 0, stream, a, infos, pairs, keys, counts, chunks, moves, groups);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
   if (!many) {
     const int64_t in_lds = keys ? kRankChunks : chunks;
     hipLaunchKernelGGL(evict_select_kernel, dim3(a.n_views), dim3(kEvictThreads), (size_t)(in_lds + 4) * sizeof(uint32_t),
                        stream, a, infos, pairs, keys, chunks, moves);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   // A fill workgroup moves kTurn bytes per turn: as many as the most chunks that may
   // move keep busy, but about four rounds of the device at most.  A strip is as wide
@@ -826,9 +845,9 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
   const int shifts = (a.q8 ? 3 : 1) + 2 * ((a.row_bytes / 16) >> strip_log);
   hipLaunchKernelGGL(evict_move_kernel, dim3(a.n_views, shifts + 2 * fills + acc_fills), dim3(kMoveThreads), 0, stream, a,
                      infos, pairs, moves, fills, acc_fills, strip_log, keys == nullptr);
-  if (keys)
-    hipLaunchKernelGGL(evict_zero_kernel, dim3((unsigned)((a.max_rows + kKeyRows - 1) / kKeyRows * a.n_views)),
-                       dim3(kMoveThreads), 0, stream, a, infos);
+  if ((e = hipGetLastError()) != hipSuccess || !keys) return e;
+  hipLaunchKernelGGL(evict_zero_kernel, dim3((unsigned)(zero_groups(a.max_rows) * a.n_views)), dim3(kMoveThreads), 0, stream, a,
+                     infos);
   return hipGetLastError();
 }
 

@@ -1,0 +1,40 @@
+"""Sizes at which the calls of include/catekv_cache.h would need a launch of 2^32
+threads or more, which HIP does not take: refused on the host, before any launch."""
+import ctypes
+import os
+
+import pytest
+
+import paper_2608_30295_amd as ck
+from paper_2608_30295_amd import _lib
+
+pytestmark = pytest.mark.skipif(not os.path.exists(_lib.LIB_PATH), reason="libcatekv.so not built")
+
+FAKE = 0x100000   # a non-null pointer value; never dereferenced on these paths
+INVALID, UNSUPPORTED = _lib.CATEKV_ERR_INVALID_ARG, _lib.CATEKV_ERR_UNSUPPORTED
+HUGE = 1 << 60
+
+
+@pytest.mark.parametrize("n_views,max_rows,cs", [
+    (16384, 1 << 20, 64),             # keys: 256 workgroups of 1024 threads per view
+    (65536, 1 << 26, 64), (65536, 1 << 20, 4096), (65536, 1 << 26, 1 << 20),
+    (16384, 1 << 20, 1), (8192, 1 << 21, 8),
+    (8192, 1 << 24, 1 << 20),         # keys fit, the zeros behind the new lengths do not
+    (6000, 1 << 21, 2112),            # one chunk per workgroup of the keys: twice as many as of 4096 rows
+])
+def test_evictions_that_no_launch_takes(n_views, max_rows, cs):
+    L = ck.lib()
+    assert ck.evict_workspace(n_views, max_rows, cs) == 0
+    rest = (FAKE, FAKE, FAKE, FAKE, n_views, max_rows, cs, 0, 128, FAKE, HUGE, None)
+    assert L.catekv_evict_kv(1, *rest) == UNSUPPORTED
+    assert L.catekv_q8_evict(64, *rest) == UNSUPPORTED
+
+
+def test_evictions_just_below_the_limit_have_a_workspace():
+    for n_views, max_rows, cs in ((16383, 1 << 20, 64), (8191, 1 << 21, 8), (4095, 1 << 22, 1), (65536, 1 << 16, 8),
+                                  (65536, 16384, 1), (64, 1 << 26, 64)):
+        assert ck.evict_workspace(n_views, max_rows, cs) > 0, (n_views, max_rows, cs)
+    # as the header states: whatever cs is, while n_views * max_rows is at most 2^32
+    for cs in (1, 7, 64, 2049, 4096, 4097, 100_000, 1 << 20):
+        for n_views in (64, 4096, 65536):
+            assert ck.evict_workspace(n_views, (1 << 32) // n_views, cs) > 0, (n_views, cs)
