@@ -60,8 +60,9 @@ typedef struct catekv_q8_view {
  * views  [n_views] device
  * max_rows  a bound on lens (sizes the launch)
  * Errors: INVALID_ARG for null pointers, n_views < 1, max_rows < 1 or a block
- * other than 32 or 64; UNSUPPORTED for an unknown format or dtype, d != 128 or
- * max_rows above 2^31 - 1. */
+ * other than 32 or 64; UNSUPPORTED for an unknown format or dtype, d != 128,
+ * max_rows above 2^31 - 1 or sizes that would take a launch of 2^32 threads (64
+ * for each block and each tail, in fours: 2^26 of all views together). */
 int catekv_q8_quantize(int format, int dtype, int block, const catekv_kv_ptrs* kv, const int64_t* lens,
                        const catekv_q8_view* views, int n_views, int64_t max_rows, int d, void* stream);
 

@@ -33,7 +33,8 @@ struct Q8Args {
   int n_views;
   int64_t max_rows;
 };
-// Workgroups per view (K or V) of the first two; times n_views at most 2^31 - 1.
+// Workgroups per view (K or V) of the first two, of kQ8Threads threads.
+constexpr int kQ8Threads = 256;
 int64_t q8_groups(int64_t max_rows, int block);
 hipError_t launch_q8_quantize(int fmt, int dtype, const Q8Args& a, hipStream_t stream);
 hipError_t launch_q8_dequantize(int fmt, int dtype, const Q8Args& a, hipStream_t stream);

@@ -55,7 +55,7 @@ int check_convert(int format, int dtype, int block, const void* kv, const void* 
   if (!rc && (!kv || !lens || !views)) rc = fail(CATEKV_ERR_INVALID_ARG, "null pointer");
   if (!rc) rc = check_block(block);
   if (!rc) rc = check_rows(n_views, max_rows, d);
-  if (!rc && q8_groups(max_rows, block) * n_views > INT32_MAX)
+  if (!rc && !launch_fits(q8_groups(max_rows, block) * n_views, kQ8Threads))
     rc = fail(CATEKV_ERR_UNSUPPORTED, "n_views=%d of max_rows=%lld: too many blocks for one launch", n_views, (long long)max_rows);
   return rc;
 }

@@ -15,7 +15,7 @@
 namespace catekv {
 
 constexpr float kTinyMax = 7.888609052210118e-31f;   // 2^-100
-constexpr int kQ8Waves = 4;
+constexpr int kQ8Waves = kQ8Threads / 64;
 
 // 16 bytes that are read once: the rows on their way into codes.  They and the rows
 // written on the way back pass the caches by, which leaves these to the codes (8
@@ -171,7 +171,7 @@ struct BlockRows {
 // grid: (groups of kQ8Waves blocks x views, views fastest; 1; K and V).  The wave
 // behind a view's last whole block copies the remaining rows into the tail.
 template <int FMT, typename T, int BLOCK>
-__global__ __launch_bounds__(kQ8Waves * 64) void q8_quantize_kernel(Q8Args a) {
+__global__ __launch_bounds__(kQ8Threads) void q8_quantize_kernel(Q8Args a) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int group = blockIdx.x / a.n_views, bh = blockIdx.x - group * a.n_views;
   const bool is_v = blockIdx.z;
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(kQ8Waves * 64) void q8_quantize_kernel(Q8Args a) {
 }
 
 template <int FMT, typename T, int BLOCK>
-__global__ __launch_bounds__(kQ8Waves * 64) void q8_dequantize_kernel(Q8Args a) {
+__global__ __launch_bounds__(kQ8Threads) void q8_dequantize_kernel(Q8Args a) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int group = blockIdx.x / a.n_views, bh = blockIdx.x - group * a.n_views;
   const bool is_v = blockIdx.z;
@@ -294,7 +294,7 @@ enum Q8Op { kQuantize, kDequantize, kAppend };
 
 template <int FMT, typename T, int BLOCK>
 static hipError_t launch_q8_t(Q8Op op, const Q8Args& a, hipStream_t stream) {
-  const dim3 grid((unsigned)(q8_groups(a.max_rows, BLOCK) * a.n_views), 1, 2), block(kQ8Waves * 64);
+  const dim3 grid((unsigned)(q8_groups(a.max_rows, BLOCK) * a.n_views), 1, 2), block(kQ8Threads);
   if (op == kQuantize)
     hipLaunchKernelGGL((q8_quantize_kernel<FMT, T, BLOCK>), grid, block, 0, stream, a);
   else if (op == kDequantize)

@@ -38,3 +38,13 @@ def test_evictions_just_below_the_limit_have_a_workspace():
     for cs in (1, 7, 64, 2049, 4096, 4097, 100_000, 1 << 20):
         for n_views in (64, 4096, 65536):
             assert ck.evict_workspace(n_views, (1 << 32) // n_views, cs) > 0, (n_views, cs)
+
+
+@pytest.mark.parametrize("block,n_views,max_rows", [
+    (64, 4096, 1 << 20),              # 4097 workgroups of 256 threads per view: 4095 views are the most
+    (32, 2048, 1 << 20), (32, 16, (1 << 31) - 1), (64, 1 << 24, 1), (64, 1 << 22, 1000),
+])
+def test_conversions_that_no_launch_takes(block, n_views, max_rows):
+    L = ck.lib()
+    assert L.catekv_q8_quantize(0, 1, block, FAKE, FAKE, FAKE, n_views, max_rows, 128, None) == UNSUPPORTED
+    assert L.catekv_q8_dequantize(1, 0, block, FAKE, FAKE, FAKE, n_views, max_rows, 128, None) == UNSUPPORTED
