@@ -78,8 +78,8 @@ int catekv_q8_dequantize(int format, int dtype, int block, const catekv_q8_view*
  * [0, capacity[bh]) is left unchanged and sets *overflow = 1 when overflow is
  * not NULL.  The result is that of catekv_q8_quantize on the longer rows.
  * k_new, v_new  [batch][hkv][d] (dtype)
- * Errors: INVALID_ARG for null pointers, batch < 1, hkv < 1 or a bad block;
- * UNSUPPORTED for an unknown format or dtype or d != 128. */
+ * Errors: INVALID_ARG for null pointers, batch < 1, hkv < 1, batch * hkv of 2^23
+ * or more or a bad block; UNSUPPORTED for an unknown format or dtype or d != 128. */
 int catekv_q8_append(int format, int dtype, int block, const catekv_q8_view* views, const int64_t* capacity,
                      int64_t* lens, const void* k_new, const void* v_new, int batch, int hkv, int d,
                      int32_t* overflow, void* stream);

@@ -35,6 +35,7 @@ struct Q8Args {
 };
 // Workgroups per view (K or V) of the first two, of kQ8Threads threads.
 constexpr int kQ8Threads = 256;
+constexpr int kAppendThreads = 512;   // of the append's one workgroup per view
 int64_t q8_groups(int64_t max_rows, int block);
 hipError_t launch_q8_quantize(int fmt, int dtype, const Q8Args& a, hipStream_t stream);
 hipError_t launch_q8_dequantize(int fmt, int dtype, const Q8Args& a, hipStream_t stream);

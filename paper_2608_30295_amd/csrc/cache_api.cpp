@@ -175,7 +175,7 @@ int catekv_q8_append(int format, int dtype, int block, const catekv_q8_view* vie
   if (rc) return rc;
   if (batch < 1 || hkv < 1) return fail(CATEKV_ERR_INVALID_ARG, "batch=%d hkv=%d must be >= 1", batch, hkv);
   if (d != kD) return fail(CATEKV_ERR_UNSUPPORTED, "head dimension %d unsupported (only %d)", d, kD);
-  if ((int64_t)batch * hkv > (int64_t)INT32_MAX) return fail(CATEKV_ERR_INVALID_ARG, "batch * hkv too large");
+  if (!launch_fits((int64_t)batch * hkv, kAppendThreads)) return fail(CATEKV_ERR_INVALID_ARG, "batch * hkv too large");
   rc = check_aligned(k_new, "k_new");
   if (!rc) rc = check_aligned(v_new, "v_new");
   if (rc) return rc;

@@ -250,7 +250,6 @@ __global__ __launch_bounds__(kQ8Threads) void q8_dequantize_kernel(Q8Args a) {
 // One workgroup per view: four waves for K, four for V, a quarter of a block each
 // when the new row fills it.  That row is taken from the call's arguments, not from
 // the tail it was just stored in.
-constexpr int kAppendThreads = 512;
 template <int FMT, typename T, int BLOCK>
 __global__ __launch_bounds__(kAppendThreads) void q8_append_kernel(Q8Args a) {
   const int bh = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = wave & 3;

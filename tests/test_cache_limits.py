@@ -48,3 +48,10 @@ def test_conversions_that_no_launch_takes(block, n_views, max_rows):
     L = ck.lib()
     assert L.catekv_q8_quantize(0, 1, block, FAKE, FAKE, FAKE, n_views, max_rows, 128, None) == UNSUPPORTED
     assert L.catekv_q8_dequantize(1, 0, block, FAKE, FAKE, FAKE, n_views, max_rows, 128, None) == UNSUPPORTED
+
+
+def test_appends_that_no_launch_takes():
+    # 512 threads per view
+    for batch, hkv in ((1 << 20, 8), (1 << 23, 1), (1 << 24, 127)):
+        assert ck.lib().catekv_q8_append(1, 0, 32, FAKE, FAKE, FAKE, FAKE, FAKE, batch, hkv, 128, None, None) == INVALID
+        assert "too large" in ck.lib().catekv_last_error().decode()
