@@ -29,8 +29,8 @@
 
 namespace catekv {
 
-constexpr int kAtWaves = 8;
-constexpr int kAtThreads = kAtWaves * 64;
+constexpr int kAtThreads = kAttendThreads;
+constexpr int kAtWaves = kAtThreads / 64;
 constexpr int kAtMaxSeg = kDecodeV2MaxSeg;   // segments described in LDS at a time
 constexpr float kShift = 11.f;
 constexpr float kSlack = 4.f;
@@ -942,6 +942,8 @@ static hipError_t launch_attend_t(const AttendArgs& a, hipStream_t stream) {
   AttendArgs b = a;
   b.staged = staged;
   hipLaunchKernelGGL((attend_stream_kernel<K, G, ACC>), dim3(a.n_workers), dim3(kAtThreads), staged ? lds : 0, stream, b);
+  const hipError_t e = hipGetLastError();        // the join takes up what the stream kernel left
+  if (e != hipSuccess) return e;
   const int n_joins = a.n_multi > 0 ? a.n_views * G : 0;
   const int blocks = n_joins + (ACC ? a.n_workers : 0);
   if (blocks > 0)

@@ -42,6 +42,7 @@ hipError_t launch_q8_dequantize(int fmt, int dtype, const Q8Args& a, hipStream_t
 hipError_t launch_q8_append(int fmt, int dtype, const Q8Args& a, hipStream_t stream);
 
 // ---- attention -----------------------------------------------------------------
+constexpr int kAttendThreads = 512;   // of a workgroup of either kernel
 struct AttendArgs {
   const void* q;
   const void* views;               // catekv_kv_ptrs or catekv_q8_view, one per view

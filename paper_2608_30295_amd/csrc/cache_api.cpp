@@ -75,6 +75,10 @@ int attend_args(const catekv_decode_plan_t* plan, const void* q, const void* vie
                 hkv, plan->batch, plan->hq, plan->hkv);
   if (!(scale > 0.f) || !std::isfinite(scale))
     return fail(CATEKV_ERR_INVALID_ARG, "scale=%g must be positive and finite", (double)scale);
+  const int64_t joins = plan->n_multi > 0 ? (int64_t)batch * hq : 0;   // a workgroup per view and head of its group
+  if (!launch_fits(plan->n_workers, kAttendThreads) || !launch_fits(joins + (acc ? plan->n_workers : 0), kAttendThreads))
+    return fail(CATEKV_ERR_UNSUPPORTED, "batch=%d hq=%d, a plan of %d shares: too many workgroups for one launch", batch, hq,
+                plan->n_workers);
   rc = host_check_ws(ws, ws_bytes, plan->ws_bytes);
   if (rc) return rc;
   if (acc) {

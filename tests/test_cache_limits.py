@@ -55,3 +55,23 @@ def test_appends_that_no_launch_takes():
     for batch, hkv in ((1 << 20, 8), (1 << 23, 1), (1 << 24, 127)):
         assert ck.lib().catekv_q8_append(1, 0, 32, FAKE, FAKE, FAKE, FAKE, FAKE, batch, hkv, 128, None, None) == INVALID
         assert "too large" in ck.lib().catekv_last_error().decode()
+
+
+def plan_of(batch, hq, hkv, n_workers, n_multi):
+    p = _lib.DecodePlanT()
+    p.magic = 0x43617465504c414e                    # a plan header as catekv_decode_plan fills it
+    p.batch, p.hq, p.hkv, p.ws_bytes, p.n_workers, p.n_multi, p.variant = batch, hq, hkv, 1 << 12, n_workers, n_multi, 1
+    p.max_len_total = 1000
+    return p
+
+
+@pytest.mark.parametrize("batch,hq,hkv,n_workers,n_multi", [
+    (1, 8, 2, 1 << 23, 0),            # the stream: 512 threads per worker
+    (1 << 20, 8, 8, 4, 1),            # the join: as many per view and head, where a view has several parts
+    (1 << 18, 32, 4, 4, 1), (1 << 16, 8, 2, (1 << 23) - (1 << 19), 1),
+])
+def test_attention_steps_that_no_launch_takes(batch, hq, hkv, n_workers, n_multi):
+    L, p = ck.lib(), plan_of(batch, hq, hkv, n_workers, n_multi)
+    rest = (ctypes.byref(p), FAKE, FAKE, FAKE, batch, hq, hkv, 128, 0.1, FAKE, None, FAKE, 1.0, FAKE, HUGE, FAKE, HUGE, None)
+    assert L.catekv_decode_attn_weights(1, *rest) == UNSUPPORTED
+    assert L.catekv_q8_decode_attn(0, 1, 64, *rest) == UNSUPPORTED
