@@ -92,7 +92,9 @@ size_t catekv_weights_workspace(const catekv_decode_plan_t* plan);
  * their codes times their scales.  dtype is that of q and of the tails.  With
  * acc, the step's softmax weights are added up per row,
  *   acc[bh][t] = decay * acc[bh][t] + (1/G) sum_g softmax_g(t),  t < L,
- * over the G query heads of the view's group; rows from L on are not touched.
+ * over the G query heads of the view's group; rows from L on are not touched.  A head
+ * whose rows all score -inf (out 0, lse -inf) adds nothing; one whose output is NaN
+ * adds NaN.
  * views   [batch][hkv] device
  * lens    [batch][hkv] int64, device; L = min(lens, planned max_len).  The tail
  *         starts at lens / block * block whatever the plan says

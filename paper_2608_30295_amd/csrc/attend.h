@@ -901,7 +901,8 @@ __global__ __launch_bounds__(kAtThreads) void attend_join_kernel(AttendArgs a) {
 #pragma unroll
         for (int u = 0; u < NT / 64; ++u) Lx += s_s[u][g] * fast_exp2(s_m[u][g] - Mx);
         mg[g] = Mx;
-        ig[g] = fast_exp2(kShift) / (Lx * (float)G);
+        // a head whose rows all score -inf gives none of them weight (out 0, lse -inf)
+        ig[g] = Lx == 0.f ? 0.f : fast_exp2(kShift) / (Lx * (float)G);
       }
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
