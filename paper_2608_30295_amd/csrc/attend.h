@@ -34,7 +34,9 @@ constexpr int kAtWaves = kAtThreads / 64;
 constexpr int kAtMaxSeg = kDecodeV2MaxSeg;   // segments described in LDS at a time
 constexpr float kShift = 11.f;
 constexpr float kSlack = 4.f;
-constexpr float kAtFloor = -1e30f;           // maximum of no row: 2^(floor - m) = 0, and no inf - inf
+// Maximum of no row, the lowest finite number: 2^(floor - m) is 0 for any score above
+// it, 2^(-inf - floor) is 0, and inf - inf does not come up.
+constexpr float kAtFloor = -3.402823466e38f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));

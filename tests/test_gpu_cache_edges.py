@@ -73,3 +73,43 @@ def test_rows_that_score_minus_infinity_gather_no_weight(kind):
         # half of what was there, exactly
         assert np.array_equal(new[:n[i]][gone[i]], 0.5 * old[:n[i]][gone[i]]), i
         assert np.array_equal(new[n[i]:], old[n[i]:]), i
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_scores_far_below_zero(kind):
+    """Rows that are all alike and score about -10^34, which an fp32 holds: every one has
+    weight 1 / n.
+
+    Tolerances, u = 2^-24: a score is one product with at most 8 roundings (the product, the
+    scale's two, the 8-bit factor's three, ln 2 and log2 e), the rows' scores are the same
+    bits, so that P is the same number p for all.  An output sums n products p V and
+    divides by n p: at most n + 8 roundings of sum |V| / n.  A weight is p / (4 n p) four
+    times: 12 roundings, exp2's two units in the last place among them, and those of
+    decay * acc + weight."""
+    rng = np.random.default_rng(52)
+    dtype, hkv, G, u = kind if kind in DT else "bf16", 2, 4, 2.0 ** -24
+    # in 8 bits either all rows are codes or all lie in the tail, which scores the row's own value
+    n = [1, 20, 64, 192] if kind in ("int8", "e4m3") else [1, 300, 17, 64]
+    rows = []
+    for m in n:
+        k = np.zeros((m, D))
+        k[:, 5] = -1e18
+        rows.append((torch.from_numpy(k).to(DT[dtype]).double().numpy(), stored(rng, m, dtype)))
+    q = torch.zeros((2, hkv * G, D))
+    q[..., 5] = 1e17
+    q = q.to(DT[dtype]).to(DEV)
+    a, a0, table = accs(rng, n)
+    out, lse, held = attend(kind, rows, q, n, hkv, table, 1.0)
+    qd = q.double().cpu().numpy()
+    for i, (k, v) in enumerate(held):
+        b, h = divmod(i, hkv)
+        heads, m = slice(h * G, (h + 1) * G), n[i]
+        want, wl, w, _, pv = R.attend(qd[b, heads], k, v, 1 / math.sqrt(D))
+        assert wl.max() < -1e33 and np.allclose(w, 1 / m, rtol=1e-12)
+        got, gl = out[b, heads].double().cpu().numpy(), lse[b, heads].double().cpu().numpy()
+        assert (np.abs(got - want) <= (m + 8) * u * pv).all(), i
+        assert (np.abs(gl - wl) <= 8 * u * np.abs(wl)).all(), i
+        ref = a0[i].double().cpu().numpy()
+        ref[:m] += w
+        assert (np.abs(a[i].double().cpu().numpy() - ref)[:m] <= 12 * u * w + 2 * u * ref[:m]).all(), i
+        assert same(a[i][m:], a0[i][m:]), i
