@@ -855,7 +855,8 @@ __global__ __launch_bounds__(kAtThreads) void attend_join_kernel(AttendArgs a) {
       const int srows = (t1 - t0 + 63) & ~63;
       const float* sc = a.scores + ((size_t)w * a.score_rows + soff) * G;
       soff += srows;
-      const int64_t len = a.lens[bh];
+      int64_t len = a.lens[bh];
+      len = len < 0 ? 0 : len;                    // as the stream kernel reads it: the low 32 bits mean nothing
       const ViewInfo vi = a.infos[bh];
       auto acc = (__attribute__((address_space(1))) float*)(a.acc[bh] + t0);
       const int n = (int)(len < (int64_t)t1 ? len : (int64_t)t1) - t0;

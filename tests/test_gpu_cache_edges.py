@@ -113,3 +113,27 @@ def test_scores_far_below_zero(kind):
         ref[:m] += w
         assert (np.abs(a[i].double().cpu().numpy() - ref)[:m] <= 12 * u * w + 2 * u * ref[:m]).all(), i
         assert same(a[i][m:], a0[i][m:]), i
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_views_of_negative_length_are_empty(kind):
+    """Whatever the low 32 bits of the length say."""
+    rng = np.random.default_rng(53)
+    dtype = kind if kind in DT else "bf16"
+    n = [500, 500, 500, 500, 3000, 3000]
+    rows = [(stored(rng, m, dtype), stored(rng, m, dtype)) for m in n]
+    lens = lens_of(-1, 500, -2 ** 33 + 300, -2 ** 62 + 17, -2 ** 40 + 2900, 3000)
+    q = dense(rng, 24, dtype).view(3, 8, D).to(DEV)
+    a, a0, table = accs(rng, n)
+    out, lse, held = attend(kind, rows, q, n, 2, table, 1.0, lens)
+    for i, m in enumerate(lens.tolist()):
+        b, h = divmod(i, 2)
+        heads = slice(4 * h, 4 * h + 4)
+        if m < 0:
+            assert same(a[i], a0[i]) and not out[b, heads].any() and torch.isneginf(lse[b, heads]).all(), i
+        else:
+            k, v = held[i]
+            _, _, w, sa, _ = R.attend(q[b, heads].double().cpu().numpy(), k, v, 1 / math.sqrt(D))
+            new, ref = (x[i][:m].double().cpu().numpy() for x in (a, a0))
+            ref = ref + w
+            assert (np.abs(new - ref) <= R.weight_error(sa, m) * w + 2.0 ** -23 * ref).all(), i
