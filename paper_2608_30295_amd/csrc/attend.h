@@ -414,7 +414,7 @@ __global__ __launch_bounds__(kAtThreads) __attribute__((amdgpu_waves_per_eu(2, 2
 void attend_stream_kernel(AttendArgs a) {
   typedef typename K::T T;
   constexpr int WAVES = kAtWaves, NT = kAtThreads, TOK = K::TOK, NS = TOK / 16;
-  constexpr int SF = G * kD + 2 * G;
+  constexpr int SF = (int)decode_slot_floats(G);
   constexpr int QW = kD * (int)sizeof(T) / 16;   // 16-byte words of a query row
   const int lane = threadIdx.x & 63;
   const int wave = threadIdx.x >> 6;
@@ -732,7 +732,7 @@ constexpr int kFewParts = 8;
 // when it has more than one.
 template <int G, bool ACC>
 __global__ __launch_bounds__(kAtThreads) void attend_join_kernel(AttendArgs a) {
-  constexpr int SF = G * kD + 2 * G;
+  constexpr int SF = (int)decode_slot_floats(G);
   constexpr int NT = kAtThreads;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   if (!ACC || (int)blockIdx.x >= a.n_workers) {

@@ -148,7 +148,7 @@ __device__ __forceinline__ void emit(float* out, float* lse, size_t row, int e, 
 // [worker_seg[w], worker_seg[w + 1]) of the plan, each a token range of one view.
 template <typename T, int G, int WAVES, int NS>
 __global__ __launch_bounds__(WAVES * 64) void decode_stream_kernel(DecodeArgs a) {
-  constexpr int SF = G * kD + 2 * G;            // floats per partial slot
+  constexpr int SF = (int)decode_slot_floats(G);
   constexpr int NT = WAVES * 64;
   constexpr int TPW = 8;                        // tokens per wave per stage
   const int lane = threadIdx.x & 63;
@@ -343,7 +343,7 @@ template <int G, int WAVES, int NS>
 __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void decode_stream_mfma_kernel(DecodeArgs a) {
   static_assert(G <= 16, "heads of a group must fit the 16 MFMA columns");
-  constexpr int SF = G * kD + 2 * G;
+  constexpr int SF = (int)decode_slot_floats(G);
   constexpr int NT = WAVES * 64;
   constexpr int TPW = 16;                       // tokens per wave per stage
   const int lane = threadIdx.x & 63;
@@ -573,7 +573,7 @@ void decode_stream_v2_kernel(DecodeArgs a) {
   static_assert(G <= 16, "heads of a group must fit the 16 MFMA columns");
   constexpr int WAVES = kV2Waves;
   constexpr int NT = WAVES * 64;
-  constexpr int SF = G * kD + 2 * G;
+  constexpr int SF = (int)decode_slot_floats(G);
   const int lane = threadIdx.x & 63;
   const int wave = threadIdx.x >> 6;
   const int n16 = lane & 15, k4 = lane >> 4;
@@ -861,7 +861,7 @@ constexpr int kCombineBatch = 16;                      // parts per thread per r
 
 template <int G>
 __global__ __launch_bounds__(kCombineThreads) void decode_combine_kernel(DecodeArgs a) {
-  constexpr int SF = G * kD + 2 * G;
+  constexpr int SF = (int)decode_slot_floats(G);
   const int bh = blockIdx.x / G, g = blockIdx.x - (blockIdx.x / G) * G;
   const ViewInfo vi = a.views[bh];
   const int P = vi.n_parts;

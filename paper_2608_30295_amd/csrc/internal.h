@@ -49,8 +49,9 @@ struct ViewInfo {
 };
 
 // Floats per decode partial slot for a group of G query heads: o[G][128],
-// m[G], l[G].
-inline size_t decode_slot_floats(int G) { return (size_t)G * 128 + 2 * (size_t)G; }
+// m[G], l[G], and padding that keeps every slot's o on a 16-byte border (G = 1:
+// the joins read four values at a time).
+constexpr size_t decode_slot_floats(int G) { return ((size_t)G * 128 + 2 * (size_t)G + 3) & ~(size_t)3; }
 
 struct DecodeArgs {
   const void* q;

@@ -3,6 +3,7 @@ threads or more, which HIP does not take: refused on the host, before any launch
 import ctypes
 import os
 
+import numpy as np
 import pytest
 
 import paper_2608_30295_amd as ck
@@ -75,3 +76,17 @@ def test_attention_steps_that_no_launch_takes(batch, hq, hkv, n_workers, n_multi
     rest = (ctypes.byref(p), FAKE, FAKE, FAKE, batch, hq, hkv, 128, 0.1, FAKE, None, FAKE, 1.0, FAKE, HUGE, FAKE, HUGE, None)
     assert L.catekv_decode_attn_weights(1, *rest) == UNSUPPORTED
     assert L.catekv_q8_decode_attn(0, 1, 64, *rest) == UNSUPPORTED
+
+
+def test_partials_lie_on_16_byte_borders():
+    """The kernels that join a view's partials read them 16 bytes at a time.  A plan's bytes
+    differ between group sizes by its partials alone: 256 parts, each o [G][128], m [G] and
+    l [G] in fp32."""
+    def total(G):
+        n = np.array([256 * 64], dtype=np.int64)
+        return ck.lib().catekv_decode_workspace(n.ctypes.data_as(ctypes.POINTER(ctypes.c_int64)), 1, G, 1, 64)
+    more = [(total(G) - total(8)) / 256 for G in (1, 2, 4)]
+    eight = 4 * (8 * 128 + 2 * 8)
+    assert eight % 16 == 0
+    for G, m in zip((1, 2, 4), more):
+        assert (eight + m) % 16 == 0 and 0 <= eight + m - 4 * (G * 128 + 2 * G) < 16, G
