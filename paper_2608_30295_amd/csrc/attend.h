@@ -48,17 +48,13 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
-// Rows of K and V, read once per step: their loads pass the caches by.  us per step,
-// cached / past the caches: int8 1M 100.4 / 95.4, e4m3 16 x 16K-64K with the append
-// 125.4 / 119.6, bf16 128K with weights 48.4 / 44.3; over the caches of 24 layers
-// in turn e4m3 128K 28.6 / 27.8, int8 16 x 2304 with append and weights 39.4 / 37.6.
-// Where the Infinity Cache would have kept rows from one step to the next it is
-// the other way round: the same two over 3 layers 26.2 / 27.1 and 36.0 / 36.7.
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ uint4 once16(const void* p) {
-  const u32x4 v = __builtin_nontemporal_load((const __attribute__((address_space(1))) u32x4*)(p));
-  return make_uint4(v.x, v.y, v.z, v.w);
-}
+// Rows of K and V, read once per step: their loads pass the caches by (once16, and
+// the same for 8 bytes).  us per step, cached / past the caches: int8 1M 100.4 / 95.4,
+// e4m3 16 x 16K-64K with the append 125.4 / 119.6, bf16 128K with weights 48.4 / 44.3;
+// over the caches of 24 layers in turn e4m3 128K 28.6 / 27.8, int8 16 x 2304 with
+// append and weights 39.4 / 37.6.  Where the Infinity Cache would have kept rows from
+// one step to the next it is the other way round: the same two over 3 layers 26.2 /
+// 27.1 and 36.0 / 36.7.
 __device__ __forceinline__ uint2 once8(const void* p) {
   const u32x2 v = __builtin_nontemporal_load((const __attribute__((address_space(1))) u32x2*)(p));
   return make_uint2(v.x, v.y);

@@ -17,14 +17,10 @@ namespace catekv {
 constexpr float kTinyMax = 7.888609052210118e-31f;   // 2^-100
 constexpr int kQ8Waves = kQ8Threads / 64;
 
-// 16 bytes that are read once: the rows on their way into codes.  They and the rows
-// written on the way back pass the caches by, which leaves these to the codes (8
+// The rows on their way into codes are read once (once16).  They and the rows written
+// on the way back pass the caches by, which leaves these to the codes (8
 // heads of 131072 bf16 rows into e4m3 and back 306 -> 258 us, of 32768 87 -> 71; one
 // way alone 45 -> 39 and 47 -> 33 at 32768, 150 -> 149 and 155 -> 147 at 131072).
-__device__ __forceinline__ uint4 once16(const void* p) {
-  const u32x4_t v = __builtin_nontemporal_load((const __attribute__((address_space(1))) u32x4_t*)p);
-  return make_uint4(v.x, v.y, v.z, v.w);
-}
 
 // 16 bytes of a row: kN elements.
 template <typename T>
