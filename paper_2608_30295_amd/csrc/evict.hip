@@ -33,11 +33,22 @@ constexpr int kMoveThreads = 256;
 constexpr int64_t kMaxEvictRows = 1 << 26;   // 32 pieces a row, a workgroup per kKeyRows rows:
 constexpr int kMaxEvictChunk = 1 << 20;      // element, piece and workgroup numbers stay below 2^31
 constexpr int kMaxEvictViews = 1 << 16;
-constexpr int kRankChunks = 384;        // up to here a chunk's rank is counted
-constexpr int kOneChunks = 16 * kEvictThreads;   // most chunks of a selecting workgroup
+// Up to so many chunks their ranks are counted, else the k-th largest key is selected
+// by radix.  us of the selecting launch, counted / radix, 128 views of 64 chunks: 6.2 /
+// 8.8, 128: 6.2 / 9.3, 256: 7.4 / 9.4, 384: 9.4 / 10.0, 512: 10.6 / 9.3, 768: 18.6 / 10.5.
+constexpr int kRankChunks = 384;
+constexpr int kOneChunks = 16 * kEvictThreads;   // most chunks of a selecting workgroup (their keys' registers)
 constexpr int kGroupChunks = 4 * kEvictThreads;  // chunks of one of many
-constexpr int kOwnKeyRows = 16384;      // views up to here: keys by the selecting workgroup
-constexpr int kKeyRows = 4096;          // else by a workgroup per so many rows
+// Views up to here: keys and zeros by the selecting and the shifting workgroup, two
+// launches less.  us of all kernels, own / launches of their own, chunks of 8 rows, 64
+// views of 8256 rows: 26.4 / 27.7, 16384: 40 / 42, 20480: 56 / 55, 32768: 89 / 78.  Of
+// 8 views the launches are ahead throughout (8256: 20 / 18, 16384: 27 / 19, 32768: 52 /
+// 30), what two more cost the caller not counted.
+constexpr int kOwnKeyRows = 16384;
+// Else by a workgroup per so many rows.  us of the keys at 2048 / 4096 / 8192 rows: 32
+// views of 32768 rows 5.5 / 4.4 / 5.5, 8 of 131072 5.7 / 4.4 / 5.6, 32 of 131072 15.0 /
+// 9.6 / 7.5, 8 of 524288 17.4 / 10.4 / 8.6.
+constexpr int kKeyRows = 4096;
 
 struct EvictInfo {
   int32_t moves;                        // pairs; the view is left alone if shift is 0
@@ -369,7 +380,9 @@ __device__ __forceinline__ bool stays_at(uint32_t x, bool valid, uint32_t limit,
   return st;
 }
 
-// A lane's R keys in registers: nc <= 1024 R.
+// A lane's R keys in registers: nc <= 1024 R.  R = 2 where they fit, else 16: us of the
+// selecting launch with 2 / 16, 512 chunks 8.9 / 15.0, 1024: 11.1 / 17.5, 2048: 12.9 /
+// 19.2.
 template <int R, typename Load>
 __device__ __forceinline__ int register_pairs(SelectShared& s, Load load, int nc, int k, int covered, int32_t* pairs) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -831,7 +844,10 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t stream) {
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   // A fill workgroup moves kTurn bytes per turn: as many as the most chunks that may
-  // move keep busy, but about four rounds of the device at most.  A strip is as wide
+  // move keep busy, but about four rounds of the device at most (512 each for K and V,
+  // at least 4 per view.  us of the move with 128 / 512 / 2048: 128 views of 2304 rows,
+  // 40 chunks to drop, 8.4 / 8.5 / 10.0; 8 views of 131072 rows to 16384 31.1 / 23.6 /
+  // 22.9; 128 of 16384 to 8192 119.4 / 119.6 / 114.7).  A strip is as wide
   // as its workgroup moves in one turn, the rows behind the chunks being fewer than
   // recent + cs and those filled first hardly more.
   constexpr int64_t kTurn = kMoveThreads * kMoveBatch * 16;
