@@ -141,6 +141,8 @@ size_t catekv_evict_workspace(int n_views, int64_t max_rows, int cs);
  *     to L, and the rows of K and V from there on are left as they were.
  * A view with budget[bh] < 0 or nc <= budget[bh], or with lens outside
  * [0, max_rows], is left alone.
+ * Afterwards lens[bh] <= budget[bh] cs + recent + cs - 1 (where budget[bh] >= 0 and
+ * lens was in range), a bound for the plan and max_rows of the steps that follow.
  * kv      [n_views] device, rows in dtype
  * lens    [n_views] int64, device, read and written
  * acc     [n_views] device pointers to fp32 arrays of at least lens values

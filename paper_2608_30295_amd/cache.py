@@ -256,7 +256,13 @@ def evict_kv(kv: torch.Tensor, lens: torch.Tensor, acc: torch.Tensor, budget: to
     view's chunks before the last `recent` rows, the budget[view] with the
     largest acc stay (catekv_evict_kv).  lens is updated on the device; acc moves
     with its rows.  budget: int32 on the GPU, one per view, < 0 leaves a view
-    alone.  dtype: that of the rows."""
+    alone.  dtype: that of the rows.
+
+    Afterwards a view has at most budget * cs + recent + cs - 1 rows.  A plan cuts its
+    shares by the lengths planned for, and one for the rows before leaves most of the
+    GPU idle: make a new one (and choose max_rows) for that bound and the steps until
+    the next eviction (8 int8 views from 131072 to 16512 rows: 50 us a step under the
+    old plan, 17 under the new one)."""
     if dtype not in (torch.bfloat16, torch.float32):
         raise TypeError(f"unsupported dtype {dtype} (bfloat16 or float32)")
     _need_table(kv, kv.shape[0])
