@@ -12,9 +12,11 @@
 // Bound by HBM: 4 FLOP per byte of bf16, 8 per byte of codes.  128K rows (3 full
 // views, 5 of 2112 rows) in e4m3: 103 MB in 24 us, 6 TB/s from the first tile's
 // request (2.6 us: three dependent loads, the query rows) to the end of the average
-// share, 3 us more to that of the slowest XCD; the same in bf16 with weights: 206 MB
-// in 36 us; 1M rows (2 views) in int8: 544 MB in 97 us (5.6 TB/s).  The join takes
-// 4 to 5 us more, with weights 7.
+// share, 3 us more to that of the slowest XCD (by time stamps in a copy); the same in
+// bf16 with weights: 206 MB in 37 us; 1M rows (2 views) in int8: 544 MB in 95 us (5.7
+// TB/s).  What is read from memory is what there is (104 MB, 207 MB and 546 MB by the
+// counters, the tables and queries with it).  The join takes 4 to 5 us more, with
+// weights 7, in fp32 9.
 //
 // Work: the plan's shares (equal numbers of rows), one workgroup of 8 waves
 // each, tile u of a segment to wave u % 8, two tiles per wave in flight across
@@ -196,8 +198,9 @@ struct Rows16 {
 // down to 2^-31 of the largest (below, off by at most 2^-39 of it); an fp32 row is
 // split into two fp16 rows (22 bits).  The block's K scale multiplies the scores
 // in fp32, its V scale the tile's P V sums.  Converting costs 1.25 (int8) or 0.5
-// instructions per code of K and about twice that with the transpose of V: by
-// count a third of the issue slots while HBM delivers 6 TB/s.  Tiles of 16 rows: 27.2
+// instructions per code of K and about twice that with the transpose of V: by the
+// counters 31% of the issue slots in e4m3 (128K rows: 4.5M wave instructions in 24 us),
+// 44% in int8 (1M: 25.6M in 95 us), the matrix cores busy 6 and 11%.  Tiles of 16 rows: 27.2
 // against 26.8 us at 128K, 135.5 against 132.0 at 16 x 16K-64K (e4m3).
 template <int FMT, typename QT>
 struct Kind8 {
@@ -727,8 +730,8 @@ constexpr int kFewParts = 8;
 
 // ---- joining the partials, and the weights ----------------------------------------
 // With acc, workgroup w < n_workers first: the weights of worker w's rows, from the
-// scores it kept (in the L2 of the same XCD) and from all of the view's (m, l); they
-// take longer than the rest.  Behind them, for every view and head: its partials,
+// scores it kept (they come from behind the L2: 9.1 MB read at 128K rows, of them 6.5
+// scores) and from all of the view's (m, l); they take longer than the rest.  Behind them, for every view and head: its partials,
 // when it has more than one.
 template <int G, bool ACC>
 __global__ __launch_bounds__(kAtThreads) void attend_join_kernel(AttendArgs a) {

@@ -19,8 +19,11 @@
 //
 // Bound by latency where little moves (16 x 8 views of 2304 rows: 9 us select, of
 // it 5 in dependent loads and barriers, 9 move) and by HBM where much does (8 views
-// of 131072 rows to 16384: 117 MB moved in 28 us, 4.2 TB/s in 2 KB chunks; loads
-// past the caches 24 us there, but 9.7 -> 11.8 for the short views).
+// of 131072 rows to 16384: 117 MB moved in 26 us, 4.5 TB/s in 2 KB chunks, 61 MB read
+// and 60 written by the counters; loads past the caches 24 us there, but 9.7 -> 11.8
+// for the short views).  Many rows behind the chunks are what it is slow at: their few
+// workgroups take them turn by turn (8 views of 131072 bf16 rows to 8192 and the rows
+// behind: move 17 us with recent = 1024, 62 with 8192; in e4m3 42 with 8192).
 #include "cache.h"
 #include "common.h"
 

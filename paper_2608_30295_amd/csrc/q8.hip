@@ -7,8 +7,9 @@
 // on the way, and both sides are read and written in whole lines (lanes with 32
 // consecutive bytes of fp32, half a line per access: 4099 fp32 rows of 8 heads back
 // from int8 15.2 -> 8.4 us).  131072 bf16 rows of 8 heads: 805 MB in 149 us into
-// e4m3, in 147 us back (5.4 and 5.5 TB/s; a copy runs at 5.15), 140 and 117 right after
-// one another, as the codes are then partly in the Infinity Cache.
+// e4m3, in 147 us back (5.4 and 5.5 TB/s; a copy runs at 5.15), 136 and 117 right after
+// one another (the codes then come partly from the Infinity Cache, it seems: the L2
+// asks for all of their 269 MB).
 #include "cache.h"
 #include "common.h"
 
