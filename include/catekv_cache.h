@@ -107,9 +107,10 @@ size_t catekv_weights_workspace(const catekv_decode_plan_t* plan);
  * wws     catekv_weights_workspace() bytes (ignored without acc); calls that
  *         overlap in time must not share it
  * Errors: those of catekv_decode_attn; INVALID_ARG for a bad block or decay;
- * UNSUPPORTED for an unknown format or 2^23 or more of a plan's shares or, where it
- * splits a view, of query rows (batch * hq; of both together with acc); WORKSPACE
- * for a wws too small. */
+ * UNSUPPORTED for an unknown format or a plan that would take a launch of 2^32
+ * threads (512 for each of its shares; 512 for each query row, batch * hq, where it
+ * splits a view, and with acc for each share besides); WORKSPACE for a wws too
+ * small. */
 int catekv_q8_decode_attn(int format, int dtype, int block, const catekv_decode_plan_t* plan, const void* q,
                           const catekv_q8_view* views, const int64_t* lens, int batch, int hq, int hkv, int d,
                           float scale, float* out, float* lse, float* const* acc, float decay, void* ws,

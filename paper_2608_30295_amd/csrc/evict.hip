@@ -44,9 +44,9 @@ constexpr int kOneChunks = 16 * kEvictThreads;   // most chunks of a selecting w
 constexpr int kGroupChunks = 4 * kEvictThreads;  // chunks of one of many
 // Views up to here: keys and zeros by the selecting and the shifting workgroup, two
 // launches less.  us of all kernels, own / launches of their own, chunks of 8 rows, 64
-// views of 8256 rows: 26.4 / 27.7, 16384: 40 / 42, 20480: 56 / 55, 32768: 89 / 78.  Of
-// 8 views the launches are ahead throughout (8256: 20 / 18, 16384: 27 / 19, 32768: 52 /
-// 30), what two more cost the caller not counted.
+// views of 8256 rows: 26.4 / 27.7, 16384: 40 / 42, 20480: 56 / 55, 32768: 89 / 78; us
+// of a pass over 8 views of 8256 rows 22.5 / 22.8, 12288: 26.0 / 22.5, 16384: 30.4 /
+// 22.4 (64 of 16384: 45.8 / 44.9), so that 8192 would suit few views better.
 constexpr int kOwnKeyRows = 16384;
 // Else by a workgroup per so many rows.  us of the keys at 2048 / 4096 / 8192 rows: 32
 // views of 32768 rows 5.5 / 4.4 / 5.5, 8 of 131072 5.7 / 4.4 / 5.6, 32 of 131072 15.0 /
