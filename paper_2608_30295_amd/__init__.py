@@ -37,3 +37,17 @@ from .cache import (  # noqa: F401
     quantize_kv,
     weights_workspace,
 )
+from .paged import (  # noqa: F401
+    PagedCache,
+    PagedPlan,
+    append_kv_paged,
+    attn_paged,
+    compact_kv_paged,
+    compact_paged_workspace,
+    drop_paged,
+    fork_paged,
+    gather_kv_paged,
+    paged_alloc,
+    paged_plan,
+    paged_workspace,
+)

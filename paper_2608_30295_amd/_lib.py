@@ -92,6 +92,36 @@ CACHE_SIGNATURES = {
                                 c_void_p, c_size, c_void_p]),
 }
 
+# include/catekv_paged.h
+class PagedCacheT(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("k", "v", "table", "lens", "refs", "free_bits")] + [
+        (n, ctypes.c_int32) for n in ("dtype", "page", "n_pages", "n_slots", "hkv", "max_pages")]
+
+
+class PagedPlanT(ctypes.Structure):
+    _fields_ = [("magic", ctypes.c_uint64)] + [
+        (n, ctypes.c_int32) for n in ("n_seqs", "n_tokens", "hq", "hkv", "n_slots", "page", "dtype", "n_tile",
+                                      "n_workers", "n_joins", "join_rows", "reserved")] + [
+        (n, ctypes.c_uint64) for n in ("seqs_off", "toks_off", "tiles_off", "segs_off", "workers_off", "joins_off",
+                                       "views_off", "takes_off", "slots_off", "ws_bytes")]
+
+
+P_cache, P_plan = ctypes.POINTER(PagedCacheT), ctypes.POINTER(PagedPlanT)
+PAGED_SIGNATURES = {
+    "catekv_paged_init": (c_int, [P_cache, c_void_p]),
+    "catekv_paged_workspace": (c_size, [P_cache, P_i32, P_i32, P_i64, c_int, c_int]),
+    "catekv_paged_plan": (c_int, [P_cache, P_i32, P_i32, P_i64, c_int, c_int, P_plan, c_void_p, c_size, c_void_p]),
+    "catekv_paged_append": (c_int, [P_cache, P_plan, c_void_p, c_void_p, c_i64, c_i64, c_void_p, c_void_p, c_size,
+                                    c_void_p]),
+    "catekv_paged_attn": (c_int, [P_cache, P_plan, c_void_p, c_float, c_void_p, c_void_p, c_void_p, c_size, c_void_p]),
+    "catekv_paged_fork": (c_int, [P_cache, P_i32, P_i32, c_int, c_void_p, c_void_p]),
+    "catekv_paged_drop": (c_int, [P_cache, c_void_p, c_void_p]),
+    "catekv_paged_compact_workspace": (c_size, [P_cache, c_int, c_int, c_int, c_int]),
+    "catekv_paged_compact": (c_int, [P_cache, c_int, P_i32, c_int, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p,
+                                     c_size, c_void_p]),
+    "catekv_paged_gather": (c_int, [P_cache, P_i32, c_int, c_void_p, c_i64, c_void_p]),
+}
+
 _lib = None
 
 
@@ -109,7 +139,7 @@ def lib() -> ctypes.CDLL:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing; build it with `python -m paper_2608_30295_amd.build`")
         L = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in {**SIGNATURES, **CACHE_SIGNATURES}.items():
+        for name, (res, args) in {**SIGNATURES, **CACHE_SIGNATURES, **PAGED_SIGNATURES}.items():
             fn = getattr(L, name)
             fn.restype = res
             fn.argtypes = args

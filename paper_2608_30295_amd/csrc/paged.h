@@ -1,0 +1,132 @@
+// Internal interface of the caches in pages: what paged_api.cpp passes to the
+// kernels of paged_pages.hip, paged_tile.hip and paged_stream.hip.
+#pragma once
+
+#include "cache.h"
+#include "catekv_paged.h"
+
+namespace catekv {
+
+constexpr int64_t kPagedMaxRows = (int64_t)1 << 26;   // of a view
+constexpr int kPagedMaxList = 256;                    // slots of a fork or a gather
+constexpr int kPagedMaxHeads = 128;                   // heads of a compaction
+constexpr int kPagedMaxHkv = 1024;                    // views of a slot (threads of the taking workgroup)
+
+// The cache as kernels see it.
+struct PagedCache {
+  char* k;
+  char* v;
+  int32_t* table;
+  int64_t* lens;
+  int32_t* refs;
+  uint64_t* bits;
+  int32_t n_pages, n_slots, hkv, max_pages;
+  int32_t page_log;                 // page = 1 << page_log rows
+  int32_t row_bytes;                // of a K or V row
+};
+
+// A sequence of a plan.
+struct PagedSeq {
+  int32_t slot, n_new, tok0, pad;
+};
+
+// What the append's first launch leaves for its second, per view of the batch.
+struct PagedTake {
+  int64_t len;                      // rows before the call; -1: nothing is appended
+  int32_t start;                    // the view's first page among those taken
+  int32_t from;                     // the shared last page that is copied, or -1
+};
+
+struct PagedAppend {
+  PagedCache c;
+  const PagedSeq* seqs;
+  const int32_t* tok_seq;           // sequence of every token
+  PagedTake* views;                 // [n_seqs * hkv]
+  int32_t* takes;                   // pages taken
+  const char* k_new;
+  const char* v_new;
+  int64_t tok_bytes, head_bytes;    // strides of k_new and v_new
+  int32_t* overflow;
+  int32_t n_seqs, n_tokens;
+};
+hipError_t launch_paged_init(const PagedCache& c, hipStream_t stream);
+hipError_t launch_paged_append(const PagedAppend& a, hipStream_t stream);
+
+struct PagedFork {
+  PagedCache c;
+  int32_t* refused;
+  int32_t n;
+  int32_t src[kPagedMaxList], dst[kPagedMaxList];
+};
+hipError_t launch_paged_fork(const PagedFork& a, hipStream_t stream);
+hipError_t launch_paged_drop(const PagedCache& c, const int64_t* rows, hipStream_t stream);
+
+struct PagedCompact {
+  PagedCache c;
+  const int32_t* idx;
+  int32_t* offs;                    // [n_sel][b] first row of every listed chunk among the view's new rows
+  PagedTake* views;                 // [n_sel]; from: the view's new rows
+  int32_t* takes;
+  int32_t* overflow;
+  int32_t slot, n_sel, b, cs, tail;
+  int32_t heads[kPagedMaxHeads];
+};
+hipError_t launch_paged_compact(const PagedCompact& a, hipStream_t stream);
+
+struct PagedGather {
+  PagedCache c;
+  const catekv_kv_ptrs* out;
+  int64_t max_rows;
+  int32_t n;
+  int32_t slots[kPagedMaxList];
+};
+constexpr int kGatherThreads = 256;
+int64_t paged_gather_groups(int64_t max_rows, int row_bytes);   // workgroups per view
+hipError_t launch_paged_gather(const PagedGather& a, hipStream_t stream);
+
+// ---- attention -----------------------------------------------------------------
+// New rows of a sequence in one view's group: row = token * G + head of the group.
+// A piece of work: new rows [row0, row0 + R) over the cached rows [t0, t1) of a view.
+struct PagedPiece {
+  int32_t view;                     // slot * hkv + head
+  int32_t tok0, n_new;              // of the sequence
+  int32_t row0;
+  int32_t t0, t1;
+  int32_t max_rows;                 // planned rows of the view
+  int32_t slot;                     // partial slot at that many 16-byte units, or -1: the rows' only piece
+};
+// New rows whose pieces are joined: n_parts slots of `rows` rows, one behind the other.
+struct PagedJoin {
+  int32_t view, tok0, n_new, row0;
+  int32_t slot, n_parts, rows, pad;
+};
+// A partial slot of R rows: o [R][128], then m [R] and l [R]: o = sum exp2(s - m) v and
+// l = sum exp2(s - m) of the scaled scores s in units of log2; m = -inf: no row.
+constexpr size_t paged_slot_floats(int R) { return (size_t)R * (kD + 2); }
+
+constexpr int kStreamRows = 16;     // new rows of a stream piece at most (the 16 columns of an MFMA)
+constexpr int kPagedUnit = 64;      // pieces begin at multiples of so many cached rows
+
+struct PagedAttn {
+  PagedCache c;
+  const char* q;
+  char* out;
+  float* lse;
+  const PagedPiece* pieces;         // tile pieces, or the stream workers' segments
+  const int32_t* workers;           // stream: first segment of every worker
+  const PagedJoin* joins;
+  float* slots;
+  int32_t n;                        // tile pieces, or stream workers
+  int32_t n_joins, join_rows;       // joins, and the most rows of one
+  int32_t hq;
+  float scale;
+};
+constexpr int kTileThreads = 512;        // of a workgroup of either, at most
+constexpr int kJoinThreads = 256;
+constexpr int kJoinRows = kJoinThreads / 32;   // rows of a joining workgroup
+int paged_tile_rows(int dtype);     // new rows of a tile piece at most
+hipError_t launch_paged_tile(int dtype, int G, const PagedAttn& a, hipStream_t stream);
+hipError_t launch_paged_stream(int dtype, int G, const PagedAttn& a, hipStream_t stream);
+hipError_t launch_paged_join(int dtype, int G, const PagedAttn& a, hipStream_t stream);
+
+}  // namespace catekv

@@ -1,0 +1,86 @@
+// What the attention kernels over pages share (gfx950).
+#pragma once
+
+#include "common.h"
+#include "paged.h"
+
+namespace catekv {
+
+typedef float pg_f32x2 __attribute__((ext_vector_type(2)));
+typedef float pg_f32x4 __attribute__((ext_vector_type(4)));
+typedef float pg_f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 pg_bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 pg_bf16x8 __attribute__((ext_vector_type(8)));
+typedef short pg_s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLn2 = 0.6931471805599453f;
+
+// exp2(s c - m c) with m c rounded is off by a factor that all of a row's weights share
+// and that its sum takes out again, up to 2^(|m c| 2^-24): from here on weights are
+// exp2((s - m) c), so that equal scores of any size weigh the same.
+constexpr float kPgBig = 4194304.f;
+
+// bf16 pair (to nearest, ties to even) of two fp32 values, x in the low half.
+__device__ __forceinline__ uint32_t pg_pack2(float x, float y) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((pg_f32x2{x, y}), pg_bf16x2));
+}
+__device__ __forceinline__ void pg_put4(uint16_t*, char* p, float a, float b, float c, float d) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pg_pack2(a, b), pg_pack2(c, d));
+}
+__device__ __forceinline__ void pg_put4(float*, char* p, float a, float b, float c, float d) {
+  *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+}
+
+// fp32 queries are scaled on their way in (one rounding of 2^-24 more; a product q k
+// that only fits fp32 with the scale in it does); bf16 ones enter their products as they
+// are, and the scores are scaled.
+__device__ __forceinline__ uint4 pg_scale_q(const float*, uint4 q, float scale) {
+  return make_uint4(__float_as_uint(__uint_as_float(q.x) * scale), __float_as_uint(__uint_as_float(q.y) * scale),
+                    __float_as_uint(__uint_as_float(q.z) * scale), __float_as_uint(__uint_as_float(q.w) * scale));
+}
+__device__ __forceinline__ uint4 pg_scale_q(const uint16_t*, uint4 q, float) { return q; }
+template <typename T>
+__device__ __forceinline__ float pg_log2_scale(float scale) { return sizeof(T) == 4 ? kLog2e : scale * kLog2e; }
+
+// Rows of a view as attention takes them: none if its length is out of range, and
+// no more than were planned for.
+__device__ __forceinline__ int pg_rows(const PagedCache& c, int view, int max_rows) {
+  const int64_t len = c.lens[view], cap = (int64_t)c.max_pages << c.page_log;
+  return len < 0 || len > cap ? 0 : (int)min(len, (int64_t)max_rows);
+}
+__device__ __forceinline__ size_t pg_page(const PagedCache& c, int id) {
+  return (size_t)((uint32_t)id < (uint32_t)c.n_pages ? id : 0) << c.page_log;
+}
+
+// A table's entry, the same for all lanes, through the scalar cache: its wait is its own,
+// and not one for every vector load issued before it.
+__device__ __forceinline__ int pg_entry(const int32_t* ids, int p) {
+  const uint64_t at = reinterpret_cast<uint64_t>(ids + p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
+  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>((uint64_t)hi << 32 | lo);
+}
+
+// ---- V that is not finite where some of the tokens do not see it -----------------
+// 0 * NaN and 0 * inf are NaN: such values are taken as 0 in the product, and counted
+// for the tokens that see them in a second one, by a code each: 1, 2^7 and 2^14 for
+// +inf, -inf and NaN (exact in bf16 and, for up to 127 rows, in the sum).
+__device__ __forceinline__ bool pg_bad16(uint32_t x) { return (x & 0x7f80u) == 0x7f80u; }
+__device__ __forceinline__ uint32_t pg_code16(uint32_t x) {
+  return !pg_bad16(x) ? 0u : (x & 0x7fu) ? 0x4680u : (x & 0x8000u) ? 0x4300u : 0x3f80u;
+}
+__device__ __forceinline__ uint32_t pg_clean16(uint32_t x) { return pg_bad16(x) ? 0u : x; }
+// f of both halves of a word
+template <class F>
+__device__ __forceinline__ uint32_t pg_both(uint32_t w, F f) { return f(w & 0xffffu) | (uint32_t)f(w >> 16) << 16; }
+__device__ __forceinline__ bool pg_bad32(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ float pg_code32(float v) {
+  const uint32_t x = __float_as_uint(v);
+  return !pg_bad32(v) ? 0.f : (x & 0x7fffffu) ? 16384.f : (x >> 31) ? 128.f : 1.f;
+}
+// What a count adds to a sum.
+__device__ __forceinline__ float pg_of_codes(float n) {
+  const uint32_t k = (uint32_t)n;
+  return !k ? 0.f : (k >> 14) || ((k & 127) && (k >> 7 & 127)) ? NAN : (k & 127) ? INFINITY : -INFINITY;
+}
+
+}  // namespace catekv

@@ -1,0 +1,375 @@
+// Attention of few new tokens (up to 16 rows: tokens x heads of a group) over caches
+// in pages (gfx950): bound by reading K and V once.
+//
+// All views are laid end to end and cut into equal shares, one per workgroup of 8
+// waves, one workgroup per compute unit.  A wave streams tiles of 16 cached rows (a
+// page holds whole ones) through two stages of registers, also from one segment into
+// the next; the page number of the tile after the next is on its way meanwhile.
+// Scores are S^T = K Q^T: lane l holds row l % 16 of the new ones and cached rows
+// 4 (l / 16) + i, which is how O^T = V^T P^T takes P; what belongs to a new row
+// (maximum, sum, factor) is a lane's own.  V^T's rows are the 8 dims that a lane
+// loaded of each cached row, one product per dim.
+#include <type_traits>
+
+#include "paged_math.h"
+
+namespace catekv {
+namespace {
+
+constexpr int kWaves = 8;
+constexpr int kThreads = kWaves * 64;
+constexpr int kBatch = 8;                 // segments described in LDS at a time
+constexpr int R = kStreamRows;
+constexpr int kTile = 16;
+constexpr int kPad = kD + 4;
+
+template <typename T> struct Ops;
+
+template <> struct Ops<uint16_t> {
+  static constexpr int kK = 4, kV = 4;    // 16-byte registers of a tile, K and V each
+  static __device__ __forceinline__ int v_chunk(int, int n16) { return n16; }
+  static constexpr int kVPer = 1;         // registers per cached row of V
+  static __device__ __forceinline__ pg_f32x4 score(const uint4 (&k)[kK], const uint4 (&q)[kK]) {
+    pg_f32x4 s = {};
+#pragma unroll
+    for (int i = 0; i < kK; ++i)
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pg_bf16x8, k[i]), __builtin_bit_cast(pg_bf16x8, q[i]), s, 0, 0, 0);
+    return s;
+  }
+  // element e of the four rows
+  static __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+  static __device__ __forceinline__ uint2 column(const uint4 (&v)[kV], int e) {
+    const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
+    return make_uint2(__builtin_amdgcn_perm(word(v[1], e / 2), word(v[0], e / 2), sel),
+                      __builtin_amdgcn_perm(word(v[3], e / 2), word(v[2], e / 2), sel));
+  }
+  static __device__ __forceinline__ pg_f32x4 mul(uint2 v, uint2 p, pg_f32x4 o) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(pg_s16x4, v), __builtin_bit_cast(pg_s16x4, p), o, 0, 0, 0);
+  }
+  // the weights in two parts, 16 bits of them in all: p = hi + lo
+  static __device__ __forceinline__ void split(const pg_f32x4& p, uint2& hi, uint2& lo) {
+    hi = make_uint2(pg_pack2(p[0], p[1]), pg_pack2(p[2], p[3]));
+    lo = make_uint2(pg_pack2(p[0] - bf16_lo(hi.x), p[1] - bf16_hi(hi.x)), pg_pack2(p[2] - bf16_lo(hi.y), p[3] - bf16_hi(hi.y)));
+  }
+  static __device__ __forceinline__ void pv(const uint4 (&v)[kV], const pg_f32x4& p, pg_f32x4 (&o)[8]) {
+    uint2 hi, lo;
+    split(p, hi, lo);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint2 c = column(v, e);
+      o[e] = mul(c, lo, mul(c, hi, o[e]));
+    }
+  }
+  static __device__ __forceinline__ bool any_bad(const uint4 (&v)[kV]) {
+    uint32_t b = 0;
+#pragma unroll
+    for (int r = 0; r < kV; ++r)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) b |= pg_both(word(v[r], i), [](uint32_t x) { return (uint32_t)pg_bad16(x); });
+    return b != 0;
+  }
+  static __device__ __forceinline__ void pv_clean(const uint4 (&v)[kV], const pg_f32x4& p, const pg_f32x4& seen, pg_f32x4 (&o)[8]) {
+    uint2 hi, lo;
+    split(p, hi, lo);
+    const uint2 one = make_uint2(pg_pack2(seen[0], seen[1]), pg_pack2(seen[2], seen[3]));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint2 c = column(v, e);
+      const uint2 f = make_uint2(pg_both(c.x, pg_clean16), pg_both(c.y, pg_clean16));
+      const uint2 b = make_uint2(pg_both(c.x, pg_code16), pg_both(c.y, pg_code16));
+      o[e] = mul(f, lo, mul(f, hi, o[e]));
+      const pg_f32x4 n = mul(b, one, pg_f32x4{});
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[e][i] += pg_of_codes(n[i]);
+    }
+  }
+  // dims of o[4 x .. 4 x + 3][i]
+  static __device__ __forceinline__ int dim(int x, int k4, int i) { return 8 * (4 * k4 + i) + 4 * x; }
+};
+
+template <> struct Ops<float> {
+  static constexpr int kK = 8, kV = 8;
+  static constexpr int kVPer = 2;
+  static __device__ __forceinline__ int v_chunk(int x, int n16) { return n16 + 16 * x; }
+  static __device__ __forceinline__ float el(const uint4& v, int i) {
+    return __uint_as_float(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w);
+  }
+  static __device__ __forceinline__ pg_f32x4 score(const uint4 (&k)[kK], const uint4 (&q)[kK]) {
+    pg_f32x4 s = {};
+#pragma unroll
+    for (int i = 0; i < kK; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(el(k[i], e), el(q[i], e), s, 0, 0, 0);
+    return s;
+  }
+  static __device__ __forceinline__ void pv(const uint4 (&v)[kV], const pg_f32x4& p, pg_f32x4 (&o)[8]) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(el(v[2 * r + e / 4], e & 3), p[r], o[e], 0, 0, 0);
+  }
+  static __device__ __forceinline__ bool any_bad(const uint4 (&v)[kV]) {
+    bool b = false;
+#pragma unroll
+    for (int r = 0; r < kV; ++r)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) b = b || pg_bad32(el(v[r], i));
+    return b;
+  }
+  static __device__ __forceinline__ void pv_clean(const uint4 (&v)[kV], const pg_f32x4& p, const pg_f32x4& seen, pg_f32x4 (&o)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      pg_f32x4 n = {};
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float x = el(v[2 * r + e / 4], e & 3);
+        o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(pg_bad32(x) ? 0.f : x, p[r], o[e], 0, 0, 0);
+        n = __builtin_amdgcn_mfma_f32_16x16x4f32(pg_code32(x), seen[r], n, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[e][i] += pg_of_codes(n[i]);
+    }
+  }
+  static __device__ __forceinline__ int dim(int x, int k4, int i) { return 4 * (4 * k4 + i) + 64 * x; }
+};
+
+// A segment as the waves read it.
+struct Seg {
+  int32_t view, t0, t_end, n_units;
+  int32_t see0;                           // cached rows that the first new token sees
+  int32_t rows;                           // new rows
+  int32_t q0;                             // their first (token, head) row: tok0 * hq + head * G
+  int32_t slot;
+};
+
+template <typename T, int G>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void paged_stream_kernel(PagedAttn a) {
+  using X = Ops<T>;
+  constexpr int RB = kD * (int)sizeof(T);
+  __shared__ Seg s_seg[kBatch];
+  __shared__ uint4 s_q[kBatch][R][RB / 16];
+  __shared__ float s_o[kWaves][R][kPad];
+  __shared__ float s_m[kWaves][R], s_l[kWaves][R];
+  const PagedCache& c = a.c;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n16 = lane & 15, k4 = lane >> 4;
+  const float cs = pg_log2_scale<T>(a.scale), thr = 8.0f / cs;
+  const int mask = (1 << c.page_log) - 1;
+  const int first = a.workers[blockIdx.x], last = a.workers[blockIdx.x + 1];
+
+  for (int s0 = first; s0 < last; s0 += kBatch) {
+    const int nseg = min(last - s0, kBatch);
+    __syncthreads();                                  // the batch before is done
+    if ((int)threadIdx.x < nseg) {
+      const PagedPiece p = a.pieces[s0 + threadIdx.x];
+      const int L = pg_rows(c, p.view, p.max_rows);
+      Seg s;
+      s.view = p.view;
+      s.t0 = p.t0;
+      s.t_end = min(p.t1, L);
+      s.n_units = s.t_end > p.t0 ? (s.t_end - p.t0 + kTile - 1) / kTile : 0;
+      s.see0 = L - p.n_new + 1;
+      s.rows = p.n_new * G;
+      s.q0 = p.tok0 * a.hq + (p.view % c.hkv) * G;
+      s.slot = p.slot;
+      s_seg[threadIdx.x] = s;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < nseg * R * (RB / 16); i += kThreads) {
+      const int sg = i / (R * (RB / 16)), x = i - sg * (R * (RB / 16)), r = x / (RB / 16), ch = x - r * (RB / 16);
+      const int tok = r / G;
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (r < s_seg[sg].rows) v = ldg16(a.q + ((size_t)s_seg[sg].q0 + (size_t)tok * a.hq + (r - tok * G)) * RB + ch * 16);
+      v = pg_scale_q((const T*)nullptr, v, a.scale);
+      s_q[sg][r][ch] = v;
+    }
+    __syncthreads();
+
+    // ---- this wave's tiles: those of number wave, wave + 8, ... of every segment ----
+    int is = 0, iu = wave;                            // next tile to load
+    auto skip = [&]() {
+      while (is < nseg && iu >= s_seg[is].n_units) {
+        ++is;
+        iu = wave;
+      }
+    };
+    skip();
+    int next_id = 0;
+    auto fetch_id = [&]() {                           // the page number of that tile
+      if (is < nseg) {
+        const int t = s_seg[is].t0 + iu * kTile;
+        next_id = pg_entry(c.table + (size_t)s_seg[is].view * c.max_pages, t >> c.page_log);
+      }
+    };
+    fetch_id();
+    uint4 kb[2][X::kK], vb[2][X::kV];
+    int seg_of[2] = {kBatch, kBatch}, tile_of[2] = {0, 0};
+    auto issue = [&](auto tag) {
+      constexpr int B = decltype(tag)::value;
+      if (is >= nseg) {
+        seg_of[B] = kBatch;
+        return;
+      }
+      const int tile = s_seg[is].t0 + iu * kTile, rows = s_seg[is].t_end - tile;   // at least one row
+      const size_t base = (pg_page(c, next_id) + (tile & mask)) * RB;
+      const char* kr = c.k + base + (size_t)min(n16, rows - 1) * RB + k4 * 16;
+#pragma unroll
+      for (int i = 0; i < X::kK; ++i) kb[B][i] = once16(kr + i * 64);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const char* vr = c.v + base + (size_t)min(4 * k4 + r, rows - 1) * RB;
+#pragma unroll
+        for (int x = 0; x < X::kVPer; ++x) vb[B][r * X::kVPer + x] = once16(vr + X::v_chunk(x, n16) * 16);
+      }
+      seg_of[B] = is;
+      tile_of[B] = tile;
+      iu += kWaves;
+      skip();
+      fetch_id();
+    };
+
+    uint4 q[X::kK];
+    pg_f32x4 o[8];
+    float m, l;
+    bool big;                                         // in the wave: kPgBig
+    int cur = 0;
+    auto begin = [&]() {
+      m = -INFINITY;
+      l = 0.f;
+      big = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = pg_f32x4{};
+#pragma unroll
+      for (int i = 0; i < X::kK; ++i) q[i] = s_q[cur][n16][i * 4 + k4];
+    };
+    auto consume = [&](auto tag) {
+      constexpr int B = decltype(tag)::value;
+      const Seg& sg = s_seg[cur];
+      const int tile = tile_of[B];
+      pg_f32x4 s = X::score(kb[B], q);
+      const bool masked = tile + kTile > sg.see0;       // the first token does not see all of it
+      const int see = min(sg.see0 + n16 / G, sg.t_end);
+      pg_f32x4 seen = {1.f, 1.f, 1.f, 1.f};
+      if (masked) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int t = tile + 4 * k4 + r;
+          s[r] = t < see ? s[r] : -INFINITY;
+          seen[r] = t < see ? 1.f : 0.f;
+          if (t >= sg.t_end)
+#pragma unroll
+            for (int x = 0; x < X::kVPer; ++x) vb[B][r * X::kVPer + x] = make_uint4(0, 0, 0, 0);
+        }
+      }
+      float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+      mx = max_xor32(max_xor16(mx));
+      if (__builtin_amdgcn_ballot_w64(mx > m && !(mx <= m + thr))) {
+        const float corr = mx > m ? fast_exp2((m - mx) * cs) : 1.f;
+        m = fmaxf(m, mx);
+        big = __builtin_amdgcn_ballot_w64(fabsf(m) * cs > kPgBig && m != -INFINITY) != 0;
+        l *= corr;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[e][i] *= corr;
+      }
+      const float m0 = m == -INFINITY ? 0.f : m, mc = m0 * cs;
+      pg_f32x4 p;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        p[r] = big ? fast_exp2((s[r] - m0) * cs) : fast_exp2(__builtin_fmaf(s[r], cs, -mc));
+        l += p[r];
+      }
+      if (masked && __builtin_amdgcn_ballot_w64(X::any_bad(vb[B]))) X::pv_clean(vb[B], p, seen, o);
+      else X::pv(vb[B], p, o);
+    };
+    // The waves' parts of segment cur joined; its result or partial slot written.
+    auto finish = [&]() {
+      l = add_xor32(add_xor16(l));
+      barrier_lds_only();                             // the join before has been read
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<float4*>(&s_o[wave][n16][X::dim(x, k4, i)]) =
+              make_float4(o[4 * x][i], o[4 * x + 1][i], o[4 * x + 2][i], o[4 * x + 3][i]);
+      if (k4 == 0) {
+        s_m[wave][n16] = m == -INFINITY ? -INFINITY : m * cs;
+        s_l[wave][n16] = l;
+      }
+      barrier_lds_only();
+      const Seg sg = s_seg[cur];
+      for (int t = threadIdx.x; t < sg.rows * (kD / 4); t += kThreads) {
+        const int r = t / (kD / 4), d = (t - r * (kD / 4)) * 4;
+        float M = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][r]);
+        float sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          const float mw = s_m[w][r];
+          const float f = mw == -INFINITY ? 0.f : fast_exp2(mw - M);
+          const float4 v = *reinterpret_cast<const float4*>(&s_o[w][r][d]);
+          if (mw == -INFINITY) continue;
+          sum += f * s_l[w][r];
+          x[0] += f * v.x;
+          x[1] += f * v.y;
+          x[2] += f * v.z;
+          x[3] += f * v.w;
+        }
+        if (sg.slot >= 0) {
+          float* slot = a.slots + (size_t)sg.slot * 4;
+          *reinterpret_cast<float4*>(slot + r * kD + d) = make_float4(x[0], x[1], x[2], x[3]);
+          if (d == 0) {
+            slot[R * kD + r] = M;
+            slot[R * (kD + 1) + r] = sum;
+          }
+        } else {
+          const bool none = M == -INFINITY;
+          const float inv = none ? 0.f : 1.f / sum;
+          const int tok = r / G;
+          const size_t row = (size_t)sg.q0 + (size_t)tok * a.hq + (r - tok * G);
+          pg_put4((T*)nullptr, a.out + (row * kD + d) * sizeof(T), x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+          if (a.lse && d == 0) a.lse[row] = none ? -INFINITY : (M + __builtin_amdgcn_logf(sum)) * kLn2;
+        }
+      }
+    };
+    auto turn = [&](auto tag) {                       // uses the tile in a stage and fills it again
+      constexpr int B = decltype(tag)::value;
+      while (cur < seg_of[B] && cur < nseg) {
+        finish();
+        if (++cur < nseg) begin();
+      }
+      if (seg_of[B] >= nseg) return false;
+      consume(tag);
+      issue(tag);
+      return true;
+    };
+    using B0 = std::integral_constant<int, 0>;
+    using B1 = std::integral_constant<int, 1>;
+    issue(B0{});
+    issue(B1{});
+    begin();
+    while (turn(B0{}) && turn(B1{})) {
+    }
+  }
+}
+
+template <typename T, int G>
+hipError_t stream_tg(const PagedAttn& a, hipStream_t stream) {
+  paged_stream_kernel<T, G><<<a.n, kThreads, 0, stream>>>(a);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t stream_t(int G, const PagedAttn& a, hipStream_t s) {
+  return G == 1 ? stream_tg<T, 1>(a, s) : G == 2 ? stream_tg<T, 2>(a, s) : G == 4 ? stream_tg<T, 4>(a, s) : stream_tg<T, 8>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_paged_stream(int dtype, int G, const PagedAttn& a, hipStream_t stream) {
+  return dtype == CATEKV_BF16 ? stream_t<uint16_t>(G, a, stream) : stream_t<float>(G, a, stream);
+}
+
+}  // namespace catekv
