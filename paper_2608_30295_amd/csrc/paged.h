@@ -117,16 +117,17 @@ struct PagedAttn {
   const PagedJoin* joins;
   float* slots;
   int32_t n;                        // tile pieces, or stream workers
-  int32_t n_joins, join_rows;       // joins, and the most rows of one
   int32_t hq;
   float scale;
 };
 constexpr int kTileThreads = 512;        // of a workgroup of either, at most
 constexpr int kJoinThreads = 256;
-constexpr int kJoinRows = kJoinThreads / 32;   // rows of a joining workgroup
+constexpr int kJoinRows = kJoinThreads / 32;   // rows of a joining workgroup, where rows have few parts
+inline int paged_join_rows(int parts) { return parts > 4 ? 1 : kJoinRows; }
 int paged_tile_rows(int dtype);     // new rows of a tile piece at most
 hipError_t launch_paged_tile(int dtype, int G, const PagedAttn& a, hipStream_t stream);
 hipError_t launch_paged_stream(int dtype, int G, const PagedAttn& a, hipStream_t stream);
-hipError_t launch_paged_join(int dtype, int G, const PagedAttn& a, hipStream_t stream);
+// Joins first ... first + n - 1 of the plan's: rows and parts, the most of any of them.
+hipError_t launch_paged_join(int dtype, int G, const PagedAttn& a, int first, int n, int rows, int parts, hipStream_t stream);
 
 }  // namespace catekv

@@ -101,7 +101,8 @@ struct Plan {
   std::vector<int32_t> workers;     // the first of every worker
   std::vector<PagedJoin> joins;
   int64_t slot16 = 0;               // 16-byte units of partial slots
-  int join_rows = 0;
+  int tile_joins = 0;               // joins of tiles, which come first
+  int tile_parts = 0, few_parts = 0;   // the most parts of one join
   size_t seqs_off = 0, toks_off = 0, views_off = 0, takes_off = 0, tiles_off = 0, segs_off = 0, workers_off = 0, joins_off = 0, slots_off = 0, total = 0;
 };
 
@@ -157,7 +158,8 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
   auto join = [&](const PagedPiece& p, int64_t parts, int rows) {    // slots for the parts of p
     if (parts < 2) return;
     P.joins.push_back({p.view, p.tok0, p.n_new, p.row0, (int32_t)P.slot16, (int32_t)parts, rows, 0});
-    P.join_rows = std::max(P.join_rows, rows);
+    int& most = rows == kStreamRows ? P.few_parts : P.tile_parts;
+    most = std::max(most, (int)parts);
     P.slot16 += parts * (int64_t)(paged_slot_floats(rows) / 4);
   };
   int64_t tile_units = 0, n_tiles = 0, few_units = 0;
@@ -190,6 +192,8 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
       }
   std::stable_sort(P.tiles.begin(), P.tiles.end(),
                    [](const PagedPiece& x, const PagedPiece& y) { return x.t1 - x.t0 > y.t1 - y.t0; });
+
+  P.tile_joins = (int)P.joins.size();
 
   // the rest laid end to end and cut into equal shares, one per workgroup
   if (few_units > 0) {
@@ -228,7 +232,7 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
     P.workers.push_back((int32_t)P.segs.size());
   }
   if (!launch_fits((int64_t)P.tiles.size(), kTileThreads) ||
-      !launch_fits((int64_t)P.joins.size() * ((P.join_rows + kJoinRows - 1) / kJoinRows), kJoinThreads))
+      !launch_fits((int64_t)P.joins.size() * std::max(R, kStreamRows), kJoinThreads))
     return fail(CATEKV_ERR_UNSUPPORTED, "%zu pieces of work: too many for one launch", P.tiles.size());
 
   size_t at = 0;
@@ -350,7 +354,9 @@ int catekv_paged_plan(const catekv_paged_cache* cache, const int32_t* slots_host
     plan->n_tile = (int32_t)P.tiles.size();
     plan->n_workers = P.workers.empty() ? 0 : (int32_t)P.workers.size() - 1;
     plan->n_joins = (int32_t)P.joins.size();
-    plan->join_rows = P.join_rows;
+    plan->tile_joins = P.tile_joins;
+    plan->tile_parts = P.tile_parts;
+    plan->few_parts = P.few_parts;
     plan->seqs_off = P.seqs_off;
     plan->toks_off = P.toks_off;
     plan->tiles_off = P.tiles_off;
@@ -411,8 +417,6 @@ int catekv_paged_attn(const catekv_paged_cache* cache, const catekv_paged_plan_t
   a.lse = lse;
   a.joins = reinterpret_cast<const PagedJoin*>(w + plan->joins_off);
   a.slots = reinterpret_cast<float*>(w + plan->slots_off);
-  a.n_joins = plan->n_joins;
-  a.join_rows = plan->join_rows;
   a.hq = plan->hq;
   a.scale = scale;
   const int G = plan->hq / plan->hkv;
@@ -431,10 +435,10 @@ int catekv_paged_attn(const catekv_paged_cache* cache, const catekv_paged_plan_t
     e = launch_paged_stream(cache->dtype, G, a, s);
     if (e != hipSuccess) return hip_fail(e, "paged_attn stream launch");
   }
-  if (plan->n_joins > 0) {
-    e = launch_paged_join(cache->dtype, G, a, s);
-    if (e != hipSuccess) return hip_fail(e, "paged_attn join launch");
-  }
+  e = launch_paged_join(cache->dtype, G, a, 0, plan->tile_joins, paged_tile_rows(cache->dtype), plan->tile_parts, s);
+  if (e == hipSuccess)
+    e = launch_paged_join(cache->dtype, G, a, plan->tile_joins, plan->n_joins - plan->tile_joins, kStreamRows, plan->few_parts, s);
+  if (e != hipSuccess) return hip_fail(e, "paged_attn join launch");
   return host_ok();
 }
 

@@ -204,13 +204,9 @@ void paged_stream_kernel(PagedAttn a) {
     };
     fetch_id();
     uint4 kb[2][X::kK], vb[2][X::kV];
-    int seg_of[2] = {kBatch, kBatch}, tile_of[2] = {0, 0};
-    auto issue = [&](auto tag) {
+    int seg_of[2] = {0, 0}, tile_of[2] = {0, 0};
+    auto issue = [&](auto tag) {                      // the next tile; there is one
       constexpr int B = decltype(tag)::value;
-      if (is >= nseg) {
-        seg_of[B] = kBatch;
-        return;
-      }
       const int tile = s_seg[is].t0 + iu * kTile, rows = s_seg[is].t_end - tile;   // at least one row
       const size_t base = (pg_page(c, next_id) + (tile & mask)) * RB;
       const char* kr = c.k + base + (size_t)min(n16, rows - 1) * RB + k4 * 16;
@@ -335,23 +331,45 @@ void paged_stream_kernel(PagedAttn a) {
         }
       }
     };
-    auto turn = [&](auto tag) {                       // uses the tile in a stage and fills it again
-      constexpr int B = decltype(tag)::value;
-      while (cur < seg_of[B] && cur < nseg) {
+    auto use = [&](auto tag) {
+      while (cur < seg_of[decltype(tag)::value]) {
         finish();
-        if (++cur < nseg) begin();
+        ++cur;
+        begin();
       }
-      if (seg_of[B] >= nseg) return false;
       consume(tag);
-      issue(tag);
-      return true;
     };
     using B0 = std::integral_constant<int, 0>;
     using B1 = std::integral_constant<int, 1>;
-    issue(B0{});
-    issue(B1{});
+    int n = 0;
+    for (int i = 0; i < nseg; ++i) n += max(0, (s_seg[i].n_units - wave + kWaves - 1) / kWaves);
+    n = __builtin_amdgcn_readfirstlane(n);
     begin();
-    while (turn(B0{}) && turn(B1{})) {
+    // Two tiles are on their way at the loop's head, and every turn asks for as many as
+    // it uses: a wait for one tile is then never one for the other, too.
+    if (n > 0) issue(B0{});
+    if (n > 1) issue(B1{});
+    for (; n >= 4; n -= 2) {
+      use(B0{});
+      issue(B0{});
+      use(B1{});
+      issue(B1{});
+    }
+    for (; n > 0; --n) {
+      use(B0{});
+      if (n == 1) break;
+#pragma unroll
+      for (int i = 0; i < X::kK; ++i) kb[0][i] = kb[1][i];
+#pragma unroll
+      for (int i = 0; i < X::kV; ++i) vb[0][i] = vb[1][i];
+      seg_of[0] = seg_of[1];
+      tile_of[0] = tile_of[1];
+      if (n == 3) issue(B1{});
+    }
+    for (;;) {
+      finish();
+      if (++cur == nseg) break;
+      begin();
     }
   }
 }
