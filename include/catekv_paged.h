@@ -57,7 +57,7 @@ typedef struct catekv_paged_plan_t {
   uint64_t magic;
   int32_t n_seqs, n_tokens, hq, hkv, n_slots, page, dtype;
   int32_t n_tile, n_workers, n_joins, tile_joins, tile_parts, few_parts, reserved;
-  uint64_t seqs_off, toks_off, tiles_off, segs_off, workers_off, joins_off, views_off, takes_off, slots_off, ws_bytes;
+  uint64_t seqs_off, toks_off, tiles_off, tile_workers_off, segs_off, workers_off, joins_off, views_off, takes_off, slots_off, ws_bytes;
 } catekv_paged_plan_t;
 
 /* An empty cache: lens 0, table -1, refs 0, every page free.  k and v stay as

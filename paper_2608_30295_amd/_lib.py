@@ -102,7 +102,7 @@ class PagedPlanT(ctypes.Structure):
     _fields_ = [("magic", ctypes.c_uint64)] + [
         (n, ctypes.c_int32) for n in ("n_seqs", "n_tokens", "hq", "hkv", "n_slots", "page", "dtype", "n_tile",
                                       "n_workers", "n_joins", "tile_joins", "tile_parts", "few_parts", "reserved")] + [
-        (n, ctypes.c_uint64) for n in ("seqs_off", "toks_off", "tiles_off", "segs_off", "workers_off", "joins_off",
+        (n, ctypes.c_uint64) for n in ("seqs_off", "toks_off", "tiles_off", "tile_workers_off", "segs_off", "workers_off", "joins_off",
                                        "views_off", "takes_off", "slots_off", "ws_bytes")]
 
 

@@ -20,7 +20,7 @@ ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
 HIP_SOURCES = ["decode.hip", "prefill.hip", "retrieve.hip", "score_rowstats.hip", "score_colmass.hip", "score_obs.hip", "score_obsb.hip", "cv.hip",
                "q8.hip", "attend_dense.hip", "attend_i8.hip", "attend_e4m3.hip", "evict.hip",
-               "paged_pages.hip", "paged_tile.hip", "paged_stream.hip"]
+               "paged_pages.hip", "paged_tile.hip", "paged_tile_f32.hip", "paged_stream.hip", "paged_join.hip"]
 HOST_SOURCES = ["api.cpp", "cache_api.cpp", "paged_api.cpp"]
 
 # Packed fp32 ops are kept out of the device code: hipcc only emits them when

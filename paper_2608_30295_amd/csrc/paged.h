@@ -112,20 +112,25 @@ struct PagedAttn {
   const char* q;
   char* out;
   float* lse;
-  const PagedPiece* pieces;         // tile pieces, or the stream workers' segments
-  const int32_t* workers;           // stream: first segment of every worker
+  const PagedPiece* pieces;         // by worker, and
+  const int32_t* workers;           // the first of every worker
   const PagedJoin* joins;
   float* slots;
-  int32_t n;                        // tile pieces, or stream workers
+  int32_t n;                        // workers
   int32_t hq;
   float scale;
+  float log2_scale;                 // of the scores as the products give them, to units of log2
+  float rise;                       // by how much a maximum grows before it is moved: 8 / log2_scale
 };
-constexpr int kTileThreads = 512;        // of a workgroup of either, at most
+constexpr int kTileThreads = 512;        // bf16; fp32: 256
 constexpr int kJoinThreads = 256;
 constexpr int kJoinRows = kJoinThreads / 32;   // rows of a joining workgroup, where rows have few parts
 inline int paged_join_rows(int parts) { return parts > 4 ? 1 : kJoinRows; }
-int paged_tile_rows(int dtype);     // new rows of a tile piece at most
-hipError_t launch_paged_tile(int dtype, int G, const PagedAttn& a, hipStream_t stream);
+// New rows of a tile piece at most, and the launch, per type.
+constexpr int kTileRows = 256, kTileRowsF32 = 128;
+inline int paged_tile_rows(int dtype) { return dtype == CATEKV_BF16 ? kTileRows : kTileRowsF32; }
+hipError_t launch_paged_tile(int G, const PagedAttn& a, hipStream_t stream);       // bf16
+hipError_t launch_paged_tile_f32(int G, const PagedAttn& a, hipStream_t stream);
 hipError_t launch_paged_stream(int dtype, int G, const PagedAttn& a, hipStream_t stream);
 // Joins first ... first + n - 1 of the plan's: rows and parts, the most of any of them.
 hipError_t launch_paged_join(int dtype, int G, const PagedAttn& a, int first, int n, int rows, int parts, hipStream_t stream);

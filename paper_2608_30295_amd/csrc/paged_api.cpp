@@ -8,6 +8,9 @@
 #include <cstdio>
 #include <cstring>
 #include <exception>
+#include <functional>
+#include <queue>
+#include <utility>
 #include <vector>
 
 #include "paged.h"
@@ -96,18 +99,85 @@ int device_cus() {
 struct Plan {
   int64_t n_tokens = 0, takes = 0;
   std::vector<PagedSeq> seqs;
-  std::vector<PagedPiece> tiles;    // of many new rows
+  std::vector<PagedPiece> tiles;    // pieces of many new rows, by worker, and
+  std::vector<int32_t> tile_workers;   // the first of every worker
   std::vector<PagedPiece> segs;     // of few: the stream workers' segments, and
   std::vector<int32_t> workers;     // the first of every worker
   std::vector<PagedJoin> joins;
   int64_t slot16 = 0;               // 16-byte units of partial slots
   int tile_joins = 0;               // joins of tiles, which come first
   int tile_parts = 0, few_parts = 0;   // the most parts of one join
-  size_t seqs_off = 0, toks_off = 0, views_off = 0, takes_off = 0, tiles_off = 0, segs_off = 0, workers_off = 0, joins_off = 0, slots_off = 0, total = 0;
+  size_t seqs_off = 0, toks_off = 0, views_off = 0, takes_off = 0, tiles_off = 0, tile_workers_off = 0, segs_off = 0, workers_off = 0, joins_off = 0, slots_off = 0, total = 0;
 };
 
-// A piece's work beside its tiles, in units: the query rows' way in and the results' out.
+// ---- tiles of many new rows --------------------------------------------------------
+// Cut into pieces and dealt out to workgroups, one per compute unit, here: the GPU deals
+// workgroups to its engines in turn and lets one engine's compute units stand idle while
+// another's queue (2048 tokens at 32K in 376 pieces of unequal length: 1280 us where its
+// longest share takes 890).  Costs in units: a piece of u units takes u + kPieceFixed (new
+// rows in, results out); joining takes a launch, and its partial results' way to memory and
+// back, kSlotUnits for each.
 constexpr int64_t kPieceFixed = 4;
+constexpr int64_t kJoinLaunch = 4;
+constexpr double kSlotUnits = 0.04;
+constexpr int kXcds = 8;               // a worker's engine is its number modulo this
+
+struct Tile {
+  PagedPiece p;
+  int64_t rows, units;
+};
+
+struct Deal {
+  int64_t share = 0;                   // most units of a piece; 0: tiles stay whole
+  double cost = 0;
+  std::vector<int> worker;             // of every piece, pieces in order of size
+};
+
+struct Cut {
+  int tile, part, parts;
+  int64_t units;
+};
+
+std::vector<Cut> cut_tiles(const std::vector<Tile>& tiles, int64_t share) {
+  std::vector<Cut> cuts;
+  for (size_t i = 0; i < tiles.size(); ++i) {
+    const int64_t u = tiles[i].units, parts = share ? (u + share - 1) / share : 1;
+    for (int64_t s = 0; s < parts; ++s) cuts.push_back({(int)i, (int)s, (int)parts, u * (s + 1) / parts - u * s / parts});
+  }
+  std::stable_sort(cuts.begin(), cuts.end(), [](const Cut& x, const Cut& y) { return x.units > y.units; });
+  return cuts;
+}
+
+// The longest pieces first, each to the worker with least to do; one of the engine that
+// has the view's other pieces (its cache holds what they read) if that costs little.
+Deal deal(const std::vector<Tile>& tiles, int64_t share, int workers) {
+  Deal d;
+  d.share = share;
+  const std::vector<Cut> cuts = cut_tiles(tiles, share);
+  using Load = std::pair<int64_t, int>;
+  std::vector<std::priority_queue<Load, std::vector<Load>, std::greater<Load>>> engines(kXcds);
+  for (int w = 0; w < workers; ++w) engines[w % kXcds].push({0, w});
+  int64_t total = 0, most = 0;
+  for (const Cut& c : cuts) total += c.units + kPieceFixed;
+  const int64_t slack = total / workers / 64;
+  double slots = 0;
+  for (const Cut& c : cuts) {
+    int best = 0;
+    for (int x = 1; x < kXcds; ++x)
+      if (!engines[x].empty() && (engines[best].empty() || engines[x].top() < engines[best].top())) best = x;
+    const int own = tiles[c.tile].p.view % kXcds;
+    if (!engines[own].empty() && engines[own].top().first <= engines[best].top().first + slack) best = own;
+    const Load l = engines[best].top();
+    engines[best].pop();
+    const int64_t load = l.first + c.units + kPieceFixed;
+    engines[best].push({load, l.second});
+    most = std::max(most, load);
+    d.worker.push_back(l.second);
+    if (c.parts > 1) slots += 1;
+  }
+  d.cost = (double)most + (slots > 0 ? (double)kJoinLaunch + kSlotUnits * slots : 0);
+  return d;
+}
 
 int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t* n_new, const int64_t* max_rows, int n_seqs,
                int hq, Plan& P) {
@@ -171,28 +241,50 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
       }
       for (int64_t r = 0; r < (int64_t)n_new[i] * G; r += R, ++n_tiles) tile_units += units_of(rows_seen(i, h, r, R));
     }
-  if (n_tiles > (int64_t)1 << 24) return fail(CATEKV_ERR_UNSUPPORTED, "%lld tiles of new rows: too many for one launch", (long long)n_tiles);
+  if (n_tiles > (int64_t)1 << 22) return fail(CATEKV_ERR_UNSUPPORTED, "%lld tiles of new rows: too many for one launch", (long long)n_tiles);
 
-  // tiles: whole, or cut so that none takes longer than an equal share; the long ones first
-  const int64_t share = std::max<int64_t>(kPieceFixed, (tile_units + cus - 1) / cus);
-  for (int i = 0; i < n_seqs; ++i)
-    for (int h = 0; n_new[i] > 0 && !few(i) && h < hkv; ++h)
-      for (int64_t r = 0; r < (int64_t)n_new[i] * G; r += R) {
-        const int64_t rows = rows_seen(i, h, r, R), u = units_of(rows), parts = (u + share - 1) / share;
-        const int64_t slot = P.slot16, each = (int64_t)(paged_slot_floats(R) / 4);
-        PagedPiece p = piece(i, h, r);
-        join(p, parts, R);
-        if (P.slot16 > INT32_MAX) return fail(CATEKV_ERR_UNSUPPORTED, "too many partial results");
-        for (int64_t s = 0; s < parts; ++s) {
-          p.t0 = (int32_t)(u * s / parts * kPagedUnit);
-          p.t1 = (int32_t)std::min<int64_t>(rows, u * (s + 1) / parts * kPagedUnit);
-          p.slot = parts > 1 ? (int32_t)(slot + s * each) : -1;
-          P.tiles.push_back(p);
+  // tiles: whole, or cut at some share of the work, whichever is done first
+  if (n_tiles > 0) {
+    std::vector<Tile> tiles;
+    tiles.reserve(n_tiles);
+    for (int i = 0; i < n_seqs; ++i)
+      for (int h = 0; n_new[i] > 0 && !few(i) && h < hkv; ++h)
+        for (int64_t r = 0; r < (int64_t)n_new[i] * G; r += R) {
+          const int64_t rows = rows_seen(i, h, r, R);
+          tiles.push_back({piece(i, h, r), rows, units_of(rows)});
         }
+    Deal best = deal(tiles, 0, cus);
+    const int64_t even = (tile_units + cus - 1) / cus;
+    for (int k = 1; k <= 4 && n_tiles < 8 * (int64_t)cus; ++k) {
+      const int64_t share = std::max<int64_t>(kPieceFixed, (even + k - 1) / k);
+      Deal d = deal(tiles, share, cus);
+      if (d.cost < best.cost) best = std::move(d);
+    }
+    const std::vector<Cut> cuts = cut_tiles(tiles, best.share);
+    std::vector<int64_t> slot(tiles.size(), -1);
+    const int64_t each = (int64_t)(paged_slot_floats(R) / 4);
+    for (const Cut& c : cuts)
+      if (c.parts > 1 && slot[c.tile] < 0) {
+        slot[c.tile] = P.slot16;
+        join(tiles[c.tile].p, c.parts, R);
+        if (P.slot16 > INT32_MAX) return fail(CATEKV_ERR_UNSUPPORTED, "too many partial results");
       }
-  std::stable_sort(P.tiles.begin(), P.tiles.end(),
-                   [](const PagedPiece& x, const PagedPiece& y) { return x.t1 - x.t0 > y.t1 - y.t0; });
-
+    std::vector<size_t> order(cuts.size());
+    for (size_t i = 0; i < order.size(); ++i) order[i] = i;
+    std::stable_sort(order.begin(), order.end(), [&](size_t x, size_t y) { return best.worker[x] < best.worker[y]; });
+    P.tile_workers.assign(1, 0);
+    for (size_t i : order) {
+      const Cut& c = cuts[i];
+      while ((int)P.tile_workers.size() <= best.worker[i]) P.tile_workers.push_back((int32_t)P.tiles.size());
+      const int64_t u = tiles[c.tile].units;
+      PagedPiece p = tiles[c.tile].p;
+      p.t0 = (int32_t)(u * c.part / c.parts * kPagedUnit);
+      p.t1 = (int32_t)std::min<int64_t>(tiles[c.tile].rows, u * (c.part + 1) / c.parts * kPagedUnit);
+      p.slot = c.parts > 1 ? (int32_t)(slot[c.tile] + c.part * each) : -1;
+      P.tiles.push_back(p);
+    }
+    P.tile_workers.push_back((int32_t)P.tiles.size());
+  }
   P.tile_joins = (int)P.joins.size();
 
   // the rest laid end to end and cut into equal shares, one per workgroup
@@ -231,9 +323,8 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
       }
     P.workers.push_back((int32_t)P.segs.size());
   }
-  if (!launch_fits((int64_t)P.tiles.size(), kTileThreads) ||
-      !launch_fits((int64_t)P.joins.size() * std::max(R, kStreamRows), kJoinThreads))
-    return fail(CATEKV_ERR_UNSUPPORTED, "%zu pieces of work: too many for one launch", P.tiles.size());
+  if (!launch_fits((int64_t)P.joins.size() * std::max(R, kStreamRows), kJoinThreads))
+    return fail(CATEKV_ERR_UNSUPPORTED, "%zu views' results to join: too many for one launch", P.joins.size());
 
   size_t at = 0;
   auto put = [&](size_t& off, size_t bytes) {
@@ -243,6 +334,7 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
   put(P.seqs_off, P.seqs.size() * sizeof(PagedSeq));
   put(P.toks_off, (size_t)tokens * sizeof(int32_t));
   put(P.tiles_off, P.tiles.size() * sizeof(PagedPiece));
+  put(P.tile_workers_off, P.tile_workers.size() * sizeof(int32_t));
   put(P.segs_off, P.segs.size() * sizeof(PagedPiece));
   put(P.workers_off, P.workers.size() * sizeof(int32_t));
   put(P.joins_off, P.joins.size() * sizeof(PagedJoin));
@@ -334,6 +426,7 @@ int catekv_paged_plan(const catekv_paged_cache* cache, const int32_t* slots_host
         std::memcpy(host.data() + P.toks_off + ((size_t)P.seqs[i].tok0 + t) * sizeof s, &s, sizeof s);
       }
     copy(P.tiles_off, P.tiles.data(), P.tiles.size() * sizeof(PagedPiece));
+    copy(P.tile_workers_off, P.tile_workers.data(), P.tile_workers.size() * sizeof(int32_t));
     copy(P.segs_off, P.segs.data(), P.segs.size() * sizeof(PagedPiece));
     copy(P.workers_off, P.workers.data(), P.workers.size() * sizeof(int32_t));
     copy(P.joins_off, P.joins.data(), P.joins.size() * sizeof(PagedJoin));
@@ -351,7 +444,7 @@ int catekv_paged_plan(const catekv_paged_cache* cache, const int32_t* slots_host
     plan->n_slots = cache->n_slots;
     plan->page = cache->page;
     plan->dtype = cache->dtype;
-    plan->n_tile = (int32_t)P.tiles.size();
+    plan->n_tile = P.tile_workers.empty() ? 0 : (int32_t)P.tile_workers.size() - 1;
     plan->n_workers = P.workers.empty() ? 0 : (int32_t)P.workers.size() - 1;
     plan->n_joins = (int32_t)P.joins.size();
     plan->tile_joins = P.tile_joins;
@@ -360,6 +453,7 @@ int catekv_paged_plan(const catekv_paged_cache* cache, const int32_t* slots_host
     plan->seqs_off = P.seqs_off;
     plan->toks_off = P.toks_off;
     plan->tiles_off = P.tiles_off;
+    plan->tile_workers_off = P.tile_workers_off;
     plan->segs_off = P.segs_off;
     plan->workers_off = P.workers_off;
     plan->joins_off = P.joins_off;
@@ -419,13 +513,17 @@ int catekv_paged_attn(const catekv_paged_cache* cache, const catekv_paged_plan_t
   a.slots = reinterpret_cast<float*>(w + plan->slots_off);
   a.hq = plan->hq;
   a.scale = scale;
+  // fp32 queries are scaled on their way in, bf16 scores behind their products
+  a.log2_scale = 1.4426950408889634f * (cache->dtype == CATEKV_BF16 ? scale : 1.f);
+  a.rise = 8.f / a.log2_scale;
   const int G = plan->hq / plan->hkv;
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   hipError_t e = hipSuccess;
   if (plan->n_tile > 0) {
     a.pieces = reinterpret_cast<const PagedPiece*>(w + plan->tiles_off);
+    a.workers = reinterpret_cast<const int32_t*>(w + plan->tile_workers_off);
     a.n = plan->n_tile;
-    e = launch_paged_tile(cache->dtype, G, a, s);
+    e = cache->dtype == CATEKV_BF16 ? launch_paged_tile(G, a, s) : launch_paged_tile_f32(G, a, s);
     if (e != hipSuccess) return hip_fail(e, "paged_attn launch");
   }
   if (plan->n_workers > 0) {

@@ -1,0 +1,94 @@
+// Partial results of attention over pages joined (gfx950).
+#include "paged_math.h"
+
+namespace catekv {
+namespace {
+
+// Joins the partial slots of rows that were cut.  A row has 32 lanes per group (4 dims
+// each) and S groups, which take every S-th part; a workgroup has 8 / S rows.
+template <typename T, int G, int S>
+__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedAttn a, int first, int blocks) {
+  constexpr int ROWS = kJoinRows / S;
+  __shared__ float s_x[S][ROWS][kD], s_l[S][ROWS], s_m[S][ROWS];
+  const int ji = blockIdx.x / blocks;
+  const PagedJoin j = a.joins[first + ji];
+  const int lane = threadIdx.x & 31, row = (threadIdx.x >> 5) % ROWS, g = (threadIdx.x >> 5) / ROWS;
+  const int at = (blockIdx.x - ji * blocks) * ROWS + row, r = j.row0 + at;
+  const bool mine = at < j.rows && r < j.n_new * G;
+  const float* slot = a.slots + (size_t)j.slot * 4;
+  const size_t step = paged_slot_floats(j.rows);
+  const float* ms = slot + (size_t)j.rows * kD + (mine ? at : 0);
+  float M = -INFINITY, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+  if (mine) {
+    // the largest of the group's parts, 32 at a time
+    for (int p = g + lane * S; p < j.n_parts; p += 32 * S) M = fmaxf(M, ms[p * step]);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
+#pragma unroll 4
+    for (int p = g; p < j.n_parts; p += S) {
+      const float mp = ms[p * step], lp = ms[p * step + j.rows];
+      const float4 v = *reinterpret_cast<const float4*>(slot + p * step + (size_t)at * kD + lane * 4);
+      const bool some = mp != -INFINITY;               // a part without rows holds zeros
+      const float w = some ? fast_exp2(mp - M) : 0.f;
+      l += w * lp;
+      x[0] += w * v.x;
+      x[1] += w * v.y;
+      x[2] += w * v.z;
+      x[3] += w * v.w;
+    }
+  }
+  if (S > 1) {
+    *reinterpret_cast<float4*>(&s_x[g][row][lane * 4]) = make_float4(x[0], x[1], x[2], x[3]);
+    if (lane == 0) {
+      s_m[g][row] = M;
+      s_l[g][row] = l;
+    }
+    __syncthreads();
+    if (g > 0) return;
+    M = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < S; ++i) M = fmaxf(M, s_m[i][row]);
+    l = x[0] = x[1] = x[2] = x[3] = 0.f;
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      const float mi = s_m[i][row], w = mi == -INFINITY ? 0.f : fast_exp2(mi - M);
+      const float4 v = *reinterpret_cast<const float4*>(&s_x[i][row][lane * 4]);
+      l += w * s_l[i][row];
+      x[0] += w * v.x;
+      x[1] += w * v.y;
+      x[2] += w * v.z;
+      x[3] += w * v.w;
+    }
+  }
+  if (!mine) return;
+  const bool none = M == -INFINITY;
+  const float inv = none ? 0.f : 1.f / l;
+  const int tok = r / G, h = j.view % a.c.hkv;
+  const size_t q = (size_t)(j.tok0 + tok) * a.hq + h * G + (r - tok * G);
+  pg_put4((T*)nullptr, a.out + (q * kD + lane * 4) * sizeof(T), x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+  if (a.lse && lane == 0) a.lse[q] = none ? -INFINITY : (M + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Joins first ... first + n of at most `rows` rows each.
+template <typename T, int G>
+hipError_t join(const PagedAttn& a, int first, int n, int rows, int parts, hipStream_t stream) {
+  if (n == 0) return hipSuccess;
+  const int per = paged_join_rows(parts), blocks = (rows + per - 1) / per;
+  if (per == kJoinRows) paged_join_kernel<T, G, 1><<<n * blocks, kJoinThreads, 0, stream>>>(a, first, blocks);
+  else paged_join_kernel<T, G, kJoinRows><<<n * blocks, kJoinThreads, 0, stream>>>(a, first, blocks);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t join_g(int G, const PagedAttn& a, int first, int n, int rows, int parts, hipStream_t s) {
+  return G == 1 ? join<T, 1>(a, first, n, rows, parts, s) : G == 2 ? join<T, 2>(a, first, n, rows, parts, s)
+       : G == 4 ? join<T, 4>(a, first, n, rows, parts, s) : join<T, 8>(a, first, n, rows, parts, s);
+}
+
+}  // namespace
+
+hipError_t launch_paged_join(int dtype, int G, const PagedAttn& a, int first, int n, int rows, int parts, hipStream_t stream) {
+  return dtype == CATEKV_BF16 ? join_g<uint16_t>(G, a, first, n, rows, parts, stream)
+                              : join_g<float>(G, a, first, n, rows, parts, stream);
+}
+
+}  // namespace catekv

@@ -15,10 +15,14 @@ typedef short pg_s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLn2 = 0.6931471805599453f;
 
-// exp2(s c - m c) with m c rounded is off by a factor that all of a row's weights share
-// and that its sum takes out again, up to 2^(|m c| 2^-24): from here on weights are
-// exp2((s - m) c), so that equal scores of any size weigh the same.
-constexpr float kPgBig = 4194304.f;
+// A row's weights are exp2(s c - m c), m c rounded once: off by a factor 2^(|m c| 2^-24)
+// that all of them share and that their sum takes out again.  From |m c| = 2^29 on that
+// could overflow, but there scores that differ do so by 32 and more (a step of fp32), and
+// any factor c' from c / 2 on gives weights of 1 and next to 0: with a power of two m c'
+// and s c' are exact, and equal scores of any size weigh the same.
+__device__ __forceinline__ float pg_factor(float m, float c) {
+  return fabsf(m) * c < 536870912.f || m == -INFINITY ? c : __uint_as_float(__float_as_uint(c) & 0x7f800000u);
+}
 
 // bf16 pair (to nearest, ties to even) of two fp32 values, x in the low half.
 __device__ __forceinline__ uint32_t pg_pack2(float x, float y) {
@@ -39,8 +43,6 @@ __device__ __forceinline__ uint4 pg_scale_q(const float*, uint4 q, float scale) 
                     __float_as_uint(__uint_as_float(q.z) * scale), __float_as_uint(__uint_as_float(q.w) * scale));
 }
 __device__ __forceinline__ uint4 pg_scale_q(const uint16_t*, uint4 q, float) { return q; }
-template <typename T>
-__device__ __forceinline__ float pg_log2_scale(float scale) { return sizeof(T) == 4 ? kLog2e : scale * kLog2e; }
 
 // Rows of a view as attention takes them: none if its length is out of range, and
 // no more than were planned for.

@@ -154,7 +154,7 @@ void paged_stream_kernel(PagedAttn a) {
   const PagedCache& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, k4 = lane >> 4;
-  const float cs = pg_log2_scale<T>(a.scale), thr = 8.0f / cs;
+  const float cs = a.log2_scale, thr = a.rise;
   const int mask = (1 << c.page_log) - 1;
   const int first = a.workers[blockIdx.x], last = a.workers[blockIdx.x + 1];
 
@@ -188,7 +188,7 @@ void paged_stream_kernel(PagedAttn a) {
 
     // ---- this wave's tiles: those of number wave, wave + 8, ... of every segment ----
     int is = 0, iu = wave;                            // next tile to load
-    auto skip = [&]() {
+    auto skip = [&]() __attribute__((always_inline)) {
       while (is < nseg && iu >= s_seg[is].n_units) {
         ++is;
         iu = wave;
@@ -196,7 +196,7 @@ void paged_stream_kernel(PagedAttn a) {
     };
     skip();
     int next_id = 0;
-    auto fetch_id = [&]() {                           // the page number of that tile
+    auto fetch_id = [&]() __attribute__((always_inline)) {                           // the page number of that tile
       if (is < nseg) {
         const int t = s_seg[is].t0 + iu * kTile;
         next_id = pg_entry(c.table + (size_t)s_seg[is].view * c.max_pages, t >> c.page_log);
@@ -205,7 +205,7 @@ void paged_stream_kernel(PagedAttn a) {
     fetch_id();
     uint4 kb[2][X::kK], vb[2][X::kV];
     int seg_of[2] = {0, 0}, tile_of[2] = {0, 0};
-    auto issue = [&](auto tag) {                      // the next tile; there is one
+    auto issue = [&](auto tag) __attribute__((always_inline)) {                      // the next tile; there is one
       constexpr int B = decltype(tag)::value;
       const int tile = s_seg[is].t0 + iu * kTile, rows = s_seg[is].t_end - tile;   // at least one row
       const size_t base = (pg_page(c, next_id) + (tile & mask)) * RB;
@@ -228,18 +228,18 @@ void paged_stream_kernel(PagedAttn a) {
     uint4 q[X::kK];
     pg_f32x4 o[8];
     float m, l;
-    bool big;                                         // in the wave: kPgBig
+    float cw;                                         // of the weights: pg_factor()
     int cur = 0;
-    auto begin = [&]() {
+    auto begin = [&]() __attribute__((always_inline)) {
       m = -INFINITY;
       l = 0.f;
-      big = false;
+      cw = cs;
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = pg_f32x4{};
 #pragma unroll
       for (int i = 0; i < X::kK; ++i) q[i] = s_q[cur][n16][i * 4 + k4];
     };
-    auto consume = [&](auto tag) {
+    auto consume = [&](auto tag) __attribute__((always_inline)) {
       constexpr int B = decltype(tag)::value;
       const Seg& sg = s_seg[cur];
       const int tile = tile_of[B];
@@ -263,25 +263,25 @@ void paged_stream_kernel(PagedAttn a) {
       if (__builtin_amdgcn_ballot_w64(mx > m && !(mx <= m + thr))) {
         const float corr = mx > m ? fast_exp2((m - mx) * cs) : 1.f;
         m = fmaxf(m, mx);
-        big = __builtin_amdgcn_ballot_w64(fabsf(m) * cs > kPgBig && m != -INFINITY) != 0;
+        cw = pg_factor(m, cs);
         l *= corr;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[e][i] *= corr;
       }
-      const float m0 = m == -INFINITY ? 0.f : m, mc = m0 * cs;
+      const float mc = m == -INFINITY ? 0.f : m * cw;
       pg_f32x4 p;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        p[r] = big ? fast_exp2((s[r] - m0) * cs) : fast_exp2(__builtin_fmaf(s[r], cs, -mc));
+        p[r] = fast_exp2(__builtin_fmaf(s[r], cw, -mc));
         l += p[r];
       }
       if (masked && __builtin_amdgcn_ballot_w64(X::any_bad(vb[B]))) X::pv_clean(vb[B], p, seen, o);
       else X::pv(vb[B], p, o);
     };
     // The waves' parts of segment cur joined; its result or partial slot written.
-    auto finish = [&]() {
+    auto finish = [&]() __attribute__((always_inline)) {
       l = add_xor32(add_xor16(l));
       barrier_lds_only();                             // the join before has been read
 #pragma unroll
@@ -331,7 +331,7 @@ void paged_stream_kernel(PagedAttn a) {
         }
       }
     };
-    auto use = [&](auto tag) {
+    auto use = [&](auto tag) __attribute__((always_inline)) {
       while (cur < seg_of[decltype(tag)::value]) {
         finish();
         ++cur;
