@@ -25,6 +25,7 @@ namespace {
 typedef pg_f32x16 f32x16;
 typedef pg_bf16x8 bf16x8;
 typedef pg_s16x4 s16x4;
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
@@ -59,11 +60,6 @@ __device__ __forceinline__ uint4 v_op(const uint4* vt, int st, int db, uint32_t 
   return make_uint4(x.x, x.y, y.x, y.y);
 }
 
-template <class F>
-__device__ __forceinline__ uint4 each(uint4 v, F f) {
-  return make_uint4(pg_both(v.x, f), pg_both(v.y, f), pg_both(v.z, f), pg_both(v.w, f));
-}
-
 // Weights of 16 cached rows, number h of 64, as an operand.
 __device__ __forceinline__ uint4 pack16(const f32x16 (&x)[2], int h) {
   const f32x16& y = x[h >> 1];
@@ -71,79 +67,94 @@ __device__ __forceinline__ uint4 pack16(const f32x16 (&x)[2], int h) {
   return make_uint4(pg_pack2(y[o], y[o + 1]), pg_pack2(y[o + 2], y[o + 3]), pg_pack2(y[o + 4], y[o + 5]), pg_pack2(y[o + 6], y[o + 7]));
 }
 
+// What is the same for all lanes about a piece.
+struct Piece {
+  int32_t view, tok0, n_new, row0, t0, slot;
+  int32_t see0;                                        // cached rows that the first new token sees
+  int32_t n_tiles, n_full;                             // tiles; those that every new row sees in full come first
+};
+
 template <int G>
 __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void paged_tile_kernel(PagedAttn a) {
-  __shared__ uint4 s_k0[kStage], s_k1[kStage], s_v0[kStage], s_v1[kStage];
+  // aligned so that they come first: their places fit the reads' 16-bit offsets
+  __shared__ __attribute__((aligned(1024))) uint4 s_k0[kStage], s_k1[kStage], s_v0[kStage], s_v1[kStage];
+  __shared__ uint4 s_q[kTileRows * kSeg];              // new rows, laid out as K is
+  __shared__ int s_bad;
 
   const PagedCache& c = a.c;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  for (int w = a.workers[blockIdx.x]; w < a.workers[blockIdx.x + 1]; ++w) {
-  uint32_t lane = threadIdx.x & 63;
-  asm volatile("" : "+v"(lane));                       // nothing of a piece is kept in registers for the next
-  const int hi = lane >> 5;
-  const PagedPiece pc = a.pieces[w];
-  const int L = pg_rows(c, pc.view, pc.max_rows);
-  const int n_rows = pc.n_new * G;
-  const int see0 = L - pc.n_new + 1;                   // cached rows that the first new token sees
-  const int r_end = min(pc.row0 + kTileRows, n_rows);  // past the piece's last new row
-  const int t_end = min(pc.t1, see0 + (r_end - 1) / G);
-  const int n_tiles = t_end > pc.t0 ? (t_end - pc.t0 + kTile - 1) / kTile : 0;
-  // tiles that every new row of the piece sees in full come first, the others are masked
-  const int n_full = max(0, min(n_tiles, (min(see0 + pc.row0 / G, t_end) - pc.t0) / kTile));
-  const bool idle = pc.row0 + wave * 32 >= n_rows;     // none of the wave's rows exists
-
-  const int h = pc.view % c.hkv;
-  const int row = pc.row0 + wave * 32 + (lane & 31);   // this lane's new row and what it sees
-  const bool mine = row < n_rows;
-  const int tok = mine ? row / G : 0;
-  const int see = mine ? see0 + tok : 0;
-  const size_t qrow = ((size_t)(pc.tok0 + tok) * a.hq + h * G + (mine ? row - tok * G : 0)) * kRB;
-  uint4 q[8];
-#pragma unroll
-  for (int ks = 0; ks < 8; ++ks) {
-    const uint4 x = ldg16(a.q + qrow + ks * 32 + hi * 16);
-    q[ks] = mine ? x : make_uint4(0, 0, 0, 0);
-  }
-
-  // ---- tiles into LDS ------------------------------------------------------------
-  // Load i of a wave fills rows 32 i + 4 wave + [0, 4) of a tile, which never lie in two
-  // pages.  Rows past the view's come from where its table's clamped entries point; masked
-  // tiles let none of them through.
-  const int32_t* ids = c.table + (size_t)pc.view * c.max_pages;
+  const int last = a.workers[blockIdx.x + 1];
   const int mask = (1 << c.page_log) - 1;
-  const int wrow = wave * 4, lrow = wrow + (lane >> 4), place = lane & 15;
-  const uint32_t k_off = (lane >> 4) * kRB + (place ^ (lrow & 15)) * 16;
-  const uint32_t v_off = (lane >> 4) * kRB + (place ^ ((lrow & 3) << 2)) * 16;
-  constexpr int kLoads = kStage / kTileThreads;        // per thread, K and V each
-  struct Ids { int id[kLoads]; };
-  auto fetch = [&](int t) __attribute__((always_inline)) {
-    Ids x;
-    const int r = pc.t0 + min(t, n_tiles - 1) * kTile + wrow;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) x.id[i] = pg_entry(ids, min((r + 32 * i) >> c.page_log, c.max_pages - 1));
+  const int wrow = wave * 4;
+  const float cs = a.log2_scale, thr = a.rise;
+  constexpr int kLoads = kStage / kTileThreads;        // DMA per thread and tile, K and V each
+
+  uint32_t lane = threadIdx.x & 63;
+  // Places of the operands in LDS, and of a lane's 16 bytes in 4 rows of a tile.  own() makes
+  // them new values to the compiler, which would otherwise keep what it makes of them, and
+  // every step's address, in registers of their own throughout.
+  uint32_t ka = k_lane(lane), va = v_lane(lane);
+  const char* k_at = c.k + (lane >> 4) * kRB + ((lane & 15) ^ ((wrow + (lane >> 4)) & 15)) * 16;
+  const char* v_at = c.v + (lane >> 4) * kRB + ((lane & 15) ^ ((lane >> 4) << 2)) * 16;
+  auto own = [&]() __attribute__((always_inline)) { asm volatile("" : "+v"(ka), "+v"(va), "+v"(lane)); };
+
+  // ---- a piece's way in ------------------------------------------------------------
+  auto open = [&](int w) __attribute__((always_inline)) {
+    const PagedPiece p = a.pieces[w];
+    Piece x;
+    x.view = p.view;
+    x.tok0 = p.tok0;
+    x.n_new = p.n_new;
+    x.row0 = p.row0;
+    x.t0 = p.t0;
+    x.slot = p.slot;
+    const int L = __builtin_amdgcn_readfirstlane(pg_rows(c, p.view, p.max_rows));
+    x.see0 = L - p.n_new + 1;
+    const int t_end = min(p.t1, x.see0 + (min(p.row0 + kTileRows, p.n_new * G) - 1) / G);
+    // without a cached row that is seen: one tile, all of it masked
+    x.n_tiles = max(1, (t_end - p.t0 + kTile - 1) / kTile);
+    x.n_full = max(0, (min(x.see0 + p.row0 / G, t_end) - p.t0) / kTile);
     return x;
   };
-  auto issue = [&](const char* pool, uint32_t off, uint4* stage, int t, const Ids& x) __attribute__((always_inline)) {
-    const int r = pc.t0 + min(t, n_tiles - 1) * kTile + wrow;
+  // Tile t's DMA: load i of a wave fills rows 32 i + 4 wave + [0, 4) of it, which never lie in
+  // two pages.  Rows past the view's come from where its table's clamped entries point;
+  // masked tiles let none of them through.
+  struct Ids { int id[kLoads]; };
+  auto fetch = [&](const Piece& x, int t) __attribute__((always_inline)) {
+    Ids y;
+    const int r = x.t0 + min(t, x.n_tiles - 1) * kTile + wrow;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      y.id[i] = pg_entry(c.table + (size_t)x.view * c.max_pages, min((r + 32 * i) >> c.page_log, c.max_pages - 1));
+    return y;
+  };
+  auto issue = [&](const Piece& x, const char* at, uint4* stage, int t, const Ids& y) __attribute__((always_inline)) {
+    const int r = x.t0 + min(t, x.n_tiles - 1) * kTile + wrow;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const char* base = pool + (pg_page(c, x.id[i]) + ((r + 32 * i) & mask)) * kRB;
-      __builtin_amdgcn_global_load_lds(base + off, (lds_void*)&stage[i * kTileThreads + wave * 64], 16, 0, 0);
+      const size_t off = (pg_page(c, y.id[i]) + ((r + 32 * i) & mask)) * kRB;
+      __builtin_amdgcn_global_load_lds(at + off, (lds_void*)&stage[i * kTileThreads + wave * 64], 16, 0, 0);
     }
   };
 
-  // Places of the operands in LDS.  own() makes them new values to the compiler, which
-  // would otherwise keep every step's in a register of its own through the loop.
-  uint32_t ka = k_lane(lane), va = v_lane(lane);
-  auto own = [&]() __attribute__((always_inline)) { asm volatile("" : "+v"(ka), "+v"(va)); };
-
-  // ---- the softmax's state ---------------------------------------------------------
-  f32x16 o[4] = {};
-  float m = -INFINITY, l = 0.f;
-  const float cs = a.log2_scale, thr = a.rise;
-  float cw = cs;                                       // of the weights: pg_factor()
-
+  // ---- the softmax's state and its steps ---------------------------------------------
+  uint4 q[8];
+  f32x16 o[4];
+  float m, l, cw;                                      // cw: pg_factor()
+  int see;                                             // cached rows that this lane's new row sees
+  // The wave's new rows, 4 per load; those past the last are the first token's.
+  auto queries = [&](const Piece& x) __attribute__((always_inline)) {
+    const int n = x.n_new * G;
+    const char* base = a.q + ((size_t)x.tok0 * a.hq + (x.view % c.hkv) * G) * kRB;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int y = 4 * i + (lane >> 4), r = x.row0 + wave * 32 + y;
+      const int tok = r < n ? r / G : 0, g = r < n ? r - tok * G : 0;
+      const char* from = base + ((size_t)tok * a.hq + g) * kRB + ((lane & 15) ^ (y & 15)) * 16;
+      __builtin_amdgcn_global_load_lds(from, (lds_void*)&s_q[(wave * 32 + 4 * i) * kSeg], 16, 0, 0);
+    }
+  };
   auto scores = [&](const uint4* kt, f32x16 (&s)[2]) __attribute__((always_inline)) {
     s[0] = s[1] = f32x16{};
 #pragma unroll
@@ -151,12 +162,12 @@ void paged_tile_kernel(PagedAttn a) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) s[kb] = mfma(k_op(kt, kb, ks, ka), q[ks], s[kb]);
   };
-  auto hide = [&](f32x16 (&s)[2], int t) __attribute__((always_inline)) {
-    const int r = pc.t0 + t * kTile + 4 * hi;
+  auto hide = [&](f32x16 (&s)[2], int r0) __attribute__((always_inline)) {
+    const int d = see - r0 - 4 * (int)(lane >> 5);
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[kb][i] = r + kb * 32 + 8 * (i >> 2) + (i & 3) < see ? s[kb][i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) s[kb][i] = kb * 32 + 8 * (i >> 2) + (i & 3) < d ? s[kb][i] : -INFINITY;
   };
   auto maximum = [&](const f32x16 (&s)[2]) __attribute__((always_inline)) {
     float mx = -INFINITY;
@@ -190,63 +201,110 @@ void paged_tile_kernel(PagedAttn a) {
     }
   };
   auto reference = [&]() __attribute__((always_inline)) { return m == -INFINITY ? 0.f : m * cw; };
-  auto product = [&](const uint4* vt, const uint4 (&p)[4]) __attribute__((always_inline)) {
+  auto weights = [&](f32x16 (&s)[2], uint4 (&p)[4]) __attribute__((always_inline)) {
+    const float mc = reference();
 #pragma unroll
-    for (int st = 0; st < 4; ++st)
-#pragma unroll
-      for (int d = 0; d < 4; ++d) o[d] = mfma(v_op(vt, st, d, va), p[st], o[d]);
+    for (int x = 0; x < 4; ++x) {
+      weights4(s, 2 * x, mc);
+      weights4(s, 2 * x + 1, mc);
+      p[x] = pack16(s, x);
+    }
   };
-  // The same for a masked tile: 0 * NaN is NaN, so V that is not finite is taken as 0 in
-  // the product and added, row by row, to the sums of the new rows that see it.
-  auto product_masked = [&](const uint4* vt, const uint4 (&p)[4], int t) __attribute__((always_inline)) {
-    uint32_t bad = 0;
-#pragma unroll 1
-    for (int i = 0; i < kStage / 64; ++i) {
-      const uint4 x = each(vt[i * 64 + lane], pg_bad16);
-      bad |= x.x | x.y | x.z | x.w;
-    }
-    if (!__builtin_amdgcn_ballot_w64(bad)) {
-      product(vt, p);
-      return;
-    }
+  auto product = [&](const uint4* vt, const uint4 (&p)[4]) __attribute__((always_inline)) {
+    uint4 f[2][4];
 #pragma unroll
-    for (int st = 0; st < 4; ++st)
+    for (int i = 0; i < 4; ++i) f[0][i] = v_op(vt, 0, i, va);
 #pragma unroll
-      for (int d = 0; d < 4; ++d) o[d] = mfma(each(v_op(vt, st, d, va), pg_clean16), p[st], o[d]);
-    const int r0 = pc.t0 + t * kTile;
+    for (int x = 0; x < 4; ++x) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (x < 3)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[(x + 1) & 1][i] = v_op(vt, x + 1, i, va);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = mfma(f[x & 1][i], p[x], o[i]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // ---- V that is not finite in masked tiles ------------------------------------------
+  // 0 * NaN is NaN: such values are taken out of the tile, and added to the sums of the new
+  // rows that see them at the piece's end.  Every thread looks at its part of the tile; a
+  // barrier later all waves know.
+  int tag = 0;                                         // of the masked tile
+  auto look = [&](const uint4* vt) __attribute__((always_inline)) {
+    ++tag;
+    u16x2 top = {0, 0};                                // the largest magnitude, as bits
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const uint4 x = vt[i * kTileThreads + wave * 64 + lane];
+      const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, y[e] & 0x7fff7fffu));
+    }
+    if (top[0] >= 0x7f80 || top[1] >= 0x7f80) s_bad = tag;
+  };
+  bool purged = false;                                 // a tile of the piece
+  auto purge = [&](uint4* vt) __attribute__((always_inline)) {
+    barrier_lds_only();
+    if (s_bad != tag) return;
+    purged = true;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      uint4& x = vt[i * kTileThreads + wave * 64 + lane];
+      x = make_uint4(pg_both(x.x, pg_clean16), pg_both(x.y, pg_clean16), pg_both(x.z, pg_clean16), pg_both(x.w, pg_clean16));
+    }
+    barrier_lds_only();
+  };
+  // what was taken out of tiles first ... of piece x
+  auto restore = [&](const Piece& x, int first) __attribute__((always_inline)) {
 #pragma unroll 1
-    for (int r = 0; r < kTile; ++r) {
-      const bool sees = r0 + r < see;
+    for (int r = x.t0 + first * kTile; r < x.t0 + x.n_tiles * kTile; ++r) {
+      const int id = pg_entry(c.table + (size_t)x.view * c.max_pages, min(r >> c.page_log, c.max_pages - 1));
+      const char* from = c.v + (pg_page(c, id) + (r & mask)) * kRB + (lane >> 5) * 8;
+      const bool sees = r < see;
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {                  // dims 32 d + 8 i + 4 hi + [0, 4)
-          const char* at = reinterpret_cast<const char*>(vt) + (r * kSeg + ((4 * d + i) ^ ((r & 3) << 2))) * 16 + hi * 8;
-          const uint2 w = *reinterpret_cast<const uint2*>(at);
-          const float x[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
+        for (int i = 0; i < 4; ++i) {                  // dims 32 d + 8 i + 4 (l / 32) + [0, 4)
+          const uint2 y = *reinterpret_cast<const uint2*>(from + (32 * d + 8 * i) * 2);
+          const float z[4] = {bf16_lo(y.x), bf16_hi(y.x), bf16_lo(y.y), bf16_hi(y.y)};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[d][4 * i + e] += sees && pg_bad32(x[e]) ? x[e] : 0.f;
+          for (int e = 0; e < 4; ++e) o[d][4 * i + e] += sees && pg_bad32(z[e]) ? z[e] : 0.f;
         }
     }
   };
 
-  // ---- the loop --------------------------------------------------------------------
+  Ids next = {}, after = {};                           // pages of the tile after the one whose scores are there, and of the one behind
+
+  // ---- turns -----------------------------------------------------------------------
   // At the head of turn t: tile t's scores are in s and their maxima taken in; K of t + 1
   // and V of t are in LDS or on their way.  Leaves tile t + 1's scores in s2.
-  Ids next = {}, after = {};                           // pages of the tiles t + 1 and t + 2
-  auto turn = [&](auto stage, auto mask_tag, int t, f32x16 (&s)[2], f32x16 (&s2)[2]) __attribute__((always_inline)) {
+  auto turn = [&](auto stage, auto mask_tag, Piece& x, int t, bool idle, f32x16 (&s)[2], f32x16 (&s2)[2]) __attribute__((always_inline)) {
     constexpr bool B = decltype(stage)::value, MASK = decltype(mask_tag)::value;
     const uint4* kt = B ? s_k0 : s_k1;
-    const uint4* vt = B ? s_v1 : s_v0;
+    uint4* vt = B ? s_v1 : s_v0;
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    issue(c.k, k_off, B ? s_k1 : s_k0, t + 2, after);
-    issue(c.v, v_off, B ? s_v0 : s_v1, t + 1, next);
+    issue(x, k_at, B ? s_k1 : s_k0, t + 2, after);
+    issue(x, v_at, B ? s_v0 : s_v1, t + 1, next);
     next = after;
-    after = fetch(t + 3);
-    if (idle) return;
+    after = fetch(x, t + 3);
     own();
     uint4 p[4];
+    if (MASK) {
+      look(vt);
+      if (!idle) {
+        scores(kt, s2);
+        weights(s, p);
+      }
+      purge(vt);
+      if (idle) return;
+      product(vt, p);
+      hide(s2, x.t0 + (t + 1) * kTile);
+      raise(maximum(s2));
+      return;
+    }
+    if (idle) return;
     // Operands come in fours, one four ahead: their wait is then for reads that have had
     // four products' time (a wait counts all LDS reads on their way).
     const float mc = reference();
@@ -255,123 +313,158 @@ void paged_tile_kernel(PagedAttn a) {
     for (int i = 0; i < 4; ++i) f[0][i] = k_op(kt, i & 1, i >> 1, ka);
     s2[0] = s2[1] = f32x16{};
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
+    for (int y = 0; y < 4; ++y) {
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        f[(x + 1) & 1][i] = x < 3 ? k_op(kt, i & 1, 2 * x + 2 + (i >> 1), ka) : v_op(vt, 0, i, va);
+        f[(y + 1) & 1][i] = y < 3 ? k_op(kt, i & 1, 2 * y + 2 + (i >> 1), ka) : v_op(vt, 0, i, va);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         __builtin_amdgcn_sched_barrier(0);
-        s2[i & 1] = mfma(f[x & 1][i], q[2 * x + (i >> 1)], s2[i & 1]);
-        if (i & 1) weights4(s, 2 * x + (i >> 1), mc);
+        s2[i & 1] = mfma(f[y & 1][i], q[2 * y + (i >> 1)], s2[i & 1]);
+        if (i & 1) weights4(s, 2 * y + (i >> 1), mc);
       }
-      p[x] = pack16(s, x);
+      p[y] = pack16(s, y);
     }
-    if (MASK) {
-      __builtin_amdgcn_sched_barrier(0);
-      product_masked(vt, p, t);
-      hide(s2, t + 1);
-      raise(maximum(s2));
-    } else {
-      float mx = -INFINITY;
+    float mx = -INFINITY;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
+    for (int y = 0; y < 4; ++y) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (y < 3)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[(y + 1) & 1][i] = v_op(vt, y + 1, i, va);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
         __builtin_amdgcn_sched_barrier(0);
-        if (x < 3)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) f[(x + 1) & 1][i] = v_op(vt, x + 1, i, va);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          __builtin_amdgcn_sched_barrier(0);
-          o[i] = mfma(f[x & 1][i], p[x], o[i]);
-          const int y = 4 * x + i;
-          mx = fmaxf(fmaxf(mx, s2[y >> 3][(y & 7) * 2]), s2[y >> 3][(y & 7) * 2 + 1]);
-        }
+        o[i] = mfma(f[y & 1][i], p[y], o[i]);
+        const int z = 4 * y + i;
+        mx = fmaxf(fmaxf(mx, s2[z >> 3][(z & 7) * 2]), s2[z >> 3][(z & 7) * 2 + 1]);
       }
-      __builtin_amdgcn_sched_barrier(0);
-      raise(mx);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    raise(mx);
   };
   using B0 = std::false_type;
   using B1 = std::true_type;
-  f32x16 sa[2], sb[2];
-  __syncthreads();                                     // the piece before has left the LDS
-  if (n_tiles > 0) {
-    next = fetch(0);
-    issue(c.k, k_off, s_k0, 0, next);
-    issue(c.v, v_off, s_v0, 0, next);
-    next = fetch(1);
-    issue(c.k, k_off, s_k1, 1, next);
-    after = fetch(2);
+
+  // ---- the worker's pieces -----------------------------------------------------------
+  // The next piece's way in begins before this one's results' way out.
+  int w = a.workers[blockIdx.x];
+  Piece x = open(w);
+  const Ids tile0 = fetch(x, 0);
+  next = fetch(x, 1);
+  queries(x);
+  issue(x, k_at, s_k0, 0, tile0);
+  issue(x, k_at, s_k1, 1, next);
+  issue(x, v_at, s_v0, 0, tile0);
+  if (threadIdx.x == 0) s_bad = 0;
+  for (;;) {
+    own();
+    {
+      const int row = x.row0 + wave * 32 + (lane & 31);
+      see = row < x.n_new * G ? x.see0 + row / G : 0;
+    }
+    const bool idle = x.row0 + wave * 32 >= x.n_new * G;   // none of the wave's rows exists
+#pragma unroll
+    for (int d = 0; d < 4; ++d) o[d] = f32x16{};
+    m = -INFINITY;
+    l = 0.f;
+    cw = cs;
+    f32x16 sa[2], sb[2];
+    const bool more = w + 1 < last;
+    const Piece y = open(more ? w + 1 : w);            // the next piece, under the wait for this one's tiles
+    const Ids y0 = fetch(y, 0), y1 = fetch(y, 1);
+    after = fetch(x, 2);
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) q[ks] = k_op(s_q + wave * 32 * kSeg, 0, ks, ka);
     if (!idle) {
       scores(s_k0, sa);
-      if (n_full < 1) hide(sa, 0);
+      if (x.n_full < 1) hide(sa, x.t0);
       raise(maximum(sa));
     }
     int t = 0;
-    for (; t + 2 < n_full; t += 2) {
-      turn(B0{}, std::false_type{}, t, sa, sb);
-      turn(B1{}, std::false_type{}, t + 1, sb, sa);
+    for (; t + 2 < x.n_full; t += 2) {
+      turn(B0{}, std::false_type{}, x, t, idle, sa, sb);
+      turn(B1{}, std::false_type{}, x, t + 1, idle, sb, sa);
     }
-    for (; t + 2 < n_tiles; t += 2) {
-      turn(B0{}, std::true_type{}, t, sa, sb);
-      turn(B1{}, std::true_type{}, t + 1, sb, sa);
+    const int first = t;
+    purged = false;
+    for (; t + 2 < x.n_tiles; t += 2) {
+      turn(B0{}, std::true_type{}, x, t, idle, sa, sb);
+      turn(B1{}, std::true_type{}, x, t + 1, idle, sb, sa);
     }
-    const bool odd = t + 1 < n_tiles;
+    const bool odd = t + 1 < x.n_tiles;
     if (odd) {
-      turn(B0{}, std::true_type{}, t++, sa, sb);
+      turn(B0{}, std::true_type{}, x, t++, idle, sa, sb);
       sa[0] = sb[0];
       sa[1] = sb[1];
     }
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    if (!idle) {
-      uint4 p[4];
-      const float mc = reference();
-#pragma unroll
-      for (int j = 0; j < 8; ++j) weights4(sa, j, mc);
-#pragma unroll
-      for (int h = 0; h < 4; ++h) p[h] = pack16(sa, h);
-      if (odd) product_masked(s_v1, p, t);
-      else product_masked(s_v0, p, t);
+    own();
+    uint4* vt = odd ? s_v1 : s_v0;
+    uint4 p[4];
+    look(vt);
+    if (!idle) weights(sa, p);
+    purge(vt);
+    if (!idle) product(vt, p);
+    if (more) {
+      barrier_lds_only();                              // V is free
+      queries(y);
+      issue(y, k_at, s_k0, 0, y0);
+      issue(y, k_at, s_k1, 1, y1);
+      issue(y, v_at, s_v0, 0, y0);
     }
-  }
 
-  // ---- results ---------------------------------------------------------------------
-  if (!mine) continue;
-  const float sum = add_xor32(l);                      // lanes l and l ^ 32 hold the same row
-  const bool none = m == -INFINITY;
-  const float mc = none ? -INFINITY : m * cs;
-  if (pc.slot >= 0) {
-    float* slot = a.slots + (size_t)pc.slot * 4;
-    const int at = row - pc.row0;
+    // ---- results -------------------------------------------------------------------
+    if (purged) restore(x, first);
+    const int at = wave * 32 + (lane & 31), row = x.row0 + at;
+    if (row < x.n_new * G) {
+      const int hi = lane >> 5, tok = row / G;
+      const size_t qrow = ((size_t)(x.tok0 + tok) * a.hq + (x.view % c.hkv) * G + (row - tok * G)) * kRB;
+      const float sum = add_xor32(l);                  // lanes l and l ^ 32 hold the same row
+      const bool none = m == -INFINITY;
+      const float mc = none ? -INFINITY : m * cs;
+      if (x.slot >= 0) {
+        float* slot = a.slots + (size_t)x.slot * 4;
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+        for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<float4*>(slot + (size_t)at * kD + d * 32 + 8 * i + 4 * hi) =
-            make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
-    if (hi == 0) {
-      slot[kTileRows * kD + at] = mc;
-      slot[kTileRows * (kD + 1) + at] = sum;
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<float4*>(slot + (size_t)at * kD + d * 32 + 8 * i + 4 * hi) =
+                make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
+        if (hi == 0) {
+          slot[kTileRows * kD + at] = mc;
+          slot[kTileRows * (kD + 1) + at] = sum;
+        }
+      } else {
+        const float inv = none ? 0.f : 1.f / sum;
+        char* out = a.out + qrow;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {             // dims 32 d + 8 i + [0, 16): the lower lanes' 8, the upper ones' 8
+            uint32_t y[2][2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+              for (int f = 0; f < 2; ++f) {
+                const float u = o[d][4 * (i + e) + 2 * f] * inv, v = o[d][4 * (i + e) + 2 * f + 1] * inv;
+                y[e][f] = none ? 0u : pg_pack2(u, v);
+              }
+            const auto lo = __builtin_amdgcn_permlane32_swap(y[0][0], y[1][0], false, false);
+            const auto hi2 = __builtin_amdgcn_permlane32_swap(y[0][1], y[1][1], false, false);
+            *reinterpret_cast<uint4*>(out + (d * 32 + 8 * (i + hi)) * 2) = make_uint4(lo[0], hi2[0], lo[1], hi2[1]);
+          }
+        if (a.lse && hi == 0) a.lse[qrow / kRB] = none ? -INFINITY : (mc + __builtin_amdgcn_logf(sum)) * kLn2;
+      }
     }
-    continue;
-  }
-  const float inv = none ? 0.f : 1.f / sum;
-  char* out = a.out + qrow;
-#pragma unroll
-  for (int d = 0; d < 4; ++d)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float x[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = none ? 0.f : o[d][4 * i + e] * inv;
-      pg_put4((uint16_t*)nullptr, out + (d * 32 + 8 * i + 4 * hi) * 2, x[0], x[1], x[2], x[3]);
-    }
-  if (a.lse && hi == 0) a.lse[qrow / kRB] = none ? -INFINITY : (mc + __builtin_amdgcn_logf(sum)) * kLn2;
+    if (!more) break;
+    ++w;
+    x = y;
+    next = y1;
   }
 }
 
