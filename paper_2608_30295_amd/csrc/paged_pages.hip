@@ -5,7 +5,7 @@
 // kept in an order: releasing is an atomic decrement per page and, where it reaches
 // 0, an atomic or of its bit, and the result does not depend on the order of either.
 // Taking runs in one workgroup: a scan over the views' needs, then a scan over the
-// bits' words (1024 threads x 4 words: 262144 pages a turn) until enough are found.
+// bits' words (65536 pages a turn) until enough are found.
 #include "common.h"
 #include "paged.h"
 
@@ -14,7 +14,6 @@ namespace {
 
 constexpr int kTakeThreads = 1024;
 constexpr int kTakeWaves = kTakeThreads / 64;
-constexpr int kTakeWords = 4;                    // words of bits per thread and turn
 
 // ---- state ---------------------------------------------------------------------
 
@@ -61,31 +60,40 @@ __device__ __forceinline__ int scan_block(int x, int* s_wave, int& total) {
   return before + v - x;
 }
 
+// Up to kTakeLds of the pages found stay in LDS, too.
+constexpr int kTakeLds = 4096;
+struct TakeLds {
+  int wave[kTakeWaves];
+  int page[kTakeLds];
+};
+
+// Word number `at` of the free pages' bits.
+__device__ __forceinline__ uint64_t free_word(const PagedCache& c, int at) {
+  uint64_t b = at < (c.n_pages + 63) >> 6 ? c.bits[at] : 0;
+  const int last = c.n_pages - at * 64;                     // pages of the last word
+  return last < 64 && last > 0 ? b & ((1ull << last) - 1) : b;
+}
+
 // The numbers of the lowest `need` free pages into takes; returns how many there
-// are, at most need.  Nothing is marked yet.
-__device__ int find_free(const PagedCache& c, int need, int32_t* takes, int* s_wave) {
-  const int words = (c.n_pages + 63) >> 6;
+// are, at most need.  Nothing is marked yet.  A thread counts a word (the first turn's
+// given: asked for before it was known what is needed); then a wave goes over those of its
+// 64 words that give pages, a lane per bit.
+__device__ int find_free(const PagedCache& c, uint64_t word, int need, int32_t* takes, TakeLds& s) {
+  const int words = (c.n_pages + 63) >> 6, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int found = 0;
-  for (int w0 = 0; w0 < words && found < need; w0 += kTakeThreads * kTakeWords) {
-    uint64_t bits[kTakeWords];
-    int n = 0;
-    const int at = w0 + threadIdx.x * kTakeWords;
-#pragma unroll
-    for (int i = 0; i < kTakeWords; ++i) {
-      uint64_t b = at + i < words ? c.bits[at + i] : 0;
-      const int last = c.n_pages - (at + i) * 64;           // pages of the last word
-      if (last < 64 && last > 0) b &= (1ull << last) - 1;
-      bits[i] = b;
-      n += __popcll(b);
-    }
+  for (int w0 = 0; w0 < words && found < need; w0 += kTakeThreads) {
+    if (w0 > 0) word = free_word(c, w0 + (int)threadIdx.x);
     int total;
-    int place = found + scan_block(n, s_wave, total);
-#pragma unroll
-    for (int i = 0; i < kTakeWords; ++i) {
-      uint64_t b = bits[i];
-      while (b && place < need) {
-        takes[place++] = (at + i) * 64 + __ffsll((unsigned long long)b) - 1;
-        b &= b - 1;
+    const int before = found + scan_block(__popcll(word), s.wave, total);
+    for (uint64_t give = __builtin_amdgcn_ballot_w64(word != 0 && before < need); give; give &= give - 1) {
+      const int i = __ffsll((unsigned long long)give) - 1;
+      const uint64_t b = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(word >> 32), i) << 32 |
+                         (uint32_t)__builtin_amdgcn_readlane((uint32_t)word, i);
+      const int place = __builtin_amdgcn_readlane(before, i) + __popcll(b & ((1ull << lane) - 1));
+      if ((b >> lane & 1) && place < need) {
+        const int p = (w0 + wave * 64 + i) * 64 + lane;
+        takes[place] = p;
+        if (place < kTakeLds) s.page[place] = p;
       }
     }
     found += total;
@@ -94,9 +102,9 @@ __device__ int find_free(const PagedCache& c, int need, int32_t* takes, int* s_w
   return found < need ? found : need;
 }
 
-__device__ void mark_taken(const PagedCache& c, const int32_t* takes, int n) {
+__device__ void mark_taken(const PagedCache& c, const int32_t* takes, int n, const TakeLds& s) {
   for (int j = threadIdx.x; j < n; j += kTakeThreads) {
-    const int p = takes[j];
+    const int p = j < kTakeLds ? s.page[j] : takes[j];
     c.refs[p] = 1;
     atomicAnd((unsigned long long*)&c.bits[p >> 6], ~(1ull << (p & 63)));
   }
@@ -119,97 +127,102 @@ __global__ __launch_bounds__(256) void paged_init_kernel(PagedCache c) {
 // ---- append --------------------------------------------------------------------
 
 // First launch: what every view needs, the pages, lengths and released pages.
-// Views are taken by whole sequences, as many as the workgroup has threads for.
+// Views are taken by whole sequences, as many as the workgroup has threads for; what a
+// thread found out about its view stays in registers if that is all of them.
 __global__ __launch_bounds__(kTakeThreads) void paged_take_kernel(PagedAppend a) {
-  __shared__ int s_wave[kTakeWaves];
+  __shared__ TakeLds s;
   __shared__ int s_bad[kTakeThreads];
   __shared__ int s_end[kTakeThreads];
   __shared__ int s_used;
   const PagedCache& c = a.c;
   const int hkv = c.hkv, per = kTakeThreads / hkv, tid = threadIdx.x;
   const int si = tid / hkv, h = tid - si * hkv;
+  const bool once = a.n_seqs <= per;
+  PagedTake t{-1, 0, -1};
+  PagedSeq q{};
+  int need = 0;
+  if (tid == 0) s_used = 0;
+  const uint64_t word = free_word(c, tid);
   // needs, numbered through
   int total = 0;
   for (int s0 = 0; s0 < a.n_seqs; s0 += per) {
     const bool mine = si < per && s0 + si < a.n_seqs;
     if (tid < per) s_bad[tid] = 0;
     __syncthreads();
-    int need = 0, from = -1;
-    int64_t L = -1;
+    t = PagedTake{-1, 0, -1};
+    need = 0;
     if (mine) {
-      const PagedSeq q = a.seqs[s0 + si];
+      q = a.seqs[s0 + si];
       const int view = q.slot * hkv + h;
-      L = c.lens[view];
-      if (L < 0 || L + q.n_new > cap_rows(c)) {
-        s_bad[si] = 1;
-        if (q.n_new > 0 && a.overflow) *a.overflow = 1;
-      } else if (q.n_new > 0) {
-        const int had = pages_of(c, L);
-        need = pages_of(c, L + q.n_new) - had;
-        if (L & ((1 << c.page_log) - 1)) {
-          const int last = page_in(c, row_of(c, view)[had - 1]);
-          if (c.refs[last] > 1) {
-            from = last;
-            ++need;
+      const int64_t L = c.lens[view];
+      if (q.n_new > 0) {
+        if (L < 0 || L + q.n_new > cap_rows(c)) {
+          s_bad[si] = 1;
+          if (a.overflow) *a.overflow = 1;
+        } else {
+          t.len = L;
+          const int had = pages_of(c, L);
+          need = pages_of(c, L + q.n_new) - had;
+          if (L & ((1 << c.page_log) - 1)) {
+            const int last = page_in(c, row_of(c, view)[had - 1]);
+            if (c.refs[last] > 1) {
+              t.from = last;
+              ++need;
+            }
           }
         }
       }
-      if (q.n_new == 0) L = -1;
     }
     __syncthreads();
     if (mine && s_bad[si]) {
       need = 0;
-      L = -1;
+      t.len = -1;
     }
     int sum;
-    const int start = total + scan_block(need, s_wave, sum);
+    t.start = total + scan_block(need, s.wave, sum);
     total += sum;
-    if (mine) a.views[(s0 + si) * hkv + h] = PagedTake{L, start, from};
+    if (mine && !once) a.views[(s0 + si) * hkv + h] = t;
   }
-  const int found = total > 0 ? find_free(c, total, a.takes, s_wave) : 0;
-  if (tid == 0) s_used = 0;
-  __syncthreads();
+  const int found = total > 0 ? find_free(c, word, total, a.takes, s) : 0;
   // a sequence whose last page was not found is left, and all after it that need any
   for (int s0 = 0; s0 < a.n_seqs; s0 += per) {
     const bool mine = si < per && s0 + si < a.n_seqs;
     const int v = (s0 + si) * hkv + h;
-    PagedTake t{-1, 0, -1};
-    int need = 0, n_new = 0, slot = 0;
-    if (mine) {
-      t = a.views[v];
-      n_new = a.seqs[s0 + si].n_new;
-      slot = a.seqs[s0 + si].slot;
-      if (t.len >= 0) need = pages_of(c, t.len + n_new) - pages_of(c, t.len) + (t.from >= 0);
-    }
-    if (tid < per) {
-      s_bad[tid] = 0;      // pages that the sequence needs
-      s_end[tid] = 0;
-    }
-    __syncthreads();
-    if (mine && need > 0) {
-      atomicAdd(&s_bad[si], need);
-      atomicMax(&s_end[si], t.start + need);
-    }
-    __syncthreads();
-    if (mine && t.len >= 0) {
-      if (s_bad[si] > 0 && s_end[si] > found) {
-        a.views[v].len = -1;
-        if (a.overflow) *a.overflow = 1;
-      } else {
-        const int view = slot * hkv + h;
-        c.lens[view] = t.len + n_new;
-        if (need > 0) atomicMax(&s_used, t.start + need);
+    if (!once) {
+      need = 0;
+      if (mine) {
+        t = a.views[v];
+        q = a.seqs[s0 + si];
+        if (t.len >= 0) need = pages_of(c, t.len + q.n_new) - pages_of(c, t.len) + (t.from >= 0);
       }
+    }
+    if (tid < per) s_end[tid] = 0;       // past the last page that the sequence needs
+    __syncthreads();
+    if (mine && need > 0) atomicMax(&s_end[si], t.start + need);
+    __syncthreads();
+    if (mine) {
+      if (t.len >= 0) {
+        if (s_end[si] > found) {
+          t.len = -1;
+          if (a.overflow) *a.overflow = 1;
+        } else {
+          c.lens[q.slot * hkv + h] = t.len + q.n_new;
+          if (need > 0) atomicMax(&s_used, t.start + need);
+        }
+      }
+      a.views[v] = t;
     }
     __syncthreads();
   }
+  mark_taken(c, a.takes, s_used, s);
   __syncthreads();
-  const int used = s_used;
-  mark_taken(c, a.takes, used);
-  __syncthreads();
+  if (once) {
+    if (si < per && si < a.n_seqs && t.len >= 0 && t.from >= 0) release(c, t.from);
+    return;
+  }
   for (int v = tid; v < a.n_seqs * hkv; v += kTakeThreads) {
-    const PagedTake t = a.views[v];
-    if (t.len >= 0 && t.from >= 0) release(c, t.from);
+    const PagedTake u = a.views[v];
+    if (u.len >= 0 && u.from >= 0) release(c, u.from);
   }
 }
 
@@ -258,9 +271,39 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PagedAppend a, int row_
 }
 
 // ---- fork and drop ---------------------------------------------------------------
-// One workgroup per view: the view's length is read and written by it alone.
+// One workgroup per view: the view's length is read and written by it alone.  A thread
+// has kAhead entries on their way at a time.
+constexpr int kEntryThreads = 512;
+constexpr int kAhead = 4;
 
-__global__ __launch_bounds__(256) void paged_fork_kernel(PagedFork a) {
+// f(page, entry) of the entries [p0, p1) of a row
+template <class F>
+__device__ __forceinline__ void each_entry(const int32_t* row, int p0, int p1, F f) {
+  for (int p = p0 + (int)threadIdx.x; p < p1; p += kEntryThreads * kAhead) {
+    int id[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) id[i] = p + i * kEntryThreads < p1 ? row[p + i * kEntryThreads] : -1;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (p + i * kEntryThreads < p1) f(p + i * kEntryThreads, id[i]);
+  }
+}
+
+// The entries' pages released: all counts down before the first bit.
+__device__ __forceinline__ void release_entries(const PagedCache& c, int32_t* row, int p0, int p1) {
+  for (int p = p0 + (int)threadIdx.x; p < p1; p += kEntryThreads * kAhead) {
+    int id[kAhead], was[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) id[i] = p + i * kEntryThreads < p1 ? row[p + i * kEntryThreads] : -1;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) was[i] = (uint32_t)id[i] < (uint32_t)c.n_pages ? atomicSub(&c.refs[id[i]], 1) : 0;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (was[i] == 1) atomicOr((unsigned long long*)&c.bits[id[i] >> 6], 1ull << (id[i] & 63));
+  }
+}
+
+__global__ __launch_bounds__(kEntryThreads) void paged_fork_kernel(PagedFork a) {
   const PagedCache& c = a.c;
   const int i = blockIdx.x / c.hkv, h = blockIdx.x - i * c.hkv;
   const int src = a.src[i] * c.hkv + h, dst = a.dst[i] * c.hkv + h;
@@ -269,77 +312,78 @@ __global__ __launch_bounds__(256) void paged_fork_kernel(PagedFork a) {
     if (threadIdx.x == 0 && a.refused) *a.refused = 1;
     return;
   }
-  const int n = pages_of(c, L);
-  const int32_t* from = row_of(c, src);
   int32_t* to = row_of(c, dst);
-  for (int p = threadIdx.x; p < n; p += 256) {
-    const int id = page_in(c, from[p]);
+  each_entry(row_of(c, src), 0, pages_of(c, L), [&](int p, int id) {
+    id = page_in(c, id);
     to[p] = id;
     atomicAdd(&c.refs[id], 1);
-  }
+  });
   __syncthreads();                                   // every thread has read the length
   if (threadIdx.x == 0) c.lens[dst] = L;
 }
 
-__global__ __launch_bounds__(256) void paged_drop_kernel(PagedCache c, const int64_t* rows) {
+__global__ __launch_bounds__(kEntryThreads) void paged_drop_kernel(PagedCache c, const int64_t* rows) {
   const int view = blockIdx.x, slot = view / c.hkv;
   const int64_t off = rows[slot];
   const int64_t L = rows_of(c, view);
   if (off <= 0 || L == 0) return;
   const int64_t left = off < L ? L - off : 0;
   int32_t* row = row_of(c, view);
-  const int n = pages_of(c, L);
-  for (int p = pages_of(c, left) + (int)threadIdx.x; p < n; p += 256) {
-    release(c, row[p]);
-    row[p] = -1;
-  }
+  const int p0 = pages_of(c, left), p1 = pages_of(c, L);
+  release_entries(c, row, p0, p1);
+  for (int p = p0 + (int)threadIdx.x; p < p1; p += kEntryThreads) row[p] = -1;   // a thread's own entries
   __syncthreads();
   if (threadIdx.x == 0) c.lens[view] = left;
 }
 
 // ---- compact ---------------------------------------------------------------------
 
+// First launch: how many rows every view keeps, where its chunks go, and the pages.  A
+// wave goes over a view's list.
 __global__ __launch_bounds__(kTakeThreads) void paged_compact_take_kernel(PagedCompact a) {
-  __shared__ int s_wave[kTakeWaves];
-  __shared__ int64_t s_len[kPagedMaxHeads];
+  __shared__ TakeLds s_find;
   __shared__ PagedTake s_take[kPagedMaxHeads];
-  __shared__ int s_used;
+  __shared__ int s_used, s_total;
   const PagedCache& c = a.c;
-  const int tid = threadIdx.x;
-  if (tid < a.n_sel) s_len[tid] = c.lens[a.slot * c.hkv + a.heads[tid]];
-  __syncthreads();
-  int total = 0;
-  for (int s = 0; s < a.n_sel; ++s) {
-    const int64_t L = s_len[s];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const uint64_t word = free_word(c, tid);
+  for (int s = tid >> 6; s < a.n_sel; s += kTakeWaves) {
+    const int64_t L = c.lens[a.slot * c.hkv + a.heads[s]];
     const int64_t n = L - a.tail;
     const bool fine = n >= 0 && L <= cap_rows(c);
     int64_t rows = 0;
-    for (int e0 = 0; e0 < a.b; e0 += kTakeThreads) {
-      const int e = e0 + tid;
-      int64_t len = 0;
-      if (fine && e < a.b) {
-        const int ch = a.idx[(size_t)s * a.b + e];
-        if (ch >= 0) {
-          len = n - (int64_t)ch * a.cs;
-          len = len < 0 ? 0 : len > a.cs ? a.cs : len;
-        }
+    const int32_t* list = a.idx + (size_t)s * a.b;
+    int next = lane < a.b ? list[lane] : -1;
+    for (int e0 = 0; e0 < a.b; e0 += 64) {
+      const int e = e0 + lane, ch = next;
+      next = e + 64 < a.b ? list[e + 64] : -1;
+      int64_t len = fine && ch >= 0 ? n - (int64_t)ch * a.cs : 0;
+      len = len < 0 ? 0 : len > a.cs ? a.cs : len;
+      int v = (int)len;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(v, o);
+        if (lane >= o) v += y;
       }
-      int sum;
-      const int before = scan_block((int)len, s_wave, sum);
-      if (e < a.b) a.offs[(size_t)s * a.b + e] = (int)rows + before;
-      rows += sum;
+      if (e < a.b) a.offs[(size_t)s * a.b + e] = (int)rows + v - (int)len;
+      rows += __shfl(v, 63);
     }
     rows += a.tail;
-    const bool fits = fine && rows <= cap_rows(c);
-    const int need = fits ? pages_of(c, rows) : 0;
-    if (tid == 0) {
-      s_take[s] = PagedTake{fits ? L : -1, total, (int)rows};
-      if (!fits && a.overflow) *a.overflow = 1;
-    }
-    total += need;
+    if (lane == 0) s_take[s] = PagedTake{fine && rows <= cap_rows(c) ? L : -1, 0, (int)rows};
   }
-  const int found = total > 0 ? find_free(c, total, a.takes, s_wave) : 0;
   __syncthreads();
+  if (tid == 0) {
+    int total = 0;
+    for (int s = 0; s < a.n_sel; ++s) {
+      s_take[s].start = total;
+      if (s_take[s].len >= 0) total += pages_of(c, s_take[s].from);
+      else if (a.overflow) *a.overflow = 1;
+    }
+    s_total = total;
+  }
+  __syncthreads();
+  const int total = s_total;
+  const int found = total > 0 ? find_free(c, word, total, a.takes, s_find) : 0;
   // the first view that does not find its pages and all after it that need any stay
   if (tid == 0) {
     int used = 0;
@@ -358,7 +402,7 @@ __global__ __launch_bounds__(kTakeThreads) void paged_compact_take_kernel(PagedC
   }
   __syncthreads();
   if (tid < a.n_sel) a.views[tid] = s_take[tid];
-  mark_taken(c, a.takes, s_used);
+  mark_taken(c, a.takes, s_used, s_find);
 }
 
 template <int LPR>
@@ -393,7 +437,7 @@ __global__ __launch_bounds__(256) void paged_compact_rows_kernel(PagedCompact a,
   }
 }
 
-__global__ __launch_bounds__(256) void paged_compact_swap_kernel(PagedCompact a) {
+__global__ __launch_bounds__(kEntryThreads) void paged_compact_swap_kernel(PagedCompact a) {
   const PagedCache& c = a.c;
   const int s = blockIdx.x;
   const PagedTake t = a.views[s];
@@ -401,10 +445,9 @@ __global__ __launch_bounds__(256) void paged_compact_swap_kernel(PagedCompact a)
   const int view = a.slot * c.hkv + a.heads[s];
   int32_t* row = row_of(c, view);
   const int had = pages_of(c, t.len), have = pages_of(c, t.from);
-  for (int p = threadIdx.x; p < (had > have ? had : have); p += 256) {
-    if (p < had) release(c, row[p]);
-    row[p] = p < have ? a.takes[t.start + p] : -1;
-  }
+  release_entries(c, row, 0, had);
+  // a thread's own entries: the same ones that it released
+  for (int p = threadIdx.x; p < (had > have ? had : have); p += kEntryThreads) row[p] = p < have ? a.takes[t.start + p] : -1;
   if (threadIdx.x == 0) c.lens[view] = t.from;
 }
 
@@ -465,12 +508,12 @@ hipError_t launch_paged_append(const PagedAppend& a, hipStream_t stream) {
 }
 
 hipError_t launch_paged_fork(const PagedFork& a, hipStream_t stream) {
-  paged_fork_kernel<<<a.n * a.c.hkv, 256, 0, stream>>>(a);
+  paged_fork_kernel<<<a.n * a.c.hkv, kEntryThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_paged_drop(const PagedCache& c, const int64_t* rows, hipStream_t stream) {
-  paged_drop_kernel<<<c.n_slots * c.hkv, 256, 0, stream>>>(c, rows);
+  paged_drop_kernel<<<c.n_slots * c.hkv, kEntryThreads, 0, stream>>>(c, rows);
   return hipGetLastError();
 }
 
@@ -487,7 +530,7 @@ hipError_t launch_paged_compact(const PagedCompact& a, hipStream_t stream) {
   else paged_compact_rows_kernel<32><<<grid, 256, 0, stream>>>(a, (int)groups);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  paged_compact_swap_kernel<<<a.n_sel, 256, 0, stream>>>(a);
+  paged_compact_swap_kernel<<<a.n_sel, kEntryThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
