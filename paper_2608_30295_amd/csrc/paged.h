@@ -125,7 +125,7 @@ struct PagedAttn {
 constexpr int kTileThreads = 512;        // bf16; fp32: 256
 constexpr int kJoinThreads = 256;
 constexpr int kJoinRows = kJoinThreads / 32;   // rows of a joining workgroup, where rows have few parts
-inline int paged_join_rows(int parts) { return parts > 4 ? 1 : kJoinRows; }
+inline int paged_join_rows(int parts) { return parts > 8 ? 1 : kJoinRows; }
 // New rows of a tile piece at most, and the launch, per type.
 constexpr int kTileRows = 256, kTileRowsF32 = 128;
 inline int paged_tile_rows(int dtype) { return dtype == CATEKV_BF16 ? kTileRows : kTileRowsF32; }

@@ -111,15 +111,18 @@ struct Plan {
 };
 
 // ---- tiles of many new rows --------------------------------------------------------
-// Cut into pieces and dealt out to workgroups, one per compute unit, here: the GPU deals
-// workgroups to its engines in turn and lets one engine's compute units stand idle while
-// another's queue (2048 tokens at 32K in 376 pieces of unequal length: 1280 us where its
-// longest share takes 890).  Costs in units: a piece of u units takes u + kPieceFixed (new
-// rows in, results out); joining takes a launch, and its partial results' way to memory and
-// back, kSlotUnits for each.
-constexpr int64_t kPieceFixed = 4;
-constexpr int64_t kJoinLaunch = 4;
-constexpr double kSlotUnits = 0.04;
+// Cut into pieces and dealt out to workgroups here, as many as the GPU holds at once: the
+// GPU deals workgroups to its engines in turn and lets one engine's compute units stand
+// idle while another's queue (2048 tokens at 32K in 376 pieces of unequal length: 1280 us
+// where its longest share takes 890).
+//
+// What the ways to cut are compared by, in us as measured: a unit (64 cached rows; fp32
+// with two workgroups to a compute unit), a piece's way in and out, the joining launch
+// and a partial result's way to memory and back.
+struct TileCosts {
+  double unit, piece, join, slot;
+};
+constexpr TileCosts kTileCosts = {1.8, 7.0, 6.0, 0.07}, kTileCostsF32 = {14.0, 12.0, 6.0, 0.035};
 constexpr int kXcds = 8;               // a worker's engine is its number modulo this
 
 struct Tile {
@@ -127,55 +130,88 @@ struct Tile {
   int64_t rows, units;
 };
 
-struct Deal {
-  int64_t share = 0;                   // most units of a piece; 0: tiles stay whole
-  double cost = 0;
-  std::vector<int> worker;             // of every piece, pieces in order of size
-};
-
 struct Cut {
-  int tile, part, parts;
-  int64_t units;
+  int tile;
+  int64_t u0, u1;                      // units
+  int worker;
 };
 
-std::vector<Cut> cut_tiles(const std::vector<Tile>& tiles, int64_t share) {
+struct Deal {
   std::vector<Cut> cuts;
-  for (size_t i = 0; i < tiles.size(); ++i) {
-    const int64_t u = tiles[i].units, parts = share ? (u + share - 1) / share : 1;
-    for (int64_t s = 0; s < parts; ++s) cuts.push_back({(int)i, (int)s, (int)parts, u * (s + 1) / parts - u * s / parts});
+  double cost = 0;
+};
+
+void price(Deal& d, const std::vector<Tile>& tiles, int workers, const TileCosts& k) {
+  std::vector<double> load(workers, 0.0);
+  double most = 0;
+  int64_t slots = 0;
+  for (const Cut& c : d.cuts) {
+    load[c.worker] += k.unit * (double)(c.u1 - c.u0) + k.piece;
+    most = std::max(most, load[c.worker]);
+    slots += c.u1 - c.u0 < tiles[c.tile].units;
   }
-  std::stable_sort(cuts.begin(), cuts.end(), [](const Cut& x, const Cut& y) { return x.units > y.units; });
-  return cuts;
+  d.cost = most + (slots > 0 ? k.join + k.slot * (double)slots : 0.0);
 }
 
-// The longest pieces first, each to the worker with least to do; one of the engine that
-// has the view's other pieces (its cache holds what they read) if that costs little.
-Deal deal(const std::vector<Tile>& tiles, int64_t share, int workers) {
+// Tiles in parts of at most `share` units (0: whole), the longest first, each to the
+// worker with least to do; one of the engine that has the view's other pieces (its cache
+// holds what they read) if that costs little.
+Deal deal(const std::vector<Tile>& tiles, int64_t share, int workers, const TileCosts& k) {
   Deal d;
-  d.share = share;
-  const std::vector<Cut> cuts = cut_tiles(tiles, share);
-  using Load = std::pair<int64_t, int>;
+  for (size_t i = 0; i < tiles.size(); ++i) {
+    const int64_t u = tiles[i].units, parts = share ? (u + share - 1) / share : 1;
+    for (int64_t s = 0; s < parts; ++s) d.cuts.push_back({(int)i, u * s / parts, u * (s + 1) / parts, 0});
+  }
+  std::stable_sort(d.cuts.begin(), d.cuts.end(), [](const Cut& x, const Cut& y) { return x.u1 - x.u0 > y.u1 - y.u0; });
+  using Load = std::pair<double, int>;
   std::vector<std::priority_queue<Load, std::vector<Load>, std::greater<Load>>> engines(kXcds);
-  for (int w = 0; w < workers; ++w) engines[w % kXcds].push({0, w});
-  int64_t total = 0, most = 0;
-  for (const Cut& c : cuts) total += c.units + kPieceFixed;
-  const int64_t slack = total / workers / 64;
-  double slots = 0;
-  for (const Cut& c : cuts) {
-    int best = 0;
-    for (int x = 1; x < kXcds; ++x)
-      if (!engines[x].empty() && (engines[best].empty() || engines[x].top() < engines[best].top())) best = x;
+  for (int w = 0; w < workers; ++w) engines[w % kXcds].push({0.0, w});
+  double total = 0;
+  for (const Cut& c : d.cuts) total += k.unit * (double)(c.u1 - c.u0) + k.piece;
+  const double slack = total / workers / 64;
+  for (Cut& c : d.cuts) {
+    int best = -1;
+    for (int x = 0; x < kXcds; ++x)
+      if (!engines[x].empty() && (best < 0 || engines[x].top() < engines[best].top())) best = x;
     const int own = tiles[c.tile].p.view % kXcds;
     if (!engines[own].empty() && engines[own].top().first <= engines[best].top().first + slack) best = own;
     const Load l = engines[best].top();
     engines[best].pop();
-    const int64_t load = l.first + c.units + kPieceFixed;
-    engines[best].push({load, l.second});
-    most = std::max(most, load);
-    d.worker.push_back(l.second);
-    if (c.parts > 1) slots += 1;
+    engines[best].push({l.first + k.unit * (double)(c.u1 - c.u0) + k.piece, l.second});
+    c.worker = l.second;
   }
-  d.cost = (double)most + (slots > 0 ? (double)kJoinLaunch + kSlotUnits * slots : 0);
+  price(d, tiles, workers, k);
+  return d;
+}
+
+// All tiles end to end, cut into equal shares; neighbours lie in one engine.  No part
+// is shorter than half a piece's way in and out.
+Deal deal_line(const std::vector<Tile>& tiles, int workers, const TileCosts& k) {
+  Deal d;
+  int64_t left = 0;
+  for (const Tile& t : tiles) left += t.units;
+  const int64_t least = std::max<int64_t>(1, (int64_t)(k.piece / k.unit / 2));
+  const int per = std::max(1, workers / kXcds);
+  size_t i = 0;
+  int64_t off = 0;
+  for (int s = 0; s < workers && i < tiles.size(); ++s) {
+    int64_t want = std::max<int64_t>(least, (left + workers - s - 1) / (workers - s));
+    const bool last = s == workers - 1;
+    const int w = workers % kXcds == 0 ? s % per * kXcds + s / per : s;
+    while (i < tiles.size() && (want >= least || last)) {
+      const int64_t rest = tiles[i].units - off;
+      int64_t take = last || rest <= want + least ? rest : want;
+      d.cuts.push_back({(int)i, off, off + take, w});
+      want -= take;
+      left -= take;
+      off += take;
+      if (off == tiles[i].units) {
+        ++i;
+        off = 0;
+      }
+    }
+  }
+  price(d, tiles, workers, k);
   return d;
 }
 
@@ -253,34 +289,41 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
           const int64_t rows = rows_seen(i, h, r, R);
           tiles.push_back({piece(i, h, r), rows, units_of(rows)});
         }
-    Deal best = deal(tiles, 0, cus);
-    const int64_t even = (tile_units + cus - 1) / cus;
-    for (int k = 1; k <= 4 && n_tiles < 8 * (int64_t)cus; ++k) {
-      const int64_t share = std::max<int64_t>(kPieceFixed, (even + k - 1) / k);
-      Deal d = deal(tiles, share, cus);
+    const bool half = c->dtype == CATEKV_BF16;
+    const TileCosts& costs = half ? kTileCosts : kTileCostsF32;
+    const int workers = half ? cus : 2 * cus;
+    Deal best = deal(tiles, 0, workers, costs);
+    if (n_tiles < 8 * (int64_t)workers) {
+      const int64_t even = (tile_units + workers - 1) / workers;
+      for (int k = 2; k <= 8; ++k) {                 // shares of 2 to 1/2 of an equal one
+        Deal d = deal(tiles, std::max<int64_t>(1, (4 * even + k - 1) / k), workers, costs);
+        if (d.cost < best.cost) best = std::move(d);
+      }
+      Deal d = deal_line(tiles, workers, costs);
       if (d.cost < best.cost) best = std::move(d);
     }
-    const std::vector<Cut> cuts = cut_tiles(tiles, best.share);
+    std::vector<int> parts(tiles.size(), 0);
+    for (const Cut& c : best.cuts) ++parts[c.tile];
     std::vector<int64_t> slot(tiles.size(), -1);
     const int64_t each = (int64_t)(paged_slot_floats(R) / 4);
-    for (const Cut& c : cuts)
-      if (c.parts > 1 && slot[c.tile] < 0) {
-        slot[c.tile] = P.slot16;
-        join(tiles[c.tile].p, c.parts, R);
+    for (size_t i = 0; i < tiles.size(); ++i)
+      if (parts[i] > 1) {
+        slot[i] = P.slot16;
+        join(tiles[i].p, parts[i], R);
         if (P.slot16 > INT32_MAX) return fail(CATEKV_ERR_UNSUPPORTED, "too many partial results");
       }
-    std::vector<size_t> order(cuts.size());
-    for (size_t i = 0; i < order.size(); ++i) order[i] = i;
-    std::stable_sort(order.begin(), order.end(), [&](size_t x, size_t y) { return best.worker[x] < best.worker[y]; });
+    std::stable_sort(best.cuts.begin(), best.cuts.end(), [](const Cut& x, const Cut& y) { return x.worker < y.worker; });
     P.tile_workers.assign(1, 0);
-    for (size_t i : order) {
-      const Cut& c = cuts[i];
-      while ((int)P.tile_workers.size() <= best.worker[i]) P.tile_workers.push_back((int32_t)P.tiles.size());
-      const int64_t u = tiles[c.tile].units;
+    for (const Cut& c : best.cuts) {
+      while ((int)P.tile_workers.size() <= c.worker) P.tile_workers.push_back((int32_t)P.tiles.size());
       PagedPiece p = tiles[c.tile].p;
-      p.t0 = (int32_t)(u * c.part / c.parts * kPagedUnit);
-      p.t1 = (int32_t)std::min<int64_t>(tiles[c.tile].rows, u * (c.part + 1) / c.parts * kPagedUnit);
-      p.slot = c.parts > 1 ? (int32_t)(slot[c.tile] + c.part * each) : -1;
+      p.t0 = (int32_t)(c.u0 * kPagedUnit);
+      p.t1 = (int32_t)std::min<int64_t>(tiles[c.tile].rows, c.u1 * kPagedUnit);
+      p.slot = -1;
+      if (parts[c.tile] > 1) {
+        p.slot = (int32_t)slot[c.tile];
+        slot[c.tile] += each;
+      }
       P.tiles.push_back(p);
     }
     P.tile_workers.push_back((int32_t)P.tiles.size());
