@@ -62,27 +62,12 @@ __device__ __forceinline__ int pg_entry(const int32_t* ids, int p) {
   return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>((uint64_t)hi << 32 | lo);
 }
 
-// ---- V that is not finite where some of the tokens do not see it -----------------
-// 0 * NaN and 0 * inf are NaN: such values are taken as 0 in the product, and counted
-// for the tokens that see them in a second one, by a code each: 1, 2^7 and 2^14 for
-// +inf, -inf and NaN (exact in bf16 and, for up to 127 rows, in the sum).
+// ---- V that is not finite: the exponent's bits all ones ----------------------------
 __device__ __forceinline__ bool pg_bad16(uint32_t x) { return (x & 0x7f80u) == 0x7f80u; }
-__device__ __forceinline__ uint32_t pg_code16(uint32_t x) {
-  return !pg_bad16(x) ? 0u : (x & 0x7fu) ? 0x4680u : (x & 0x8000u) ? 0x4300u : 0x3f80u;
-}
 __device__ __forceinline__ uint32_t pg_clean16(uint32_t x) { return pg_bad16(x) ? 0u : x; }
 // f of both halves of a word
 template <class F>
 __device__ __forceinline__ uint32_t pg_both(uint32_t w, F f) { return f(w & 0xffffu) | (uint32_t)f(w >> 16) << 16; }
 __device__ __forceinline__ bool pg_bad32(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
-__device__ __forceinline__ float pg_code32(float v) {
-  const uint32_t x = __float_as_uint(v);
-  return !pg_bad32(v) ? 0.f : (x & 0x7fffffu) ? 16384.f : (x >> 31) ? 128.f : 1.f;
-}
-// What a count adds to a sum.
-__device__ __forceinline__ float pg_of_codes(float n) {
-  const uint32_t k = (uint32_t)n;
-  return !k ? 0.f : (k >> 14) || ((k & 127) && (k >> 7 & 127)) ? NAN : (k & 127) ? INFINITY : -INFINITY;
-}
 
 }  // namespace catekv

@@ -68,20 +68,13 @@ template <> struct Ops<uint16_t> {
       for (int i = 0; i < 4; ++i) b |= pg_both(word(v[r], i), [](uint32_t x) { return (uint32_t)pg_bad16(x); });
     return b != 0;
   }
-  static __device__ __forceinline__ void pv_clean(const uint4 (&v)[kV], const pg_f32x4& p, const pg_f32x4& seen, pg_f32x4 (&o)[8]) {
-    uint2 hi, lo;
-    split(p, hi, lo);
-    const uint2 one = make_uint2(pg_pack2(seen[0], seen[1]), pg_pack2(seen[2], seen[3]));
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint2 c = column(v, e);
-      const uint2 f = make_uint2(pg_both(c.x, pg_clean16), pg_both(c.y, pg_clean16));
-      const uint2 b = make_uint2(pg_both(c.x, pg_code16), pg_both(c.y, pg_code16));
-      o[e] = mul(f, lo, mul(f, hi, o[e]));
-      const pg_f32x4 n = mul(b, one, pg_f32x4{});
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[e][i] += pg_of_codes(n[i]);
-    }
+  static __device__ __forceinline__ uint4 clean(const uint4& v) {
+    return make_uint4(pg_both(v.x, pg_clean16), pg_both(v.y, pg_clean16), pg_both(v.z, pg_clean16), pg_both(v.w, pg_clean16));
+  }
+  // dims [d, d + 4) of a row
+  static __device__ __forceinline__ float4 four(const char* row, int d) {
+    const uint2 x = *reinterpret_cast<const uint2*>(row + d * 2);
+    return make_float4(bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y));
   }
   // dims of o[4 x .. 4 x + 3][i]
   static __device__ __forceinline__ int dim(int x, int k4, int i) { return 8 * (4 * k4 + i) + 4 * x; }
@@ -116,20 +109,11 @@ template <> struct Ops<float> {
       for (int i = 0; i < 4; ++i) b = b || pg_bad32(el(v[r], i));
     return b;
   }
-  static __device__ __forceinline__ void pv_clean(const uint4 (&v)[kV], const pg_f32x4& p, const pg_f32x4& seen, pg_f32x4 (&o)[8]) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      pg_f32x4 n = {};
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float x = el(v[2 * r + e / 4], e & 3);
-        o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(pg_bad32(x) ? 0.f : x, p[r], o[e], 0, 0, 0);
-        n = __builtin_amdgcn_mfma_f32_16x16x4f32(pg_code32(x), seen[r], n, 0, 0, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[e][i] += pg_of_codes(n[i]);
-    }
+  static __device__ __forceinline__ uint4 clean(const uint4& v) {
+    return make_uint4(pg_bad32(el(v, 0)) ? 0u : v.x, pg_bad32(el(v, 1)) ? 0u : v.y, pg_bad32(el(v, 2)) ? 0u : v.z,
+                      pg_bad32(el(v, 3)) ? 0u : v.w);
   }
+  static __device__ __forceinline__ float4 four(const char* row, int d) { return *reinterpret_cast<const float4*>(row + d * 4); }
   static __device__ __forceinline__ int dim(int x, int k4, int i) { return 4 * (4 * k4 + i) + 64 * x; }
 };
 
@@ -229,33 +213,44 @@ void paged_stream_kernel(PagedAttn a) {
     pg_f32x4 o[8];
     float m, l;
     float cw;                                         // of the weights: pg_factor()
+    bool purged;                                      // a tile of the segment, in the wave
     int cur = 0;
     auto begin = [&]() __attribute__((always_inline)) {
       m = -INFINITY;
       l = 0.f;
       cw = cs;
+      purged = false;
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = pg_f32x4{};
+      if (sizeof(T) == 2)
 #pragma unroll
-      for (int i = 0; i < X::kK; ++i) q[i] = s_q[cur][n16][i * 4 + k4];
+        for (int i = 0; i < X::kK; ++i) q[i] = s_q[cur][n16][i * 4 + k4];
     };
     auto consume = [&](auto tag) __attribute__((always_inline)) {
       constexpr int B = decltype(tag)::value;
       const Seg& sg = s_seg[cur];
       const int tile = tile_of[B];
+      if (sizeof(T) == 4)                               // registers are few: the new rows come from LDS each time
+#pragma unroll
+        for (int i = 0; i < X::kK; ++i) q[i] = s_q[cur][n16][i * 4 + k4];
       pg_f32x4 s = X::score(kb[B], q);
       const bool masked = tile + kTile > sg.see0;       // the first token does not see all of it
       const int see = min(sg.see0 + n16 / G, sg.t_end);
-      pg_f32x4 seen = {1.f, 1.f, 1.f, 1.f};
       if (masked) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int t = tile + 4 * k4 + r;
           s[r] = t < see ? s[r] : -INFINITY;
-          seen[r] = t < see ? 1.f : 0.f;
           if (t >= sg.t_end)
 #pragma unroll
             for (int x = 0; x < X::kVPer; ++x) vb[B][r * X::kVPer + x] = make_uint4(0, 0, 0, 0);
+        }
+        // 0 * NaN is NaN: V that is not finite, and that some of the tokens do not see, is left
+        // out here and added to the sums of those that do at the segment's end
+        if (sg.rows > G && __builtin_amdgcn_ballot_w64(X::any_bad(vb[B]))) {
+          purged = true;
+#pragma unroll
+          for (int i = 0; i < X::kV; ++i) vb[B][i] = X::clean(vb[B][i]);
         }
       }
       float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
@@ -277,11 +272,31 @@ void paged_stream_kernel(PagedAttn a) {
         p[r] = fast_exp2(__builtin_fmaf(s[r], cw, -mc));
         l += p[r];
       }
-      if (masked && __builtin_amdgcn_ballot_w64(X::any_bad(vb[B]))) X::pv_clean(vb[B], p, seen, o);
-      else X::pv(vb[B], p, o);
+      X::pv(vb[B], p, o);
     };
     // The waves' parts of segment cur joined; its result or partial slot written.
     auto finish = [&]() __attribute__((always_inline)) {
+      if (purged) {
+        const Seg& sg = s_seg[cur];
+        const int see = min(sg.see0 + n16 / G, sg.t_end);
+#pragma unroll 1
+        for (int u = wave; u < sg.n_units; u += kWaves) {
+          const int tile = sg.t0 + u * kTile;
+          if (tile + kTile <= sg.see0) continue;        // all tokens see it: taken as it was
+          const size_t base = (pg_page(c, pg_entry(c.table + (size_t)sg.view * c.max_pages, tile >> c.page_log)) + (tile & mask)) * RB;
+#pragma unroll 1
+          for (int r = 0; r < min(kTile, sg.t_end - tile); ++r)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float4 z = X::four(c.v + base + (size_t)r * RB, X::dim(x, k4, i));
+                const float f[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[4 * x + e][i] += tile + r < see && pg_bad32(f[e]) ? f[e] : 0.f;
+              }
+        }
+      }
       l = add_xor32(add_xor16(l));
       barrier_lds_only();                             // the join before has been read
 #pragma unroll
