@@ -184,6 +184,18 @@ Deal deal(const std::vector<Tile>& tiles, int64_t share, int workers, const Tile
   return d;
 }
 
+// What a deal in parts of at most `share` units costs at least.
+double least_cost(const std::vector<Tile>& tiles, int64_t share, int workers, const TileCosts& k) {
+  int64_t units = 0, pieces = 0, slots = 0;
+  for (const Tile& t : tiles) {
+    const int64_t parts = share ? (t.units + share - 1) / share : 1;
+    units += t.units;
+    pieces += parts;
+    slots += parts > 1 ? parts : 0;
+  }
+  return (k.unit * (double)units + k.piece * (double)pieces) / workers + (slots ? k.join + k.slot * (double)slots : 0.0);
+}
+
 // All tiles end to end, cut into equal shares; neighbours lie in one engine.  No part
 // is shorter than half a piece's way in and out.
 Deal deal_line(const std::vector<Tile>& tiles, int workers, const TileCosts& k) {
@@ -293,14 +305,17 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
     const TileCosts& costs = half ? kTileCosts : kTileCostsF32;
     const int workers = half ? cus : 2 * cus;
     Deal best = deal(tiles, 0, workers, costs);
-    if (n_tiles < 8 * (int64_t)workers) {
+    // (a whole tile's way is not left for less than a twentieth)
+    if (n_tiles < 8 * (int64_t)workers && best.cost > 1.05 * least_cost(tiles, 0, workers, costs)) {
       const int64_t even = (tile_units + workers - 1) / workers;
-      for (int k = 2; k <= 8; ++k) {                 // shares of 2 to 1/2 of an equal one
-        Deal d = deal(tiles, std::max<int64_t>(1, (4 * even + k - 1) / k), workers, costs);
-        if (d.cost < best.cost) best = std::move(d);
-      }
       Deal d = deal_line(tiles, workers, costs);
       if (d.cost < best.cost) best = std::move(d);
+      for (int k = 2; k <= 8; ++k) {                 // shares of 2 to 1/2 of an equal one
+        const int64_t share = std::max<int64_t>(1, (4 * even + k - 1) / k);
+        if (least_cost(tiles, share, workers, costs) >= best.cost) continue;
+        d = deal(tiles, share, workers, costs);
+        if (d.cost < best.cost) best = std::move(d);
+      }
     }
     std::vector<int> parts(tiles.size(), 0);
     for (const Cut& c : best.cuts) ++parts[c.tile];

@@ -37,7 +37,8 @@ __device__ __forceinline__ void release(const PagedCache& c, int id) {
 
 // ---- scans within a workgroup of kTakeThreads -----------------------------------
 
-// Sum of x over the threads before this one; total: over all.  Two barriers.
+// Sum of x over the threads before this one; total: over all.  Two barriers, which wait
+// for LDS alone: stores to memory keep flowing.
 __device__ __forceinline__ int scan_block(int x, int* s_wave, int& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int v = x;
@@ -47,7 +48,7 @@ __device__ __forceinline__ int scan_block(int x, int* s_wave, int& total) {
     if (lane >= o) v += y;
   }
   if (lane == 63) s_wave[wave] = v;
-  __syncthreads();
+  barrier_lds_only();
   int before = 0, all = 0;
 #pragma unroll
   for (int w = 0; w < kTakeWaves; ++w) {
@@ -55,7 +56,7 @@ __device__ __forceinline__ int scan_block(int x, int* s_wave, int& total) {
     if (w < wave) before += y;
     all += y;
   }
-  __syncthreads();
+  barrier_lds_only();
   total = all;
   return before + v - x;
 }
@@ -98,7 +99,8 @@ __device__ int find_free(const PagedCache& c, uint64_t word, int need, int32_t* 
     }
     found += total;
   }
-  __syncthreads();
+  if (need > kTakeLds) __syncthreads();          // takes is read back
+  else barrier_lds_only();
   return found < need ? found : need;
 }
 
@@ -148,7 +150,7 @@ __global__ __launch_bounds__(kTakeThreads) void paged_take_kernel(PagedAppend a)
   for (int s0 = 0; s0 < a.n_seqs; s0 += per) {
     const bool mine = si < per && s0 + si < a.n_seqs;
     if (tid < per) s_bad[tid] = 0;
-    __syncthreads();
+    barrier_lds_only();
     t = PagedTake{-1, 0, -1};
     need = 0;
     if (mine) {
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(kTakeThreads) void paged_take_kernel(PagedAppend a)
         }
       }
     }
-    __syncthreads();
+    barrier_lds_only();
     if (mine && s_bad[si]) {
       need = 0;
       t.len = -1;
@@ -184,6 +186,7 @@ __global__ __launch_bounds__(kTakeThreads) void paged_take_kernel(PagedAppend a)
     if (mine && !once) a.views[(s0 + si) * hkv + h] = t;
   }
   const int found = total > 0 ? find_free(c, word, total, a.takes, s) : 0;
+  if (!once) __syncthreads();                    // views are read back
   // a sequence whose last page was not found is left, and all after it that need any
   for (int s0 = 0; s0 < a.n_seqs; s0 += per) {
     const bool mine = si < per && s0 + si < a.n_seqs;
@@ -197,9 +200,9 @@ __global__ __launch_bounds__(kTakeThreads) void paged_take_kernel(PagedAppend a)
       }
     }
     if (tid < per) s_end[tid] = 0;       // past the last page that the sequence needs
-    __syncthreads();
+    barrier_lds_only();
     if (mine && need > 0) atomicMax(&s_end[si], t.start + need);
-    __syncthreads();
+    barrier_lds_only();
     if (mine) {
       if (t.len >= 0) {
         if (s_end[si] > found) {
@@ -212,14 +215,15 @@ __global__ __launch_bounds__(kTakeThreads) void paged_take_kernel(PagedAppend a)
       }
       a.views[v] = t;
     }
-    __syncthreads();
+    barrier_lds_only();
   }
   mark_taken(c, a.takes, s_used, s);
-  __syncthreads();
+  // other pages than those: in any order
   if (once) {
     if (si < per && si < a.n_seqs && t.len >= 0 && t.from >= 0) release(c, t.from);
     return;
   }
+  __syncthreads();
   for (int v = tid; v < a.n_seqs * hkv; v += kTakeThreads) {
     const PagedTake u = a.views[v];
     if (u.len >= 0 && u.from >= 0) release(c, u.from);
