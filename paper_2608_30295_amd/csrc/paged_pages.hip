@@ -61,11 +61,10 @@ __device__ __forceinline__ int scan_block(int x, int* s_wave, int& total) {
   return before + v - x;
 }
 
-// Up to kTakeLds of the pages found stay in LDS, too.
-constexpr int kTakeLds = 4096;
 struct TakeLds {
   int wave[kTakeWaves];
-  int page[kTakeLds];
+  int before[kTakeThreads];
+  uint64_t word[kTakeThreads];
 };
 
 // Word number `at` of the free pages' bits.
@@ -75,40 +74,47 @@ __device__ __forceinline__ uint64_t free_word(const PagedCache& c, int at) {
   return last < 64 && last > 0 ? b & ((1ull << last) - 1) : b;
 }
 
-// The numbers of the lowest `need` free pages into takes; returns how many there
-// are, at most need.  Nothing is marked yet.  A thread counts a word (the first turn's
-// given: asked for before it was known what is needed); then a wave goes over those of its
-// 64 words that give pages, a lane per bit.
-__device__ int find_free(const PagedCache& c, uint64_t word, int need, int32_t* takes, TakeLds& s) {
-  const int words = (c.n_pages + 63) >> 6, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Takes the lowest `need` free pages, or all that there are; returns how many.  A thread
+// counts a word (the first turn's given: asked for before it was known what is needed);
+// then the waves go over the words up to the last that is needed, every sixteenth each,
+// a lane per bit.  A word has one writer, so that its bits go with a plain store.
+__device__ int take_free(const PagedCache& c, uint64_t word, int need, int32_t* takes, TakeLds& s) {
+  const int words = (c.n_pages + 63) >> 6, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int found = 0;
   for (int w0 = 0; w0 < words && found < need; w0 += kTakeThreads) {
-    if (w0 > 0) word = free_word(c, w0 + (int)threadIdx.x);
+    if (w0 > 0) word = free_word(c, w0 + tid);
     int total;
     const int before = found + scan_block(__popcll(word), s.wave, total);
-    for (uint64_t give = __builtin_amdgcn_ballot_w64(word != 0 && before < need); give; give &= give - 1) {
-      const int i = __ffsll((unsigned long long)give) - 1;
-      const uint64_t b = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(word >> 32), i) << 32 |
-                         (uint32_t)__builtin_amdgcn_readlane((uint32_t)word, i);
-      const int place = __builtin_amdgcn_readlane(before, i) + __popcll(b & ((1ull << lane) - 1));
-      if ((b >> lane & 1) && place < need) {
-        const int p = (w0 + wave * 64 + i) * 64 + lane;
+    s.word[tid] = word;
+    s.before[tid] = before;
+    barrier_lds_only();
+    for (int i = wave; i < kTakeThreads; i += kTakeWaves) {
+      const int first = __builtin_amdgcn_readfirstlane(s.before[i]);
+      if (first >= need) break;
+      const uint64_t b = s.word[i];
+      const int place = first + __popcll(b & ((1ull << lane) - 1));
+      const bool mine = (b >> lane & 1) && place < need;
+      const uint64_t gone = __builtin_amdgcn_ballot_w64(mine);
+      if (mine) {
+        const int p = (w0 + i) * 64 + lane;
         takes[place] = p;
-        if (place < kTakeLds) s.page[place] = p;
+        c.refs[p] = 1;
       }
+      if (lane == 0 && gone) c.bits[w0 + i] = b & ~gone;
     }
     found += total;
+    barrier_lds_only();
   }
-  if (need > kTakeLds) __syncthreads();          // takes is read back
-  else barrier_lds_only();
   return found < need ? found : need;
 }
 
-__device__ void mark_taken(const PagedCache& c, const int32_t* takes, int n, const TakeLds& s) {
-  for (int j = threadIdx.x; j < n; j += kTakeThreads) {
-    const int p = j < kTakeLds ? s.page[j] : takes[j];
-    c.refs[p] = 1;
-    atomicAnd((unsigned long long*)&c.bits[p >> 6], ~(1ull << (p & 63)));
+// The pages [n, found) of those taken are free again.
+__device__ void give_back(const PagedCache& c, const int32_t* takes, int n, int found) {
+  __syncthreads();
+  for (int j = n + (int)threadIdx.x; j < found; j += kTakeThreads) {
+    const int p = takes[j];
+    c.refs[p] = 0;
+    atomicOr((unsigned long long*)&c.bits[p >> 6], 1ull << (p & 63));
   }
 }
 
@@ -185,8 +191,8 @@ __global__ __launch_bounds__(kTakeThreads) void paged_take_kernel(PagedAppend a)
     total += sum;
     if (mine && !once) a.views[(s0 + si) * hkv + h] = t;
   }
-  const int found = total > 0 ? find_free(c, word, total, a.takes, s) : 0;
-  if (!once) __syncthreads();                    // views are read back
+  const int found = total > 0 ? take_free(c, word, total, a.takes, s) : 0;
+  bool copies = false;
   // a sequence whose last page was not found is left, and all after it that need any
   for (int s0 = 0; s0 < a.n_seqs; s0 += per) {
     const bool mine = si < per && s0 + si < a.n_seqs;
@@ -199,31 +205,34 @@ __global__ __launch_bounds__(kTakeThreads) void paged_take_kernel(PagedAppend a)
         if (t.len >= 0) need = pages_of(c, t.len + q.n_new) - pages_of(c, t.len) + (t.from >= 0);
       }
     }
-    if (tid < per) s_end[tid] = 0;       // past the last page that the sequence needs
-    barrier_lds_only();
-    if (mine && need > 0) atomicMax(&s_end[si], t.start + need);
-    barrier_lds_only();
-    if (mine) {
-      if (t.len >= 0) {
+    if (found < total) {
+      if (tid < per) s_end[tid] = 0;     // past the last page that the sequence needs
+      barrier_lds_only();
+      if (mine && need > 0) atomicMax(&s_end[si], t.start + need);
+      barrier_lds_only();
+      if (mine && t.len >= 0) {
         if (s_end[si] > found) {
           t.len = -1;
           if (a.overflow) *a.overflow = 1;
-        } else {
-          c.lens[q.slot * hkv + h] = t.len + q.n_new;
-          if (need > 0) atomicMax(&s_used, t.start + need);
+        } else if (need > 0) {
+          atomicMax(&s_used, t.start + need);
         }
       }
+      barrier_lds_only();
+    }
+    if (mine) {
+      if (t.len >= 0) c.lens[q.slot * hkv + h] = t.len + q.n_new;
+      copies |= t.len >= 0 && t.from >= 0;
       a.views[v] = t;
     }
-    barrier_lds_only();
   }
-  mark_taken(c, a.takes, s_used, s);
-  // other pages than those: in any order
+  if (found < total) give_back(c, a.takes, s_used, found);
+  // what is left of shared pages, once the bits above are stored
+  if (!__syncthreads_or(copies)) return;
   if (once) {
-    if (si < per && si < a.n_seqs && t.len >= 0 && t.from >= 0) release(c, t.from);
+    if (t.len >= 0 && t.from >= 0) release(c, t.from);
     return;
   }
-  __syncthreads();
   for (int v = tid; v < a.n_seqs * hkv; v += kTakeThreads) {
     const PagedTake u = a.views[v];
     if (u.len >= 0 && u.from >= 0) release(c, u.from);
@@ -387,7 +396,7 @@ __global__ __launch_bounds__(kTakeThreads) void paged_compact_take_kernel(PagedC
   }
   __syncthreads();
   const int total = s_total;
-  const int found = total > 0 ? find_free(c, word, total, a.takes, s_find) : 0;
+  const int found = total > 0 ? take_free(c, word, total, a.takes, s_find) : 0;
   // the first view that does not find its pages and all after it that need any stay
   if (tid == 0) {
     int used = 0;
@@ -406,7 +415,7 @@ __global__ __launch_bounds__(kTakeThreads) void paged_compact_take_kernel(PagedC
   }
   __syncthreads();
   if (tid < a.n_sel) a.views[tid] = s_take[tid];
-  mark_taken(c, a.takes, s_used, s_find);
+  if (s_used < found) give_back(c, a.takes, s_used, found);
 }
 
 template <int LPR>
