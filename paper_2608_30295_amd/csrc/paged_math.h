@@ -24,6 +24,11 @@ __device__ __forceinline__ float pg_factor(float m, float c) {
   return fabsf(m) * c < 536870912.f || m == -INFINITY ? c : __uint_as_float(__float_as_uint(c) & 0x7f800000u);
 }
 
+// A row's maximum as results and partial slots take it, in units of log2.  -inf stands for
+// a row without scores above -inf, whose sum is 0; where all scores are NaN the maximum stays
+// at -inf, too, but the sum is NaN and has to come through.
+__device__ __forceinline__ float pg_top(float m, float l, float c) { return m > -INFINITY ? m * c : l != l ? 0.f : -INFINITY; }
+
 // bf16 pair (to nearest, ties to even) of two fp32 values, x in the low half.
 __device__ __forceinline__ uint32_t pg_pack2(float x, float y) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((pg_f32x2{x, y}), pg_bf16x2));

@@ -306,7 +306,7 @@ void paged_stream_kernel(PagedAttn a) {
           *reinterpret_cast<float4*>(&s_o[wave][n16][X::dim(x, k4, i)]) =
               make_float4(o[4 * x][i], o[4 * x + 1][i], o[4 * x + 2][i], o[4 * x + 3][i]);
       if (k4 == 0) {
-        s_m[wave][n16] = m == -INFINITY ? -INFINITY : m * cs;
+        s_m[wave][n16] = pg_top(m, l, cs);
         s_l[wave][n16] = l;
       }
       barrier_lds_only();

@@ -431,8 +431,8 @@ void paged_tile_kernel(PagedAttn a) {
       const int hi = lane >> 5, tok = row / G;
       const size_t qrow = ((size_t)(x.tok0 + tok) * a.hq + (x.view % c.hkv) * G + (row - tok * G)) * kRB;
       const float sum = add_xor32(l);                  // lanes l and l ^ 32 hold the same row
-      const bool none = m == -INFINITY;
-      const float mc = none ? -INFINITY : m * cs;
+      const float mc = pg_top(m, sum, cs);
+      const bool none = mc == -INFINITY;
       if (x.slot >= 0) {
         float* slot = a.slots + (size_t)x.slot * 4;
 #pragma unroll

@@ -185,8 +185,8 @@ void paged_tile_f32_kernel(PagedAttn a) {
     }
     if (!mine) continue;
     l = add_xor32(l);                                  // lanes l and l ^ 32 hold the same row
-    const bool none = m == -INFINITY;
-    const float mc = none ? -INFINITY : m * cs;
+    const float mc = pg_top(m, l, cs);
+    const bool none = mc == -INFINITY;
     // a partial result is taken as it is, a whole one divided by its sum
     const bool part = pc.slot >= 0;
     const float inv = part ? 1.f : none ? 0.f : 1.f / l;

@@ -333,6 +333,23 @@ def test_scores_of_any_size(dtype, new):
     assert (out == 0).all() and (lse == -math.inf).all()
 
 
+@pytest.mark.parametrize("dtype,n,new,G", [(BF16, 100, 1, 4), (BF16, 20000, 1, 4), (BF16, 900, 60, 2), (BF16, 6000, 300, 2),
+                                           (F32, 100, 2, 1), (F32, 20000, 2, 1), (F32, 900, 60, 4), (F32, 4000, 120, 4)])
+def test_scores_that_are_all_nan_are_not_those_of_no_row(dtype, n, new, G):
+    """A query that is NaN, in views that are one piece and in cut ones: its results are NaN,
+    its neighbours' are not."""
+    hkv = 2
+    c, s = cache_of(2 * -(-n // 64) + 2 * -(-new // 64) + 4, 64, 1, hkv, -(-(n + new) // 64) + 1, dtype)
+    append(c, s, [0], [n], hkv * G, 21)
+    plan = append(c, s, [0], [new], hkv * G, 22)
+    q = randn((new, hkv * G, 128), 23, dtype)
+    q[new // 2, 1, 5] = float("nan")
+    q[new - 1, hkv * G - 1] = float("nan")
+    out, lse = check_attention(c, plan, [0], [new], hkv * G, 23, q=q)
+    nan = torch.isnan(out.float()).all(-1)
+    assert nan[new // 2, 1] and nan[new - 1, hkv * G - 1] and int(nan.sum()) == len({(new // 2, 1), (new - 1, hkv * G - 1)})
+
+
 @pytest.mark.parametrize("dtype,n,new,G", [(BF16, 20000, 1, 4), (BF16, 9000, 4, 8), (BF16, 6000, 300, 2), (F32, 5000, 2, 1),
                                            (F32, 3001, 150, 4)])
 def test_long_views_are_cut_and_joined(dtype, n, new, G):
