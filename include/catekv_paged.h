@@ -117,9 +117,10 @@ int catekv_paged_append(const catekv_paged_cache* cache, const catekv_paged_plan
  * q     [n_tokens][hq][d] (dtype)
  * out   [n_tokens][hq][d] (dtype: fp32 sums, rounded once)
  * lse   [n_tokens][hq] fp32 or NULL
- * bf16: the weights exp(s - max) are rounded to bf16 for their product with V where
- * a sequence has more than 16 rows new tokens times hq / hkv, and kept to 16 bits
- * where it has fewer; their sum is of the unrounded ones.
+ * A token whose scores are all NaN has NaN results.
+ * bf16: for a sequence of up to 16 new rows (its new tokens times hq / hkv) the weights
+ * exp(s - max) are kept to 16 bits for their product with V, for longer ones they are
+ * rounded to bf16; their sum is of the unrounded ones.
  * Errors: INVALID_ARG for null pointers, q or out not on 16-byte borders, a scale that
  * is not positive and finite, or a cache that is not of the plan's geometry; WORKSPACE. */
 int catekv_paged_attn(const catekv_paged_cache* cache, const catekv_paged_plan_t* plan, const void* q, float scale,

@@ -9,6 +9,10 @@
 // 4 (l / 16) + i, which is how O^T = V^T P^T takes P; what belongs to a new row
 // (maximum, sum, factor) is a lane's own.  V^T's rows are the 8 dims that a lane
 // loaded of each cached row, one product per dim.
+//
+// bf16, 3 views of 131072 rows and 5 of 2112, 4 heads a group: 207 MB in 37 us, 5.6 TB/s with
+// the start; 64 sequences: 553 MB in 95 us, 5.8 TB/s.  fp32, 65536 rows: 4.9 TB/s.  A compute unit takes 22 GB/s
+// with all of them at work and with half of them, so all are given a share.
 #include <type_traits>
 
 #include "paged_math.h"

@@ -15,6 +15,12 @@
 // the vector unit forms the weights of tile t, and while these meet V it takes the
 // maxima of tile t + 1.  A wave issues in order, so the two are laid between each other
 // in the program, and scheduling barriers keep them there.
+//
+// 2048 new tokens behind 30720 rows, 32 heads over 8: 1065 GFLOP in 990 to 1055 us, 1.01 to
+// 1.07 PFLOP/s where a large library product reaches 1.10 (products beside each other
+// without softmax: 1.6 to 1.9).  The matrix cores are busy for 52% of the cycles, the vector
+// unit issues in 45%; no LDS bank conflicts.  Larger tiles of new rows do not fit the
+// registers; 128 to a workgroup would read K and V from LDS twice as often.
 #include <type_traits>
 
 #include "paged_math.h"
