@@ -296,45 +296,48 @@ void paged_tile_kernel(PagedAttn a) {
     next = after;
     after = fetch(x, t + 3);
     own();
-    uint4 p[4];
-    if (MASK) {
-      look(vt);
-      if (!idle) {
-        scores(kt, s2);
-        weights(s, p);
-      }
-      purge(vt);
-      if (idle) return;
-      product(vt, p);
-      hide(s2, x.t0 + (t + 1) * kTile);
-      raise(maximum(s2));
-      return;
-    }
-    if (idle) return;
+    const bool part = MASK && t >= x.n_full;           // some new rows do not see all of V's tile
+    if (part) look(vt);
     // Operands come in fours, one four ahead: their wait is then for reads that have had
     // four products' time (a wait counts all LDS reads on their way).  A product leaves the
     // vector unit room for four instructions or so: two weights beside each of the scores'
     // first twelve and of V's first four, the maxima beside V's (all weights beside the
     // scores' products, four beside every other one: 1.4% longer).
-    const float mc = reference();
-    uint4 f[2][4];
+    uint4 p[4], f[2][4];
+    if (!idle) {
+      const float mc = reference();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[0][i] = k_op(kt, i & 1, i >> 1, ka);
-    s2[0] = s2[1] = f32x16{};
+      for (int i = 0; i < 4; ++i) f[0][i] = k_op(kt, i & 1, i >> 1, ka);
+      s2[0] = s2[1] = f32x16{};
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        f[(y + 1) & 1][i] = y < 3 ? k_op(kt, i & 1, 2 * y + 2 + (i >> 1), ka) : v_op(vt, 0, i, va);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int y = 0; y < 4; ++y) {
         __builtin_amdgcn_sched_barrier(0);
-        s2[i & 1] = mfma(f[y & 1][i], q[2 * y + (i >> 1)], s2[i & 1]);
-        if (y < 3) weights2(s, 4 * y + i, mc);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (y < 3) f[(y + 1) & 1][i] = k_op(kt, i & 1, 2 * y + 2 + (i >> 1), ka);
+          else if (!MASK) f[0][i] = v_op(vt, 0, i, va);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          __builtin_amdgcn_sched_barrier(0);
+          s2[i & 1] = mfma(f[y & 1][i], q[2 * y + (i >> 1)], s2[i & 1]);
+          if (y < 3) weights2(s, 4 * y + i, mc);
+        }
+        if (y < 3) p[y] = pack16(s, y);
       }
-      if (y < 3) p[y] = pack16(s, y);
+      if (MASK) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) weights2(s, 12 + i, mc);
+        p[3] = pack16(s, 3);
+      }
     }
+    if (part) purge(vt);
+    if (idle) return;
+    if (MASK) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[0][i] = v_op(vt, 0, i, va);
+      hide(s2, x.t0 + (t + 1) * kTile);
+    }
+    const float mc = reference();
     float mx = -INFINITY;
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
@@ -346,8 +349,8 @@ void paged_tile_kernel(PagedAttn a) {
       for (int i = 0; i < 4; ++i) {
         __builtin_amdgcn_sched_barrier(0);
         o[i] = mfma(f[y & 1][i], p[y], o[i]);
-        if (y == 0) weights2(s, 12 + i, mc);
-        if (y == 1 && i == 0) p[3] = pack16(s, 3);
+        if (!MASK && y == 0) weights2(s, 12 + i, mc);
+        if (!MASK && y == 1 && i == 0) p[3] = pack16(s, 3);
         const int z = 4 * y + i;
         mx = fmaxf(fmaxf(mx, s2[z >> 3][(z & 7) * 2]), s2[z >> 3][(z & 7) * 2 + 1]);
       }
