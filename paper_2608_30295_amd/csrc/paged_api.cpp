@@ -116,13 +116,13 @@ struct Plan {
 // idle while another's queue (2048 tokens at 32K in 376 pieces of unequal length: 1280 us
 // where its longest share takes 890).
 //
-// What the ways to cut are compared by, in us as measured: a unit (64 cached rows; fp32
+// What the ways to cut are compared by, in us as measured: a unit (64 cached rows; fp32: 32,
 // with two workgroups to a compute unit), a piece's way in and out, the joining launch
 // and a partial result's way to memory and back.
 struct TileCosts {
   double unit, piece, join, slot;
 };
-constexpr TileCosts kTileCosts = {1.8, 7.0, 6.0, 0.07}, kTileCostsF32 = {14.0, 12.0, 6.0, 0.035};
+constexpr TileCosts kTileCosts = {1.8, 7.0, 6.0, 0.07}, kTileCostsF32 = {7.5, 12.0, 6.0, 0.035};
 constexpr int kXcds = 8;               // a worker's engine is its number modulo this
 
 struct Tile {
@@ -196,26 +196,27 @@ double least_cost(const std::vector<Tile>& tiles, int64_t share, int workers, co
   return (k.unit * (double)units + k.piece * (double)pieces) / workers + (slots ? k.join + k.slot * (double)slots : 0.0);
 }
 
-// All tiles end to end, cut into equal shares; neighbours lie in one engine.  No part
-// is shorter than half a piece's way in and out.
+// All tiles end to end, cut into shares that take as long; neighbours lie in one engine.  No
+// part is shorter than half a piece's way in and out.
 Deal deal_line(const std::vector<Tile>& tiles, int workers, const TileCosts& k) {
   Deal d;
-  int64_t left = 0;
-  for (const Tile& t : tiles) left += t.units;
+  int64_t units = 0;
+  for (const Tile& t : tiles) units += t.units;
+  const double share = (k.unit * (double)units + k.piece * (double)(tiles.size() + workers)) / workers;
   const int64_t least = std::max<int64_t>(1, (int64_t)(k.piece / k.unit / 2));
   const int per = std::max(1, workers / kXcds);
+  double spent = 0;
   size_t i = 0;
   int64_t off = 0;
   for (int s = 0; s < workers && i < tiles.size(); ++s) {
-    int64_t want = std::max<int64_t>(least, (left + workers - s - 1) / (workers - s));
     const bool last = s == workers - 1;
     const int w = workers % kXcds == 0 ? s % per * kXcds + s / per : s;
-    while (i < tiles.size() && (want >= least || last)) {
-      const int64_t rest = tiles[i].units - off;
-      int64_t take = last || rest <= want + least ? rest : want;
+    while (i < tiles.size()) {
+      const int64_t room = (int64_t)std::floor(((s + 1) * share - spent - k.piece) / k.unit + 0.5);
+      if (room < least && !last) break;
+      const int64_t rest = tiles[i].units - off, take = last || rest <= room + least ? rest : room;
       d.cuts.push_back({(int)i, off, off + take, w});
-      want -= take;
-      left -= take;
+      spent += k.piece + k.unit * (double)take;
       off += take;
       if (off == tiles[i].units) {
         ++i;
@@ -255,7 +256,7 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
   if (!launch_fits((tokens * hkv * lanes + 255) / 256 + (int64_t)n_seqs * hkv, 256) || P.takes > INT32_MAX)
     return fail(CATEKV_ERR_UNSUPPORTED, "%lld tokens of %d heads: too many for one launch", (long long)tokens, hkv);
 
-  // Work counts in units of kPagedUnit cached rows.  A view's new rows are one piece of
+  // Work counts in units of kPagedUnit cached rows, fp32 tiles' in halves of that.  A view's new rows are one piece of
   // the stream kernel if they are few, or tiles of the other one.
   const int R = paged_tile_rows(c->dtype), cus = device_cus();
   auto few = [&](int i) { return (int64_t)n_new[i] * G <= kStreamRows; };
@@ -263,7 +264,8 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
     const int64_t last = std::min<int64_t>(row0 + rows, (int64_t)n_new[i] * G) - 1;
     return std::max<int64_t>(0, max_rows[(int64_t)i * hkv + h] - n_new[i] + 1 + last / G);
   };
-  auto units_of = [](int64_t rows) { return std::max<int64_t>(1, (rows + kPagedUnit - 1) / kPagedUnit); };
+  const int unit = c->dtype == CATEKV_BF16 ? kPagedUnit : kPagedUnit / 2;
+  auto units_of = [](int64_t rows, int each) { return std::max<int64_t>(1, (rows + each - 1) / each); };
   auto piece = [&](int i, int h, int64_t row0) {
     PagedPiece p{};
     p.view = slots[i] * hkv + h;
@@ -284,10 +286,10 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
   for (int i = 0; i < n_seqs; ++i)
     for (int h = 0; n_new[i] > 0 && h < hkv; ++h) {
       if (few(i)) {
-        few_units += units_of(rows_seen(i, h, 0, kStreamRows));
+        few_units += units_of(rows_seen(i, h, 0, kStreamRows), kPagedUnit);
         continue;
       }
-      for (int64_t r = 0; r < (int64_t)n_new[i] * G; r += R, ++n_tiles) tile_units += units_of(rows_seen(i, h, r, R));
+      for (int64_t r = 0; r < (int64_t)n_new[i] * G; r += R, ++n_tiles) tile_units += units_of(rows_seen(i, h, r, R), unit);
     }
   if (n_tiles > (int64_t)1 << 22) return fail(CATEKV_ERR_UNSUPPORTED, "%lld tiles of new rows: too many for one launch", (long long)n_tiles);
 
@@ -299,7 +301,7 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
       for (int h = 0; n_new[i] > 0 && !few(i) && h < hkv; ++h)
         for (int64_t r = 0; r < (int64_t)n_new[i] * G; r += R) {
           const int64_t rows = rows_seen(i, h, r, R);
-          tiles.push_back({piece(i, h, r), rows, units_of(rows)});
+          tiles.push_back({piece(i, h, r), rows, units_of(rows, unit)});
         }
     const bool half = c->dtype == CATEKV_BF16;
     const TileCosts& costs = half ? kTileCosts : kTileCostsF32;
@@ -332,8 +334,8 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
     for (const Cut& c : best.cuts) {
       while ((int)P.tile_workers.size() <= c.worker) P.tile_workers.push_back((int32_t)P.tiles.size());
       PagedPiece p = tiles[c.tile].p;
-      p.t0 = (int32_t)(c.u0 * kPagedUnit);
-      p.t1 = (int32_t)std::min<int64_t>(tiles[c.tile].rows, c.u1 * kPagedUnit);
+      p.t0 = (int32_t)(c.u0 * unit);
+      p.t1 = (int32_t)std::min<int64_t>(tiles[c.tile].rows, c.u1 * unit);
       p.slot = -1;
       if (parts[c.tile] > 1) {
         p.slot = (int32_t)slot[c.tile];
@@ -356,7 +358,7 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
     open();
     for (int i = 0; i < n_seqs; ++i)
       for (int h = 0; n_new[i] > 0 && few(i) && h < hkv; ++h) {
-        const int64_t rows = rows_seen(i, h, 0, kStreamRows), u = units_of(rows);
+        const int64_t rows = rows_seen(i, h, 0, kStreamRows), u = units_of(rows, kPagedUnit);
         const size_t begin = P.segs.size();
         PagedPiece p = piece(i, h, 0);
         for (int64_t off = 0; off < u;) {
