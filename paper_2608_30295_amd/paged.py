@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+from array import array
 from dataclasses import dataclass, field
 from typing import Optional, Sequence, Tuple
 
@@ -19,10 +20,16 @@ import torch
 
 from . import _lib
 from ._lib import check, lib
-from .binding import D, _dtype_code, _heads_arg, workspace
+from .binding import D, _dtype_code, workspace
 from .cache import _bytes, _call, _device_of, _need, _need_table
 
 PAGES = (16, 32, 64, 128, 256)
+
+
+def _ints(x: Sequence[int]):
+    """int32 values for a host argument (slot lists are long: the array is filled in C)."""
+    a = array("i", x)
+    return (ctypes.c_int32 * len(a)).from_buffer(a) if a else (ctypes.c_int32 * 1)()
 
 
 @dataclass
@@ -189,7 +196,7 @@ def fork_paged(cache: PagedCache, src: Sequence[int], dst: Sequence[int], refuse
     index = _device_of(cache.table, refused)
     if refused is not None:
         _need(refused, "refused", torch.int32, 1)
-    _call(index, lib().catekv_paged_fork, cache.ref, _heads_arg(src), _heads_arg(dst), len(src),
+    _call(index, lib().catekv_paged_fork, cache.ref, _ints(src), _ints(dst), len(src),
           None if refused is None else refused.data_ptr())
 
 
@@ -221,7 +228,7 @@ def compact_kv_paged(cache: PagedCache, slot: int, heads: Sequence[int], idx: to
     b = idx.shape[1]
     if ws is None:
         ws = workspace(compact_paged_workspace(cache, len(heads), b, cs, tail), cache.device)
-    _call(index, lib().catekv_paged_compact, cache.ref, int(slot), _heads_arg(heads), len(heads), idx.data_ptr(), b,
+    _call(index, lib().catekv_paged_compact, cache.ref, int(slot), _ints(heads), len(heads), idx.data_ptr(), b,
           int(cs), int(tail), None if overflow is None else overflow.data_ptr(), ws.data_ptr(), _bytes(ws))
 
 
@@ -230,5 +237,5 @@ def gather_kv_paged(cache: PagedCache, slots: Sequence[int], kv_out: torch.Tenso
     kv_out (from kv_table, [n * hkv] views, rows in the cache's type; address 0: left
     out)."""
     _need_table(kv_out, len(slots) * cache.hkv)
-    _call(_device_of(cache.table, kv_out), lib().catekv_paged_gather, cache.ref, _heads_arg(slots), len(slots),
+    _call(_device_of(cache.table, kv_out), lib().catekv_paged_gather, cache.ref, _ints(slots), len(slots),
           kv_out.data_ptr(), int(max_rows))

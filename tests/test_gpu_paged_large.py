@@ -6,6 +6,7 @@ import torch
 
 import paged_ref as R
 import paper_2608_30295_amd as ck
+from test_gpu_paged import append, cache_of
 
 pytestmark = pytest.mark.gpu
 DEV, F32, BF16 = "cuda", torch.float32, torch.bfloat16
@@ -148,3 +149,22 @@ def test_batches_without_tokens(dtype):
     out, lse = ck.attn_paged(plan, c, torch.zeros((0, 4, 128), dtype=dtype, device=DEV))
     torch.cuda.synchronize()
     assert out.shape == (0, 4, 128) and lse.shape == (0, 4) and torch.equal(c.book, before) and over.item() == 0
+
+
+@pytest.mark.parametrize("dtype,b,cs", [(BF16, 512, 2), (BF16, 513, 2), (F32, 4097, 1), (BF16, 9001, 1)])
+def test_compaction_of_long_lists(dtype, b, cs):
+    """Lists around the border of the two ways to go over them, and of several turns of the
+    longer one: unordered, with gaps, repeats, chunks without rows and a partial last one."""
+    L, tail, page, hkv = 9100, 7, 64, 3
+    c, s = cache_of(3 * R.pages_of(L, page) + 2 * 160, page, 2, hkv, 160, dtype)
+    append(c, s, [1], [L], hkv, 5)
+    r = np.random.RandomState(b)
+    idx = r.randint(-2000, R.pages_of(L, cs) + 50, size=(2, b)).astype(np.int32)
+    idx[0, 0], idx[1, -1] = R.pages_of(L - tail, cs) - 1, 1 << 30
+    over = torch.zeros(1, dtype=torch.int32, device=DEV)
+    ck.compact_kv_paged(c, 1, [2, 0], torch.from_numpy(idx).to(DEV), cs, tail, over)
+    assert s.compact(1, [2, 0], idx, cs, tail) == bool(over.item()) == False                # noqa: E712
+    s.same(c)
+    ck.compact_kv_paged(c, 1, [0, 1], torch.zeros((2, 9000 + b), dtype=torch.int32, device=DEV), 2, tail, over)
+    assert s.compact(1, [0, 1], np.zeros((2, 9000 + b), np.int32), 2, tail) and over.item() == 1   # more than max_pages
+    s.same(c)
