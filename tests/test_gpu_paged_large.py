@@ -163,7 +163,7 @@ def test_compaction_of_long_lists(dtype, b, cs):
     idx[0, 0], idx[1, -1] = R.pages_of(L - tail, cs) - 1, 1 << 30
     over = torch.zeros(1, dtype=torch.int32, device=DEV)
     ck.compact_kv_paged(c, 1, [2, 0], torch.from_numpy(idx).to(DEV), cs, tail, over)
-    assert s.compact(1, [2, 0], idx, cs, tail) == bool(over.item()) == False                # noqa: E712
+    assert not s.compact(1, [2, 0], idx.tolist(), cs, tail) and over.item() == 0
     s.same(c)
     ck.compact_kv_paged(c, 1, [0, 1], torch.zeros((2, 9000 + b), dtype=torch.int32, device=DEV), 2, tail, over)
     assert s.compact(1, [0, 1], np.zeros((2, 9000 + b), np.int32), 2, tail) and over.item() == 1   # more than max_pages
