@@ -125,14 +125,18 @@ struct PagedAttn {
 constexpr int kTileThreads = 512;        // bf16; fp32: 256
 constexpr int kJoinThreads = 256;
 constexpr int kJoinRows = kJoinThreads / 32;   // rows of a joining workgroup, where rows have few parts
-inline int paged_join_rows(int parts) { return parts > 8 ? 1 : kJoinRows; }
+// Joins of one kind (tiles, few new rows): how many, workgroups of each, and whether a row
+// is shared by eight groups, which is so from more than 8 parts on.
+struct JoinShape {
+  int32_t n, blocks, deep;
+};
+inline JoinShape paged_join_shape(int n, int rows, int parts) { return {n, parts > 8 ? rows : (rows + kJoinRows - 1) / kJoinRows, parts > 8}; }
 // New rows of a tile piece at most, and the launch, per type.
 constexpr int kTileRows = 256, kTileRowsF32 = 128;
 inline int paged_tile_rows(int dtype) { return dtype == CATEKV_BF16 ? kTileRows : kTileRowsF32; }
 hipError_t launch_paged_tile(int G, const PagedAttn& a, hipStream_t stream);       // bf16
 hipError_t launch_paged_tile_f32(int G, const PagedAttn& a, hipStream_t stream);
 hipError_t launch_paged_stream(int dtype, int G, const PagedAttn& a, hipStream_t stream);
-// Joins first ... first + n - 1 of the plan's: rows and parts, the most of any of them.
-hipError_t launch_paged_join(int dtype, int G, const PagedAttn& a, int first, int n, int rows, int parts, hipStream_t stream);
+hipError_t launch_paged_join(int dtype, int G, const PagedAttn& a, const JoinShape& tile, const JoinShape& few, hipStream_t stream);
 
 }  // namespace catekv

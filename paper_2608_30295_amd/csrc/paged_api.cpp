@@ -593,9 +593,8 @@ int catekv_paged_attn(const catekv_paged_cache* cache, const catekv_paged_plan_t
     e = launch_paged_stream(cache->dtype, G, a, s);
     if (e != hipSuccess) return hip_fail(e, "paged_attn stream launch");
   }
-  e = launch_paged_join(cache->dtype, G, a, 0, plan->tile_joins, paged_tile_rows(cache->dtype), plan->tile_parts, s);
-  if (e == hipSuccess)
-    e = launch_paged_join(cache->dtype, G, a, plan->tile_joins, plan->n_joins - plan->tile_joins, kStreamRows, plan->few_parts, s);
+  e = launch_paged_join(cache->dtype, G, a, paged_join_shape(plan->tile_joins, paged_tile_rows(cache->dtype), plan->tile_parts),
+                        paged_join_shape(plan->n_joins - plan->tile_joins, kStreamRows, plan->few_parts), s);
   if (e != hipSuccess) return hip_fail(e, "paged_attn join launch");
   return host_ok();
 }

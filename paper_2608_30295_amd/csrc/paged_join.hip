@@ -9,13 +9,13 @@ namespace {
 // dependent loads: a group that goes through 96 parts alone takes 23 us, eight that share
 // them 4.7; up to 8 parts are left to one (4 to 9 us).
 template <typename T, int G, int S>
-__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedAttn a, int first, int blocks) {
+__device__ __forceinline__ void join_rows(const PagedAttn& a, const PagedJoin& j, int block, float* s_all) {
   constexpr int ROWS = kJoinRows / S;
-  __shared__ float s_x[S][ROWS][kD], s_l[S][ROWS], s_m[S][ROWS];
-  const int ji = blockIdx.x / blocks;
-  const PagedJoin j = a.joins[first + ji];
+  float (*s_x)[ROWS][kD] = reinterpret_cast<float (*)[ROWS][kD]>(s_all);
+  float (*s_l)[ROWS] = reinterpret_cast<float (*)[ROWS]>(s_all + kJoinRows * kD);
+  float (*s_m)[ROWS] = s_l + S;
   const int lane = threadIdx.x & 31, row = (threadIdx.x >> 5) % ROWS, g = (threadIdx.x >> 5) / ROWS;
-  const int at = (blockIdx.x - ji * blocks) * ROWS + row, r = j.row0 + at;
+  const int at = block * ROWS + row, r = j.row0 + at;
   const bool mine = at < j.rows && r < j.n_new * G;
   const float* slot = a.slots + (size_t)j.slot * 4;
   const size_t step = paged_slot_floats(j.rows);
@@ -71,26 +71,33 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedAttn a, i
   if (a.lse && lane == 0) a.lse[q] = none ? -INFINITY : (M + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Joins first ... first + n of at most `rows` rows each.
+// Workgroup b of a join: the tiles' come first, then those of few new rows.
 template <typename T, int G>
-hipError_t join(const PagedAttn& a, int first, int n, int rows, int parts, hipStream_t stream) {
-  if (n == 0) return hipSuccess;
-  const int per = paged_join_rows(parts), blocks = (rows + per - 1) / per;
-  if (per == kJoinRows) paged_join_kernel<T, G, 1><<<n * blocks, kJoinThreads, 0, stream>>>(a, first, blocks);
-  else paged_join_kernel<T, G, kJoinRows><<<n * blocks, kJoinThreads, 0, stream>>>(a, first, blocks);
-  return hipGetLastError();
+__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedAttn a, JoinShape tile, JoinShape few) {
+  __shared__ float s_all[kJoinRows * (kD + 2)];
+  const int b = blockIdx.x, split = tile.n * tile.blocks;
+  const JoinShape& x = b < split ? tile : few;
+  const int i = (b < split ? b : b - split) / x.blocks, block = (b < split ? b : b - split) - i * x.blocks;
+  const PagedJoin j = a.joins[b < split ? i : tile.n + i];
+  if (x.deep) join_rows<T, G, kJoinRows>(a, j, block, s_all);
+  else join_rows<T, G, 1>(a, j, block, s_all);
 }
+
 template <typename T>
-hipError_t join_g(int G, const PagedAttn& a, int first, int n, int rows, int parts, hipStream_t s) {
-  return G == 1 ? join<T, 1>(a, first, n, rows, parts, s) : G == 2 ? join<T, 2>(a, first, n, rows, parts, s)
-       : G == 4 ? join<T, 4>(a, first, n, rows, parts, s) : join<T, 8>(a, first, n, rows, parts, s);
+hipError_t join(int G, const PagedAttn& a, const JoinShape& tile, const JoinShape& few, hipStream_t stream) {
+  const unsigned n = (unsigned)(tile.n * tile.blocks + few.n * few.blocks);
+  if (n == 0) return hipSuccess;
+  if (G == 1) paged_join_kernel<T, 1><<<n, kJoinThreads, 0, stream>>>(a, tile, few);
+  else if (G == 2) paged_join_kernel<T, 2><<<n, kJoinThreads, 0, stream>>>(a, tile, few);
+  else if (G == 4) paged_join_kernel<T, 4><<<n, kJoinThreads, 0, stream>>>(a, tile, few);
+  else paged_join_kernel<T, 8><<<n, kJoinThreads, 0, stream>>>(a, tile, few);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_paged_join(int dtype, int G, const PagedAttn& a, int first, int n, int rows, int parts, hipStream_t stream) {
-  return dtype == CATEKV_BF16 ? join_g<uint16_t>(G, a, first, n, rows, parts, stream)
-                              : join_g<float>(G, a, first, n, rows, parts, stream);
+hipError_t launch_paged_join(int dtype, int G, const PagedAttn& a, const JoinShape& tile, const JoinShape& few, hipStream_t stream) {
+  return dtype == CATEKV_BF16 ? join<uint16_t>(G, a, tile, few, stream) : join<float>(G, a, tile, few, stream);
 }
 
 }  // namespace catekv
