@@ -1,5 +1,5 @@
 // Internal interface of the caches in pages: what paged_api.cpp passes to the
-// kernels of paged_pages.hip, paged_tile.hip and paged_stream.hip.
+// kernels of paged_*.hip.
 #pragma once
 
 #include "cache.h"
@@ -112,11 +112,13 @@ struct PagedAttn {
   const char* q;
   char* out;
   float* lse;
-  const PagedPiece* pieces;         // by worker, and
+  const PagedPiece* pieces;         // tiles of many new rows by worker, and
   const int32_t* workers;           // the first of every worker
+  const PagedPiece* segs;           // segments of few new rows, the same
+  const int32_t* seg_workers;
   const PagedJoin* joins;
   float* slots;
-  int32_t n;                        // workers
+  int32_t n, n_few;                 // workers of the tiles, of the segments
   int32_t hq;
   float scale;
   float log2_scale;                 // of the scores as the products give them, to units of log2
@@ -135,6 +137,7 @@ inline JoinShape paged_join_shape(int n, int rows, int parts) { return {n, parts
 constexpr int kTileRows = 256, kTileRowsF32 = 128;
 inline int paged_tile_rows(int dtype) { return dtype == CATEKV_BF16 ? kTileRows : kTileRowsF32; }
 hipError_t launch_paged_tile(int G, const PagedAttn& a, hipStream_t stream);       // bf16
+hipError_t launch_paged_mixed(int G, const PagedAttn& a, hipStream_t stream);      // bf16, tiles and segments
 hipError_t launch_paged_tile_f32(int G, const PagedAttn& a, hipStream_t stream);
 hipError_t launch_paged_stream(int dtype, int G, const PagedAttn& a, hipStream_t stream);
 hipError_t launch_paged_join(int dtype, int G, const PagedAttn& a, const JoinShape& tile, const JoinShape& few, hipStream_t stream);

@@ -121,8 +121,10 @@ struct Plan {
 // and a partial result's way to memory and back.
 struct TileCosts {
   double unit, piece, join, slot;
+  double apart;                        // of a unit's, for tiles of a view that do not run side by side
 };
-constexpr TileCosts kTileCosts = {1.8, 7.0, 6.0, 0.07}, kTileCostsF32 = {7.5, 12.0, 6.0, 0.035};
+constexpr TileCosts kTileCosts = {1.8, 7.0, 6.0, 0.07, 0.08}, kTileCostsF32 = {7.5, 12.0, 6.0, 0.035, 0.0};
+constexpr int kGang = 4;               // tiles of a view side by side, at most
 constexpr int kXcds = 8;               // a worker's engine is its number modulo this
 
 struct Tile {
@@ -197,28 +199,56 @@ double least_cost(const std::vector<Tile>& tiles, int64_t share, int workers, co
 }
 
 // All tiles end to end, cut into shares that take as long; neighbours lie in one engine.  No
-// part is shorter than half a piece's way in and out.
-Deal deal_line(const std::vector<Tile>& tiles, int workers, const TileCosts& k) {
+// part is shorter than half a piece's way in and out.  `gang` neighbouring tiles of a view are
+// cut at the same rows and given to workers of one engine, which read them at the same time:
+// its cache is asked for them by all and the memory by one (8 tiles each of 16 views of 8498
+// and 22747 rows: 347 us with shares of single tiles, which drift apart and read 1000 MB
+// for 136; 331 in twos, 321 in fours).
+Deal deal_line(const std::vector<Tile>& tiles, int workers, TileCosts k, int gang) {
   Deal d;
+  struct Group {
+    size_t first, n;
+    int64_t units;
+  };
+  std::vector<Group> groups;
   int64_t units = 0;
-  for (const Tile& t : tiles) units += t.units;
-  const double share = (k.unit * (double)units + k.piece * (double)(tiles.size() + workers)) / workers;
+  for (size_t i = 0; i < tiles.size();) {
+    size_t n = 1;
+    while (n < (size_t)gang && i + n < tiles.size() && tiles[i + n].p.view == tiles[i].p.view) ++n;
+    groups.push_back({i, n, tiles[i + n - 1].units});  // later tiles see more
+    units += groups.back().units;
+    i += n;
+  }
+  // what smaller gangs than the views have tiles for lose, as measured
+  size_t views = 1;
+  for (size_t i = 1; i < tiles.size(); ++i) views += tiles[i].p.view != tiles[i - 1].p.view;
+  const double width = std::min<double>(kGang, (double)tiles.size() / (double)views);
+  if (width > gang) k.unit *= 1.0 + k.apart * (width - gang) / (width - 1.0);
+  int gangs = workers / gang, per = gangs / kXcds;
+  if (gang > 1) gangs = per * kXcds;
+  if (gangs == 0) {
+    d.cost = HUGE_VAL;
+    return d;
+  }
+  const double share = (k.unit * (double)units + k.piece * (double)(groups.size() + gangs)) / gangs;
   const int64_t least = std::max<int64_t>(1, (int64_t)(k.piece / k.unit / 2));
-  const int per = std::max(1, workers / kXcds);
   double spent = 0;
   size_t i = 0;
   int64_t off = 0;
-  for (int s = 0; s < workers && i < tiles.size(); ++s) {
-    const bool last = s == workers - 1;
-    const int w = workers % kXcds == 0 ? s % per * kXcds + s / per : s;
-    while (i < tiles.size()) {
+  for (int s = 0; s < gangs && i < groups.size(); ++s) {
+    const bool last = s == gangs - 1;
+    while (i < groups.size()) {
       const int64_t room = (int64_t)std::floor(((s + 1) * share - spent - k.piece) / k.unit + 0.5);
       if (room < least && !last) break;
-      const int64_t rest = tiles[i].units - off, take = last || rest <= room + least ? rest : room;
-      d.cuts.push_back({(int)i, off, off + take, w});
+      const int64_t rest = groups[i].units - off, take = last || rest <= room + least ? rest : room;
+      for (size_t j = 0; j < groups[i].n; ++j) {
+        const int64_t end = std::min(off + take, tiles[groups[i].first + j].units);
+        const int w = gangs % kXcds == 0 ? (int)((s % per * gang + j) * kXcds + s / per) : s;
+        if (off < end) d.cuts.push_back({(int)(groups[i].first + j), off, end, w});
+      }
       spent += k.piece + k.unit * (double)take;
       off += take;
-      if (off == tiles[i].units) {
+      if (off == groups[i].units) {
         ++i;
         off = 0;
       }
@@ -226,6 +256,26 @@ Deal deal_line(const std::vector<Tile>& tiles, int workers, const TileCosts& k) 
   }
   price(d, tiles, workers, k);
   return d;
+}
+
+// bf16 batches of both kinds run in one launch: as many of the compute units for the few-token
+// sequences as end both at about the same time.  A compute unit reads 64 rows of K and V in 1.2 us
+// (1.5 with all of them at it), and a share's start, joining of waves and way out take 8; a
+// tile's unit takes 2.2 beside them.  (16 sequences of 4096 to 32768 rows, two of them with 512 new
+// tokens: 455 us with 96 of 256, 564 with 64, 490 with 112; as launches one after the other 476.)
+int few_workers(int64_t tile_units, int64_t n_tiles, int64_t few_units, int cus) {
+  const TileCosts& k = kTileCosts;
+  int best = 1;
+  double least = HUGE_VAL;
+  for (int w = 8; w < cus; w += w < 32 ? 8 : 32) {     // whole gangs are left in every engine
+    const double tiles = (2.2 * (double)tile_units + k.piece * (double)std::max<int64_t>(n_tiles, cus - w)) / (cus - w);
+    const double few = 8.0 + 1.2 * (double)((few_units + w - 1) / w);
+    if (std::max(tiles, few) < least) {
+      least = std::max(tiles, few);
+      best = w;
+    }
+  }
+  return best;
 }
 
 int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t* n_new, const int64_t* max_rows, int n_seqs,
@@ -293,6 +343,7 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
     }
   if (n_tiles > (int64_t)1 << 22) return fail(CATEKV_ERR_UNSUPPORTED, "%lld tiles of new rows: too many for one launch", (long long)n_tiles);
 
+  int few_cus = cus;                                   // compute units of the few-token sequences
   // tiles: whole, or cut at some share of the work, whichever is done first
   if (n_tiles > 0) {
     std::vector<Tile> tiles;
@@ -305,13 +356,17 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
         }
     const bool half = c->dtype == CATEKV_BF16;
     const TileCosts& costs = half ? kTileCosts : kTileCostsF32;
-    const int workers = half ? cus : 2 * cus;
+    const int workers = !half ? 2 * cus : few_units > 0 ? cus - few_workers(tile_units, n_tiles, few_units, cus) : cus;
+    if (half && few_units > 0) few_cus = cus - workers;
     Deal best = deal(tiles, 0, workers, costs);
     // (a whole tile's way is not left for less than a twentieth)
     if (n_tiles < 8 * (int64_t)workers && best.cost > 1.05 * least_cost(tiles, 0, workers, costs)) {
       const int64_t even = (tile_units + workers - 1) / workers;
-      Deal d = deal_line(tiles, workers, costs);
-      if (d.cost < best.cost) best = std::move(d);
+      Deal d;
+      for (int gang = half ? kGang : 1; gang >= 1; gang /= 2) {
+        d = deal_line(tiles, workers, costs, gang);
+        if (d.cost < best.cost) best = std::move(d);
+      }
       for (int k = 2; k <= 8; ++k) {                 // shares of 2 to 1/2 of an equal one
         const int64_t share = std::max<int64_t>(1, (4 * even + k - 1) / k);
         if (least_cost(tiles, share, workers, costs) >= best.cost) continue;
@@ -349,7 +404,7 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
 
   // the rest laid end to end and cut into equal shares, one per workgroup
   if (few_units > 0) {
-    const int64_t W = std::min<int64_t>(cus, few_units);
+    const int64_t W = std::min<int64_t>(few_cus, few_units);
     int64_t w = 0, left = 0, done = 0;            // the share being filled, units left of it, units given out
     P.workers.push_back(0);
     auto open = [&] {
@@ -579,20 +634,19 @@ int catekv_paged_attn(const catekv_paged_cache* cache, const catekv_paged_plan_t
   const int G = plan->hq / plan->hkv;
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   hipError_t e = hipSuccess;
-  if (plan->n_tile > 0) {
-    a.pieces = reinterpret_cast<const PagedPiece*>(w + plan->tiles_off);
-    a.workers = reinterpret_cast<const int32_t*>(w + plan->tile_workers_off);
-    a.n = plan->n_tile;
-    e = cache->dtype == CATEKV_BF16 ? launch_paged_tile(G, a, s) : launch_paged_tile_f32(G, a, s);
-    if (e != hipSuccess) return hip_fail(e, "paged_attn launch");
+  a.pieces = reinterpret_cast<const PagedPiece*>(w + plan->tiles_off);
+  a.workers = reinterpret_cast<const int32_t*>(w + plan->tile_workers_off);
+  a.n = plan->n_tile;
+  a.segs = reinterpret_cast<const PagedPiece*>(w + plan->segs_off);
+  a.seg_workers = reinterpret_cast<const int32_t*>(w + plan->workers_off);
+  a.n_few = plan->n_workers;
+  if (a.n > 0 && a.n_few > 0 && cache->dtype == CATEKV_BF16) {
+    e = launch_paged_mixed(G, a, s);
+  } else {
+    if (a.n > 0) e = cache->dtype == CATEKV_BF16 ? launch_paged_tile(G, a, s) : launch_paged_tile_f32(G, a, s);
+    if (e == hipSuccess && a.n_few > 0) e = launch_paged_stream(cache->dtype, G, a, s);
   }
-  if (plan->n_workers > 0) {
-    a.pieces = reinterpret_cast<const PagedPiece*>(w + plan->segs_off);
-    a.workers = reinterpret_cast<const int32_t*>(w + plan->workers_off);
-    a.n = plan->n_workers;
-    e = launch_paged_stream(cache->dtype, G, a, s);
-    if (e != hipSuccess) return hip_fail(e, "paged_attn stream launch");
-  }
+  if (e != hipSuccess) return hip_fail(e, "paged_attn launch");
   e = launch_paged_join(cache->dtype, G, a, paged_join_shape(plan->tile_joins, paged_tile_rows(cache->dtype), plan->tile_parts),
                         paged_join_shape(plan->n_joins - plan->tile_joins, kStreamRows, plan->few_parts), s);
   if (e != hipSuccess) return hip_fail(e, "paged_attn join launch");

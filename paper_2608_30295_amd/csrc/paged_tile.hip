@@ -23,7 +23,7 @@
 // registers; 128 to a workgroup would read K and V from LDS twice as often.
 #include <type_traits>
 
-#include "paged_math.h"
+#include "paged_stream.h"
 
 namespace catekv {
 namespace {
@@ -73,6 +73,9 @@ __device__ __forceinline__ uint4 pack16(const f32x16 (&x)[2], int h) {
   return make_uint4(pg_pack2(y[o], y[o + 1]), pg_pack2(y[o + 2], y[o + 3]), pg_pack2(y[o + 4], y[o + 5]), pg_pack2(y[o + 6], y[o + 7]));
 }
 
+constexpr int kMixedQ = kStreamWaves * R * kPad / 4;   // 16-byte units of the streaming waves' sums
+static_assert(kTileThreads == kStreamThreads && kMixedQ >= kTileRows * kSeg, "one launch for both");
+
 // What is the same for all lanes about a piece.
 struct Piece {
   int32_t view, tok0, n_new, row0, t0, slot;
@@ -80,13 +83,25 @@ struct Piece {
   int32_t n_tiles, n_full;                             // tiles; those that every new row sees in full come first
 };
 
-template <int G>
+// MIXED: a batch with sequences of few new tokens, too; the workgroups behind those of the
+// tiles take them.
+template <int G, bool MIXED>
 __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void paged_tile_kernel(PagedAttn a) {
   // aligned so that they come first: their places fit the reads' 16-bit offsets
   __shared__ __attribute__((aligned(1024))) uint4 s_k0[kStage], s_k1[kStage], s_v0[kStage], s_v1[kStage];
-  __shared__ uint4 s_q[kTileRows * kSeg];              // new rows, laid out as K is
+  __shared__ uint4 s_q[MIXED ? kMixedQ : kTileRows * kSeg];   // new rows, laid out as K is
   __shared__ int s_bad;
+
+  if (MIXED && (int)blockIdx.x >= a.n) {
+    constexpr int BATCH = kStage / (R * kSeg);
+    float (*ml)[kStreamWaves][R] = reinterpret_cast<float (*)[kStreamWaves][R]>(s_v0);
+    const int32_t* share = a.seg_workers + ((int)blockIdx.x - a.n);
+    stream_share<uint16_t, G, BATCH>(a, a.segs, share[0], share[1],
+                                     {reinterpret_cast<Seg (*)[BATCH]>(s_v1), reinterpret_cast<uint4 (*)[BATCH][R][kSeg]>(s_k0),
+                                      reinterpret_cast<float (*)[kStreamWaves][R][kPad]>(s_q), ml, ml + 1});
+    return;
+  }
 
   const PagedCache& c = a.c;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -483,9 +498,13 @@ void paged_tile_kernel(PagedAttn a) {
   }
 }
 
-template <int G>
-hipError_t tile(const PagedAttn& a, hipStream_t stream) {
-  paged_tile_kernel<G><<<a.n, kTileThreads, 0, stream>>>(a);
+template <bool MIXED>
+hipError_t tile(int G, const PagedAttn& a, hipStream_t stream) {
+  const int n = a.n + (MIXED ? a.n_few : 0);
+  if (G == 1) paged_tile_kernel<1, MIXED><<<n, kTileThreads, 0, stream>>>(a);
+  else if (G == 2) paged_tile_kernel<2, MIXED><<<n, kTileThreads, 0, stream>>>(a);
+  else if (G == 4) paged_tile_kernel<4, MIXED><<<n, kTileThreads, 0, stream>>>(a);
+  else paged_tile_kernel<8, MIXED><<<n, kTileThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -493,8 +512,7 @@ hipError_t tile(const PagedAttn& a, hipStream_t stream) {
 
 static_assert(kTileRows == kTileThreads / 2, "32 new rows per wave");
 
-hipError_t launch_paged_tile(int G, const PagedAttn& a, hipStream_t s) {
-  return G == 1 ? tile<1>(a, s) : G == 2 ? tile<2>(a, s) : G == 4 ? tile<4>(a, s) : tile<8>(a, s);
-}
+hipError_t launch_paged_tile(int G, const PagedAttn& a, hipStream_t s) { return tile<false>(G, a, s); }
+hipError_t launch_paged_mixed(int G, const PagedAttn& a, hipStream_t s) { return tile<true>(G, a, s); }
 
 }  // namespace catekv

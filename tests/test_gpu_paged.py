@@ -251,6 +251,22 @@ def test_attention_of_new_tokens(dtype, page, hkv, G, ctx, new):
     check_attention(c, plan, slots, new, hkv * G, 9)
 
 
+@pytest.mark.parametrize("dtype,G,singles,long,chunk", [(BF16, 1, 60, 40, 600), (BF16, 2, 9, 900, 300), (BF16, 4, 40, 500, 150),
+                                                        (BF16, 8, 3, 3000, 64), (F32, 4, 20, 300, 100)])
+def test_single_tokens_beside_chunks(dtype, G, singles, long, chunk):
+    """Many short and a few long sequences of 1 or 2 tokens in one batch with two chunks: workgroups
+    that take more of them than they describe at a time, and chunks of views cut in several places."""
+    hkv, r, page = 2, np.random.RandomState(singles), 32
+    new = [chunk] + [int(x) for x in r.randint(1, 3 if 2 * G <= 16 else 2, size=singles)] + [chunk // 2 + 1]
+    ctx = [1500] + [int(x) for x in r.randint(0, long, size=singles)] + [700]
+    slots = [int(x) for x in r.permutation(singles + 4)[:singles + 2]]
+    need = sum(hkv * R.pages_of(a + b, page) for a, b in zip(ctx, new))
+    c, s = cache_of(need + 9, page, singles + 4, hkv, max(R.pages_of(a + b, page) for a, b in zip(ctx, new)) + 1, dtype)
+    append(c, s, slots, ctx, hkv * G, 31)
+    plan = append(c, s, slots, new, hkv * G, 33)
+    check_attention(c, plan, slots, new, hkv * G, 35)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_attention_of_views_cut_to_different_lengths(dtype):
     """Heads of one sequence with few rows, fewer than the new tokens, and none."""
