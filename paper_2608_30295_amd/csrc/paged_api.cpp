@@ -356,8 +356,8 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
         }
     const bool half = c->dtype == CATEKV_BF16;
     const TileCosts& costs = half ? kTileCosts : kTileCostsF32;
-    const int workers = !half ? 2 * cus : few_units > 0 ? cus - few_workers(tile_units, n_tiles, few_units, cus) : cus;
-    if (half && few_units > 0) few_cus = cus - workers;
+    const int workers = !half ? 2 * cus : few_units > 0 ? std::max(1, cus - few_workers(tile_units, n_tiles, few_units, cus)) : cus;
+    if (half && few_units > 0) few_cus = std::max(1, cus - workers);
     Deal best = deal(tiles, 0, workers, costs);
     // (a whole tile's way is not left for less than a twentieth)
     if (n_tiles < 8 * (int64_t)workers && best.cost > 1.05 * least_cost(tiles, 0, workers, costs)) {

@@ -2,17 +2,19 @@
 // in pages (gfx950): bound by reading K and V once.
 //
 // All views are laid end to end and cut into equal shares, one per workgroup of 8
-// waves, one workgroup per compute unit.  A wave streams tiles of 16 cached rows (a
-// page holds whole ones) through two stages of registers, also from one segment into
-// the next; the page number of the tile after the next is on its way meanwhile.
+// waves, one workgroup per compute unit (fewer beside chunks, in their launch).  A wave
+// streams tiles of 16 cached rows (a page holds whole ones) through two stages of registers,
+// also from one segment into the next; the page number of the tile after the next is on its
+// way meanwhile.
 // Scores are S^T = K Q^T: lane l holds row l % 16 of the new ones and cached rows
 // 4 (l / 16) + i, which is how O^T = V^T P^T takes P; what belongs to a new row
 // (maximum, sum, factor) is a lane's own.  V^T's rows are the 8 dims that a lane
 // loaded of each cached row, one product per dim.
 //
 // bf16, 3 views of 131072 rows and 5 of 2112, 4 heads a group: 207 MB in 37 us, 5.6 TB/s with
-// the start; 64 sequences: 553 MB in 95 us, 5.8 TB/s.  fp32, 65536 rows: 4.9 TB/s.  A compute unit takes 22 GB/s
-// with all of them at work and with half of them, so all are given a share.
+// the start; 64 sequences: 553 MB in 95 us, 5.8 TB/s.  fp32, 65536 rows: 4.9 TB/s.  A
+// compute unit takes 22 GB/s with all of them at work and 23 to 28 with a third: all are given a share, but for those
+// that a batch's chunks keep.
 #pragma once
 
 #include <type_traits>

@@ -16,7 +16,7 @@
 // maxima of tile t + 1.  A wave issues in order, so the two are laid between each other
 // in the program, and scheduling barriers keep them there.
 //
-// 2048 new tokens behind 30720 rows, 32 heads over 8: 1065 GFLOP in 990 to 1055 us, 1.01 to
+// 2048 new tokens, the last of 32768 rows, 32 heads over 8: 1065 GFLOP in 990 to 1055 us, 1.01 to
 // 1.07 PFLOP/s where a large library product reaches 1.10 (products beside each other
 // without softmax: 1.6 to 1.9).  The matrix cores are busy for 52% of the cycles, the vector
 // unit issues in 45%; no LDS bank conflicts.  Larger tiles of new rows do not fit the
