@@ -186,16 +186,25 @@ Deal deal(const std::vector<Tile>& tiles, int64_t share, int workers, const Tile
   return d;
 }
 
-// What a deal in parts of at most `share` units costs at least.
+// What a deal in parts of at most `share` units costs at least: no less than on average, and
+// where there are more than j workers' worth of parts, one worker has j + 1 of the longest.
 double least_cost(const std::vector<Tile>& tiles, int64_t share, int workers, const TileCosts& k) {
   int64_t units = 0, pieces = 0, slots = 0;
+  std::vector<std::pair<int64_t, int64_t>> parts;      // length (rounded down), how many
+  parts.reserve(tiles.size());
   for (const Tile& t : tiles) {
-    const int64_t parts = share ? (t.units + share - 1) / share : 1;
+    const int64_t n = share ? (t.units + share - 1) / share : 1;
+    parts.push_back({t.units / n, n});
     units += t.units;
-    pieces += parts;
-    slots += parts > 1 ? parts : 0;
+    pieces += n;
+    slots += n > 1 ? n : 0;
   }
-  return (k.unit * (double)units + k.piece * (double)pieces) / workers + (slots ? k.join + k.slot * (double)slots : 0.0);
+  double most = (k.unit * (double)units + k.piece * (double)pieces) / workers;
+  std::sort(parts.begin(), parts.end(), std::greater<>());
+  int64_t before = 0, j = 0;
+  for (const auto& p : parts)
+    for (before += p.second; before > j * workers; ++j) most = std::max(most, (double)(j + 1) * (k.unit * (double)p.first + k.piece));
+  return most + (slots ? k.join + k.slot * (double)slots : 0.0);
 }
 
 // All tiles end to end, cut into shares that take as long; neighbours lie in one engine.  No
@@ -360,8 +369,11 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
     if (half && few_units > 0) few_cus = std::max(1, cus - workers);
     Deal best = deal(tiles, 0, workers, costs);
     // (a whole tile's way is not left for less than a twentieth)
-    if (n_tiles < 8 * (int64_t)workers && best.cost > 1.05 * least_cost(tiles, 0, workers, costs)) {
+    const double even_cost = (costs.unit * (double)tile_units + costs.piece * (double)n_tiles) / workers;
+    if (n_tiles < 8 * (int64_t)workers && best.cost > 1.05 * even_cost) {
       const int64_t even = (tile_units + workers - 1) / workers;
+      int64_t longest = 0;
+      for (const Tile& t : tiles) longest = std::max(longest, t.units);
       Deal d;
       for (int gang = half ? kGang : 1; gang >= 1; gang /= 2) {
         d = deal_line(tiles, workers, costs, gang);
@@ -369,7 +381,7 @@ int build_plan(const catekv_paged_cache* c, const int32_t* slots, const int32_t*
       }
       for (int k = 2; k <= 8; ++k) {                 // shares of 2 to 1/2 of an equal one
         const int64_t share = std::max<int64_t>(1, (4 * even + k - 1) / k);
-        if (least_cost(tiles, share, workers, costs) >= best.cost) continue;
+        if (share >= longest || least_cost(tiles, share, workers, costs) >= best.cost) continue;
         d = deal(tiles, share, workers, costs);
         if (d.cost < best.cost) best = std::move(d);
       }
