@@ -51,21 +51,27 @@ __device__ __forceinline__ uint4 pg_scale_q(const uint16_t*, uint4 q, float) { r
 
 // Rows of a view as attention takes them: none if its length is out of range, and
 // no more than were planned for.
-__device__ __forceinline__ int pg_rows(const PagedCache& c, int view, int max_rows) {
-  const int64_t len = c.lens[view], cap = (int64_t)c.max_pages << c.page_log;
+__device__ __forceinline__ int pg_rows(const PagedCache& c, int64_t len, int max_rows) {
+  const int64_t cap = (int64_t)c.max_pages << c.page_log;
   return len < 0 || len > cap ? 0 : (int)min(len, (int64_t)max_rows);
 }
 __device__ __forceinline__ size_t pg_page(const PagedCache& c, int id) {
   return (size_t)((uint32_t)id < (uint32_t)c.n_pages ? id : 0) << c.page_log;
 }
 
-// A table's entry, the same for all lanes, through the scalar cache: its wait is its own,
-// and not one for every vector load issued before it.
-__device__ __forceinline__ int pg_entry(const int32_t* ids, int p) {
-  const uint64_t at = reinterpret_cast<uint64_t>(ids + p);
+// A value that is the same for all lanes, and that no one writes meanwhile, through the scalar
+// cache: its wait is its own, and not one for every vector load and store issued before it.
+template <typename T>
+__device__ __forceinline__ T pg_scalar(const T* p) {
+  const uint64_t at = reinterpret_cast<uint64_t>(p);
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
-  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>((uint64_t)hi << 32 | lo);
+  struct Words { int32_t w[sizeof(T) / 4]; } x;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(T) / 4); ++i)
+    x.w[i] = reinterpret_cast<const __attribute__((address_space(4))) int32_t*>((uint64_t)hi << 32 | lo)[i];
+  return __builtin_bit_cast(T, x);
 }
+__device__ __forceinline__ int pg_entry(const int32_t* ids, int p) { return pg_scalar(ids + p); }
 
 // ---- V that is not finite: the exponent's bits all ones ----------------------------
 __device__ __forceinline__ bool pg_bad16(uint32_t x) { return (x & 0x7f80u) == 0x7f80u; }

@@ -164,7 +164,7 @@ __device__ __forceinline__ void stream_share(const PagedAttn& a, const PagedPiec
     __syncthreads();                                  // the batch before is done
     if ((int)threadIdx.x < nseg) {
       const PagedPiece p = pieces[s0 + threadIdx.x];
-      const int L = pg_rows(c, p.view, p.max_rows);
+      const int L = pg_rows(c, c.lens[p.view], p.max_rows);
       Seg s;
       s.view = p.view;
       s.t0 = p.t0;

@@ -122,7 +122,7 @@ void paged_tile_kernel(PagedAttn a) {
 
   // ---- a piece's way in ------------------------------------------------------------
   auto open = [&](int w) __attribute__((always_inline)) {
-    const PagedPiece p = a.pieces[w];
+    const PagedPiece p = pg_scalar(a.pieces + w);
     Piece x;
     x.view = p.view;
     x.tok0 = p.tok0;
@@ -130,7 +130,7 @@ void paged_tile_kernel(PagedAttn a) {
     x.row0 = p.row0;
     x.t0 = p.t0;
     x.slot = p.slot;
-    const int L = __builtin_amdgcn_readfirstlane(pg_rows(c, p.view, p.max_rows));
+    const int L = pg_rows(c, pg_scalar(c.lens + p.view), p.max_rows);
     x.see0 = L - p.n_new + 1;
     const int t_end = min(p.t1, x.see0 + (min(p.row0 + kTileRows, p.n_new * G) - 1) / G);
     // without a cached row that is seen: one tile, all of it masked
@@ -377,7 +377,8 @@ void paged_tile_kernel(PagedAttn a) {
   using B1 = std::true_type;
 
   // ---- the worker's pieces -----------------------------------------------------------
-  // The next piece's way in begins before this one's results' way out.
+  // The next piece's new rows and K come in under this one's last products, and its V under the
+  // results' way out, which nothing waits for but the first turn.
   int w = a.workers[blockIdx.x];
   if (w >= last) return;                               // a worker without pieces
   Piece x = open(w);
@@ -388,6 +389,8 @@ void paged_tile_kernel(PagedAttn a) {
   issue(x, k_at, s_k1, 1, next);
   issue(x, v_at, s_v0, 0, tile0);
   if (threadIdx.x == 0) s_bad = 0;
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
   for (;;) {
     own();
     {
@@ -402,11 +405,9 @@ void paged_tile_kernel(PagedAttn a) {
     cw = cs;
     f32x16 sa[2], sb[2];
     const bool more = w + 1 < last;
-    const Piece y = open(more ? w + 1 : w);            // the next piece, under the wait for this one's tiles
+    const Piece y = open(more ? w + 1 : w);
     const Ids y0 = fetch(y, 0), y1 = fetch(y, 1);
     after = fetch(x, 2);
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) q[ks] = k_op(s_q + wave * 32 * kSeg, 0, ks, ka);
     if (!idle) {
@@ -434,6 +435,11 @@ void paged_tile_kernel(PagedAttn a) {
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     own();
+    if (more) {                                        // K's places are free
+      queries(y);
+      issue(y, k_at, s_k0, 0, y0);
+      issue(y, k_at, s_k1, 1, y1);
+    }
     uint4* vt = odd ? s_v1 : s_v0;
     uint4 p[4];
     look(vt);
@@ -441,10 +447,8 @@ void paged_tile_kernel(PagedAttn a) {
     purge(vt);
     if (!idle) product(vt, p);
     if (more) {
-      barrier_lds_only();                              // V is free
-      queries(y);
-      issue(y, k_at, s_k0, 0, y0);
-      issue(y, k_at, s_k1, 1, y1);
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();                                 // they are there, and V's places are free
       issue(y, v_at, s_v0, 0, y0);
     }
 

@@ -54,7 +54,7 @@ void paged_tile_f32_kernel(PagedAttn a) {
     asm volatile("" : "+v"(lane));                     // nothing of a piece is kept in registers for the next
     const int hi = lane >> 5;
     const PagedPiece pc = a.pieces[w];
-    const int L = __builtin_amdgcn_readfirstlane(pg_rows(c, pc.view, pc.max_rows));
+    const int L = __builtin_amdgcn_readfirstlane(pg_rows(c, c.lens[pc.view], pc.max_rows));
     const int n_rows = pc.n_new * G;
     const int see0 = L - pc.n_new + 1;                 // cached rows that the first new token sees
     const int t_end = min(pc.t1, see0 + (min(pc.row0 + kTileRowsF32, n_rows) - 1) / G);
