@@ -350,7 +350,7 @@ void paged_tile_kernel(PagedAttn a) {
     if (MASK) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) f[0][i] = v_op(vt, 0, i, va);
-      hide(s2, x.t0 + (t + 1) * kTile);
+      if (t + 1 >= x.n_full) hide(s2, x.t0 + (t + 1) * kTile);
     }
     const float mc = reference();
     float mx = -INFINITY;
