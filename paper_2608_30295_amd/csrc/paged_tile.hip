@@ -300,7 +300,8 @@ void paged_tile_kernel(PagedAttn a) {
   // ---- turns -----------------------------------------------------------------------
   // At the head of turn t: tile t's scores are in s and their maxima taken in; K of t + 1
   // and V of t are in LDS or on their way.  Leaves tile t + 1's scores in s2.
-  auto turn = [&](auto stage, auto mask_tag, Piece& x, int t, bool idle, f32x16 (&s)[2], f32x16 (&s2)[2]) __attribute__((always_inline)) {
+  // The first masked turn asks for the next piece's new rows.
+  auto turn = [&](auto stage, auto mask_tag, Piece& x, const Piece* y, int t, bool idle, f32x16 (&s)[2], f32x16 (&s2)[2]) __attribute__((always_inline)) {
     constexpr bool B = decltype(stage)::value, MASK = decltype(mask_tag)::value;
     const uint4* kt = B ? s_k0 : s_k1;
     uint4* vt = B ? s_v1 : s_v0;
@@ -311,6 +312,7 @@ void paged_tile_kernel(PagedAttn a) {
     next = after;
     after = fetch(x, t + 3);
     own();
+    if (MASK && y) queries(*y);
     const bool part = MASK && t >= x.n_full;           // some new rows do not see all of V's tile
     if (part) look(vt);
     // Operands come in fours, one four ahead: their wait is then for reads that have had
@@ -377,7 +379,7 @@ void paged_tile_kernel(PagedAttn a) {
   using B1 = std::true_type;
 
   // ---- the worker's pieces -----------------------------------------------------------
-  // The next piece's new rows and K come in under this one's last products, and its V under the
+  // The next piece's new rows and K come in under this one's last turns and products, and its V under the
   // results' way out, which nothing waits for but the first turn.
   int w = a.workers[blockIdx.x];
   if (w >= last) return;                               // a worker without pieces
@@ -417,18 +419,19 @@ void paged_tile_kernel(PagedAttn a) {
     }
     int t = 0;
     for (; t + 2 < x.n_full; t += 2) {
-      turn(B0{}, std::false_type{}, x, t, idle, sa, sb);
-      turn(B1{}, std::false_type{}, x, t + 1, idle, sb, sa);
+      turn(B0{}, std::false_type{}, x, nullptr, t, idle, sa, sb);
+      turn(B1{}, std::false_type{}, x, nullptr, t + 1, idle, sb, sa);
     }
     const int first = t;
     purged = false;
     for (; t + 2 < x.n_tiles; t += 2) {
-      turn(B0{}, std::true_type{}, x, t, idle, sa, sb);
-      turn(B1{}, std::true_type{}, x, t + 1, idle, sb, sa);
+      turn(B0{}, std::true_type{}, x, more && t == first ? &y : nullptr, t, idle, sa, sb);
+      turn(B1{}, std::true_type{}, x, nullptr, t + 1, idle, sb, sa);
     }
     const bool odd = t + 1 < x.n_tiles;
     if (odd) {
-      turn(B0{}, std::true_type{}, x, t++, idle, sa, sb);
+      turn(B0{}, std::true_type{}, x, more && t == first ? &y : nullptr, t, idle, sa, sb);
+      ++t;
       sa[0] = sb[0];
       sa[1] = sb[1];
     }
@@ -436,7 +439,7 @@ void paged_tile_kernel(PagedAttn a) {
     __syncthreads();
     own();
     if (more) {                                        // K's places are free
-      queries(y);
+      if (t == first) queries(y);                      // there was no masked turn
       issue(y, k_at, s_k0, 0, y0);
       issue(y, k_at, s_k1, 1, y1);
     }
