@@ -12,6 +12,7 @@ typedef float pg_f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 pg_bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 pg_bf16x8 __attribute__((ext_vector_type(8)));
 typedef short pg_s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short pg_u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLn2 = 0.6931471805599453f;
 

@@ -68,12 +68,12 @@ template <> struct Ops<uint16_t> {
     }
   }
   static __device__ __forceinline__ bool any_bad(const uint4 (&v)[kV]) {
-    uint32_t b = 0;
+    pg_u16x2 top = {0, 0};                // the largest magnitude, as bits
 #pragma unroll
     for (int r = 0; r < kV; ++r)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) b |= pg_both(word(v[r], i), [](uint32_t x) { return (uint32_t)pg_bad16(x); });
-    return b != 0;
+      for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(pg_u16x2, word(v[r], i) & 0x7fff7fffu));
+    return top[0] >= 0x7f80 || top[1] >= 0x7f80;
   }
   static __device__ __forceinline__ uint4 clean(const uint4& v) {
     return make_uint4(pg_both(v.x, pg_clean16), pg_both(v.y, pg_clean16), pg_both(v.z, pg_clean16), pg_both(v.w, pg_clean16));
@@ -262,13 +262,14 @@ __device__ __forceinline__ void stream_share(const PagedAttn& a, const PagedPiec
 #pragma unroll
             for (int x = 0; x < X::kVPer; ++x) vb[B][r * X::kVPer + x] = make_uint4(0, 0, 0, 0);
         }
-        // 0 * NaN is NaN: V that is not finite, and that some of the tokens do not see, is left
-        // out here and added to the sums of those that do at the segment's end
-        if (sg.rows > G && __builtin_amdgcn_ballot_w64(X::any_bad(vb[B]))) {
-          purged = true;
+      }
+      // 0 * NaN is NaN: V that is not finite, and that some of the tokens do not see, is left
+      // out here and added to the sums of those that do at the segment's end.  In bf16 it is
+      // wherever it stands: an infinity times the two parts of a weight is NaN, too.
+      if ((sizeof(T) == 2 || (masked && sg.rows > G)) && __builtin_amdgcn_ballot_w64(X::any_bad(vb[B]))) {
+        purged = true;
 #pragma unroll
-          for (int i = 0; i < X::kV; ++i) vb[B][i] = X::clean(vb[B][i]);
-        }
+        for (int i = 0; i < X::kV; ++i) vb[B][i] = X::clean(vb[B][i]);
       }
       float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
       mx = max_xor32(max_xor16(mx));
@@ -299,7 +300,7 @@ __device__ __forceinline__ void stream_share(const PagedAttn& a, const PagedPiec
 #pragma unroll 1
         for (int u = wave; u < sg.n_units; u += kStreamWaves) {
           const int tile = sg.t0 + u * kStreamTile;
-          if (tile + kStreamTile <= sg.see0) continue;        // all tokens see it: taken as it was
+          if (sizeof(T) == 4 && tile + kStreamTile <= sg.see0) continue;   // all tokens see it: taken as it was
           const size_t base = (pg_page(c, pg_entry(c.table + (size_t)sg.view * c.max_pages, tile >> c.page_log)) + (tile & mask)) * RB;
 #pragma unroll 1
           for (int r = 0; r < min(kStreamTile, sg.t_end - tile); ++r)

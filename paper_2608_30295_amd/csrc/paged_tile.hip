@@ -31,7 +31,6 @@ namespace {
 typedef pg_f32x16 f32x16;
 typedef pg_bf16x8 bf16x8;
 typedef pg_s16x4 s16x4;
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
@@ -254,13 +253,13 @@ void paged_tile_kernel(PagedAttn a) {
   int tag = 0;                                         // of the masked tile
   auto look = [&](const uint4* vt) __attribute__((always_inline)) {
     ++tag;
-    u16x2 top = {0, 0};                                // the largest magnitude, as bits
+    pg_u16x2 top = {0, 0};                                // the largest magnitude, as bits
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const uint4 x = vt[i * kTileThreads + wave * 64 + lane];
       const uint32_t y[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, y[e] & 0x7fff7fffu));
+      for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(pg_u16x2, y[e] & 0x7fff7fffu));
     }
     if (top[0] >= 0x7f80 || top[1] >= 0x7f80) s_bad = tag;
   };

@@ -327,6 +327,31 @@ def test_what_a_token_does_not_see_does_not_reach_it(dtype, G, new):
     assert torch.isnan(out[-1].float()).all() and torch.isfinite(out[:new - 2].float()).all()
 
 
+@pytest.mark.parametrize("dtype,G,n,new", [(BF16, 4, 150, 1), (BF16, 2, 9000, 3), (BF16, 8, 700, 30), (BF16, 1, 9000, 300),
+                                           (F32, 4, 150, 1), (F32, 1, 9000, 3), (F32, 4, 700, 30)])
+def test_infinities_that_a_token_sees_are_its_result(dtype, G, n, new):
+    """V of both infinities and NaN, alone and together in a dim, and K that takes rows out with a
+    score of -inf, in rows that all tokens see and in the first token's own."""
+    c, s = cache_of(2 * R.pages_of(n + new, 32) + 4, 32, 1, 2, R.pages_of(n + new, 32) + 1, dtype)
+    append(c, s, [0], [n], 2 * G, 1)
+    plan = append(c, s, [0], [new], 2 * G, 3)
+    q = randn((new, 2 * G, 128), 5, dtype)
+    q[..., 0] = q[..., 0].abs() + 0.5
+    inf = float("inf")
+
+    def at(row):
+        return s.table[0, 0, row // 32], row % 32
+    for row, dim, x in ((20, 3, inf), (40, 4, -inf), (21, 5, inf), (100, 5, -inf), (22, 6, float("nan")), (n, 7, inf)):
+        p, r = at(row)
+        c.v[p, r, dim] = x
+    p, r = at(60)
+    c.k[p, r, 0] = -inf
+    out, _ = check_attention(c, plan, [0], [new], 2 * G, 5, q=q)
+    o = out[:, :G].float()
+    assert (o[..., 3] == inf).all() and (o[..., 4] == -inf).all() and torch.isnan(o[..., 5:7]).all() and (o[..., 7] == inf).all()
+    assert torch.isfinite(o[..., 8:]).all() and torch.isfinite(out[:, G:].float()).all()
+
+
 @pytest.mark.parametrize("dtype,new", [(BF16, 1), (BF16, 33), (F32, 1), (F32, 33)])
 def test_scores_of_any_size(dtype, new):
     """Large and -inf scores, equal ones, a large maximum late in the view."""
