@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kTakeThreads) void paged_take_kernel(PagedAppend a)
       const int view = q.slot * hkv + h;
       const int64_t L = c.lens[view];
       if (q.n_new > 0) {
-        if (L < 0 || L + q.n_new > cap_rows(c)) {
+        if (L < 0 || L > cap_rows(c) - q.n_new) {     // (lengths of any size: L + n_new may not exist)
           s_bad[si] = 1;
           if (a.overflow) *a.overflow = 1;
         } else {
@@ -367,6 +367,10 @@ __device__ __forceinline__ PagedTake compact_take(const PagedCompact& a, int64_t
 __device__ __forceinline__ int64_t compact_len(const PagedCompact& a, int s) {
   return a.c.lens[a.slot * a.c.hkv + a.heads[s]];
 }
+// Rows before the tail of a view of L; -1: none of them can be listed.
+__device__ __forceinline__ int64_t compact_body(const PagedCompact& a, int64_t L) {
+  return L >= a.tail && L <= cap_rows(a.c) ? L - a.tail : -1;
+}
 
 // How many rows every view keeps, and where its chunks go.  Lists of up to kShortList
 // chunks are gone over by a wave each of the taking workgroup; longer ones by a workgroup
@@ -378,7 +382,7 @@ constexpr int kShortList = 512;
 __global__ __launch_bounds__(kTakeThreads) void paged_compact_list_kernel(PagedCompact a) {
   __shared__ int s_wave[kTakeWaves];
   const int s = blockIdx.x, tid = threadIdx.x;
-  const int64_t L = compact_len(a, s), n = L <= cap_rows(a.c) ? L - a.tail : -1;
+  const int64_t L = compact_len(a, s), n = compact_body(a, L);
   const int32_t* list = a.idx + (size_t)s * a.b;
   int32_t* offs = a.offs + (size_t)s * a.b;
   int rows = 0, next[4];
@@ -414,7 +418,7 @@ __global__ __launch_bounds__(kTakeThreads) void paged_compact_take_kernel(PagedC
     if (tid < a.n_sel) s_take[tid] = a.views[tid];
   } else {
     for (int s = tid >> 6; s < a.n_sel; s += kTakeWaves) {
-      const int64_t L = compact_len(a, s), n = L <= cap_rows(c) ? L - a.tail : -1;
+      const int64_t L = compact_len(a, s), n = compact_body(a, L);
       int rows = 0;
       const int32_t* list = a.idx + (size_t)s * a.b;
       int next = lane < a.b ? list[lane] : -1;

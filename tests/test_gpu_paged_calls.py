@@ -1,0 +1,38 @@
+"""Calls on caches in pages at the ends of what their arguments may be."""
+import numpy as np
+import pytest
+import torch
+
+import paged_ref as R
+import paper_2608_30295_amd as ck
+from test_gpu_paged import BF16, DEV, F32, append, cache_of, host, randn
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("L", [2 ** 63 - 1, 2 ** 63 - 5, 2 ** 62, 6 * 16 + 1, 6 * 16, 6 * 16 - 2, -1, -2 ** 63])
+def test_lengths_of_any_size_are_checked(L):
+    """A length that no call leaves, or that leaves no room for the new tokens (three are): the
+    sequence stays as it is in every call, its neighbour's rows are appended."""
+    c, s = cache_of(60, 16, 3, 2, 6, BF16)
+    append(c, s, [0, 2], [50, 40], 2, 1)
+    for h in range(2):
+        c.lens[0, h] = L if h else 50
+    before = R.Pages.of(c)
+    plan = ck.paged_plan(c, [0, 2], [3, 1], [[96] * 2] * 2, 2)
+    k, v = (randn((4, 2, 128), i, BF16) for i in (5, 6))
+    over = torch.zeros(1, dtype=torch.int32, device=DEV)
+    ck.append_kv_paged(plan, c, k, v, over)
+    assert over.item() == 1
+    before.append([2], [1], host(k[3:]), host(v[3:]))
+    before.same(c)
+    fine = 0 <= L <= 96
+    out, lse = ck.attn_paged(plan, c, randn((4, 2, 128), 7, BF16))
+    assert torch.isfinite(out.float()).all() and (fine or (out[:3, 1] == 0).all() and (lse[:3, 1] == -float("inf")).all())
+    if not fine:
+        over.zero_()
+        ck.compact_kv_paged(c, 0, [1], torch.zeros((1, 700), dtype=torch.int32, device=DEV), 1, 0, over)    # a list of its own launch
+        ck.compact_kv_paged(c, 0, [1], torch.zeros((1, 7), dtype=torch.int32, device=DEV), 1, 5, over)
+        assert over.item() == 1
+        ck.drop_paged(c, torch.tensor([0, 0, 0], device=DEV))
+        before.same(c)
