@@ -1,0 +1,108 @@
+"""Attention over caches in pages where values are not ordinary ones: results beside
+infinities of V, scores of any size, rows without weight.  Every result that is finite
+has a bound that is finite, too: what a bound counts are the rows whose scores are."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paged_ref as R
+import paper_2608_30295_amd as ck
+from test_gpu_paged import BF16, DEV, F32, append, cache_of, host, randn
+
+pytestmark = pytest.mark.gpu
+inf = float("inf")
+
+
+def reference(q, k, v, m, scale, dtype):
+    """paged_ref's results and bounds, with the largest sum of |q k| taken over the rows of
+    finite scores: the others have no weight and no part in a score's error."""
+    out, lse, A, B = R.attention(q, k, v, m, scale)
+    with np.errstate(invalid="ignore", over="ignore"):
+        for j in range(m):
+            n = max(len(k) - m + j + 1, 0)
+            s = np.asarray(q[j], np.float64) @ np.asarray(k[:n], np.float64).T * scale
+            size = np.abs(np.asarray(q[j], np.float64)) @ np.abs(np.asarray(k[:n], np.float64)).T * scale
+            B[j] = np.where(np.isfinite(s), size, 0).max(axis=1, initial=0)
+        eo, ez = R.bounds(out, lse, A, B, len(k), dtype, q.shape[0] * q.shape[1])
+    assert np.isfinite(eo[np.isfinite(out)]).all() and np.isfinite(ez[np.isfinite(lse)]).all(), "a bound that holds nothing"
+    return out, lse, eo, ez
+
+
+def check(c, plan, q, new, G, scale=None):
+    """Attention of slot 0's new tokens against the rows that the cache holds, in 64 bits."""
+    got, lse = ck.attn_paged(plan, c, q, scale=scale)
+    s, scale = R.Pages.of(c), 1 / math.sqrt(128) if scale is None else scale
+    a, b, qh = host(got).astype(np.float64), lse.cpu().numpy().astype(np.float64), host(q)
+    for h in range(c.hkv):
+        k, v = s.rows(0, h)
+        g = slice(h * G, (h + 1) * G)
+        o, z, eo, ez = reference(qh[:, g], k, v, new, scale, c.dtype)
+        x, y, fin = a[:, g], b[:, g], np.isfinite(o)
+        wrong = ~(np.isnan(o) & np.isnan(x) | (o == x)) & ~fin
+        assert not wrong.any(), f"head {h}: {[(w.tolist(), o[tuple(w)], x[tuple(w)]) for w in np.argwhere(wrong)[:4]]}"
+        err = np.where(fin, np.abs(x - np.where(fin, o, 0)), 0)
+        fine = err <= np.where(fin, eo, 0)
+        assert fine.all(), f"head {h}: off by {err[~fine].max():.3g} {np.argwhere(~fine)[:4].tolist()}"
+        fin = np.isfinite(z)
+        assert np.array_equal(z[~fin], y[~fin], equal_nan=True), f"head {h}: lse"
+        assert (np.abs(y[fin] - z[fin]) <= ez[fin]).all(), f"head {h}: lse off by {np.abs(y - z)[fin].max():.3g}"
+    return got, lse
+
+
+def view(dtype, n, new, G, hkv=1, page=32, seed=1):
+    """Slot 0 with n rows and `new` more; put(row, head, k, v, dim) changes its rows' elements."""
+    need = R.pages_of(n + new, page)
+    c, s = cache_of(hkv * need + 3, page, 1, hkv, need, dtype)
+    plan = ck.paged_plan(c, [0], [n], [[n] * hkv], hkv * G)
+    rows = [randn((n, hkv, 128), seed + i, dtype) for i in (0, 1)]
+    ck.append_kv_paged(plan, c, *rows)
+    s = R.Pages.of(c)
+    plan = append(c, s, [0], [new], hkv * G, seed + 2)
+    table = s.table[0]
+
+    def put(row, k=None, v=None, dim=slice(None), head=0):
+        p, r = int(table[head, row // page]), row % page
+        if k is not None:
+            c.k[p, r, dim] = k
+        if v is not None:
+            c.v[p, r, dim] = v
+    return c, plan, put
+
+
+FORMS = [(BF16, 4, 60, 1), (BF16, 4, 150, 1), (BF16, 2, 9000, 3), (BF16, 8, 70000, 1), (BF16, 8, 700, 30), (BF16, 1, 9000, 300),
+         (F32, 4, 60, 1), (F32, 4, 150, 1), (F32, 1, 9000, 3), (F32, 4, 40000, 1), (F32, 4, 700, 30), (F32, 2, 3000, 130)]
+
+
+@pytest.mark.parametrize("dtype,G,n,new", FORMS)
+def test_finite_results_beside_infinities(dtype, G, n, new):
+    """V of both infinities and NaN in some dims, rows that all tokens see and the last ones':
+    the other dims and the log-sum-exp are what they are without."""
+    c, plan, put = view(dtype, n, new, G, hkv=2)
+    q = randn((new, 2 * G, 128), 5, dtype)
+    for row, dim, x in ((20, 3, inf), (40, 4, -inf), (21, 5, inf), (n - 1, 5, -inf), (22, 6, math.nan), (n, 7, inf), (n + new - 1, 8, -inf)):
+        put(row, v=x, dim=dim)
+    out, _ = check(c, plan, q, new, G)
+    assert torch.isfinite(out[:, :G, 9:].float()).all() and torch.isfinite(out[:, G:].float()).all()
+
+
+@pytest.mark.parametrize("dtype,G,n,new", FORMS)
+def test_equal_scores_of_any_size_weigh_the_same(dtype, G, n, new):
+    """All keys the same, scores of 1e-30 to -1e38: the mean of what a token sees of V, within
+    what sums and the result's rounding add (weights are exactly 1)."""
+    c, plan, put = view(dtype, n, new, G)
+    q = (randn((new, G, 128), 5).abs() + 0.5).to(dtype)
+    v = R.Pages.of(c).rows(0, 0)[1].astype(np.float64)
+    mean = np.cumsum(v, axis=0)[n:] / np.arange(n + 1, n + new + 1)[:, None]
+    size = np.cumsum(np.abs(v), axis=0)[n:] / np.arange(n + 1, n + new + 1)[:, None]
+    half = torch.finfo(dtype).eps / 2
+    bound = 2 * (n + new + 200) * 2.0 ** -24 * size + half * np.abs(mean) + 1e-30
+    for x, scale in ((-1e36, 0.01), (-1e36, 0.7), (-3e9, 1.0), (1e20, 0.125), (1e-30, 0.125)):
+        c.k.fill_(x)
+        out, lse = ck.attn_paged(plan, c, q, scale=scale)
+        err = np.abs(host(out).astype(np.float64) - mean[:, None])
+        assert (err <= bound[:, None] * 1.01).all(), f"{x} {scale}: off by {err.max():.3g}"
+        z = (host(q).astype(np.float64).sum(-1) * float(c.k[0, 0, 0]) * scale) + np.log(np.arange(n + 1, n + new + 1))[:, None]
+        off = np.abs(lse.cpu().numpy() - z)
+        assert (off <= 140 * 2.0 ** -24 * np.abs(z) + 2 * (n + new + 200) * 2.0 ** -24).all(), f"{x} {scale}: lse off by {off.max():.3g}"
