@@ -100,8 +100,9 @@ struct PagedJoin {
   int32_t view, tok0, n_new, row0;
   int32_t slot, n_parts, rows, pad;
 };
-// A partial slot of R rows: o [R][128], then m [R] and l [R]: o = sum exp2(s - m) v and
-// l = sum exp2(s - m) of the scaled scores s in units of log2; m = -inf: no row.
+// A partial slot of R rows: o [R][128], then m [R] and l [R]: o = sum exp2(c (s - m)) v and
+// l = sum exp2(c (s - m)) of the scores s as the products give them, c = log2_scale; m = -inf:
+// no row.
 constexpr size_t paged_slot_floats(int R) { return (size_t)R * (kD + 2); }
 
 constexpr int kStreamRows = 16;     // new rows of a stream piece at most (the 16 columns of an MFMA)

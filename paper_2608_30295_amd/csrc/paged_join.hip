@@ -26,12 +26,12 @@ __device__ __forceinline__ void join_rows(const PagedAttn& a, const PagedJoin& j
     for (int p = g + lane * S; p < j.n_parts; p += 32 * S) M = fmaxf(M, ms[p * step]);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
+    const float f = pg_factor(M, a.log2_scale);
 #pragma unroll 4
     for (int p = g; p < j.n_parts; p += S) {
       const float mp = ms[p * step], lp = ms[p * step + j.rows];
       const float4 v = *reinterpret_cast<const float4*>(slot + p * step + (size_t)at * kD + lane * 4);
-      const bool some = mp != -INFINITY;               // a part without rows holds zeros
-      const float w = some ? fast_exp2(mp - M) : 0.f;
+      const float w = pg_share(mp, M, f);              // a part without rows holds zeros
       l += w * lp;
       x[0] += w * v.x;
       x[1] += w * v.y;
@@ -50,10 +50,11 @@ __device__ __forceinline__ void join_rows(const PagedAttn& a, const PagedJoin& j
     M = -INFINITY;
 #pragma unroll
     for (int i = 0; i < S; ++i) M = fmaxf(M, s_m[i][row]);
+    const float f = pg_factor(M, a.log2_scale);
     l = x[0] = x[1] = x[2] = x[3] = 0.f;
 #pragma unroll
     for (int i = 0; i < S; ++i) {
-      const float mi = s_m[i][row], w = mi == -INFINITY ? 0.f : fast_exp2(mi - M);
+      const float w = pg_share(s_m[i][row], M, f);
       const float4 v = *reinterpret_cast<const float4*>(&s_x[i][row][lane * 4]);
       l += w * s_l[i][row];
       x[0] += w * v.x;
@@ -68,7 +69,7 @@ __device__ __forceinline__ void join_rows(const PagedAttn& a, const PagedJoin& j
   const int tok = r / G, h = j.view % a.c.hkv;
   const size_t q = (size_t)(j.tok0 + tok) * a.hq + h * G + (r - tok * G);
   pg_put4((T*)nullptr, a.out + (q * kD + lane * 4) * sizeof(T), x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-  if (a.lse && lane == 0) a.lse[q] = none ? -INFINITY : (M + __builtin_amdgcn_logf(l)) * kLn2;
+  if (a.lse && lane == 0) a.lse[q] = pg_lse(M, l, a.log2_scale);
 }
 
 // Workgroup b of a join: the tiles' come first, then those of few new rows.

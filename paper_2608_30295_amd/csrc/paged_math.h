@@ -25,10 +25,24 @@ __device__ __forceinline__ float pg_factor(float m, float c) {
   return fabsf(m) * c < 536870912.f || m == -INFINITY ? c : __uint_as_float(__float_as_uint(c) & 0x7f800000u);
 }
 
-// A row's maximum as results and partial slots take it, in units of log2.  -inf stands for
-// a row without scores above -inf, whose sum is 0; where all scores are NaN the maximum stays
-// at -inf, too, but the sum is NaN and has to come through.
-__device__ __forceinline__ float pg_top(float m, float l, float c) { return m > -INFINITY ? m * c : l != l ? 0.f : -INFINITY; }
+// A row's maximum as results and partial slots take it.  -inf stands for a row without
+// scores above -inf, whose sum is 0; where all scores are NaN the maximum stays at -inf, too,
+// but the sum is NaN and has to come through.
+__device__ __forceinline__ float pg_top(float m, float l) { return m > -INFINITY ? m : l != l ? 0.f : -INFINITY; }
+
+// What a part of maximum m counts for beside the largest maximum M, f = pg_factor(M, c).  The
+// products are rounded each, as those that the parts' weights refer to are; scores that differ
+// must not meet in them, so that maxima stay unscaled until here.
+__device__ __forceinline__ float pg_share(float m, float M, float f) {
+#pragma clang fp contract(off)
+  return m == -INFINITY ? 0.f : fast_exp2(m * f - M * f);
+}
+
+// The log-sum-exp of a row of maximum M and sum l.
+__device__ __forceinline__ float pg_lse(float M, float l, float c) {
+#pragma clang fp contract(off)
+  return M == -INFINITY ? -INFINITY : (M * c + __builtin_amdgcn_logf(l)) * kLn2;
+}
 
 // bf16 pair (to nearest, ties to even) of two fp32 values, x in the low half.
 __device__ __forceinline__ uint32_t pg_pack2(float x, float y) {

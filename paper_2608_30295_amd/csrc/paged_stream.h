@@ -324,7 +324,7 @@ __device__ __forceinline__ void stream_share(const PagedAttn& a, const PagedPiec
           *reinterpret_cast<float4*>(&s_o[wave][n16][X::dim(x, k4, i)]) =
               make_float4(o[4 * x][i], o[4 * x + 1][i], o[4 * x + 2][i], o[4 * x + 3][i]);
       if (k4 == 0) {
-        s_m[wave][n16] = pg_top(m, l, cs);
+        s_m[wave][n16] = pg_top(m, l);
         s_l[wave][n16] = l;
       }
       barrier_lds_only();
@@ -334,11 +334,12 @@ __device__ __forceinline__ void stream_share(const PagedAttn& a, const PagedPiec
         float M = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kStreamWaves; ++w) M = fmaxf(M, s_m[w][r]);
+        const float fM = pg_factor(M, cs);
         float sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < kStreamWaves; ++w) {
           const float mw = s_m[w][r];
-          const float f = mw == -INFINITY ? 0.f : fast_exp2(mw - M);
+          const float f = pg_share(mw, M, fM);
           const float4 v = *reinterpret_cast<const float4*>(&s_o[w][r][d]);
           if (mw == -INFINITY) continue;
           sum += f * s_l[w][r];
@@ -360,7 +361,7 @@ __device__ __forceinline__ void stream_share(const PagedAttn& a, const PagedPiec
           const int tok = r / G;
           const size_t row = (size_t)sg.q0 + (size_t)tok * a.hq + (r - tok * G);
           pg_put4((T*)nullptr, a.out + (row * kD + d) * sizeof(T), x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-          if (a.lse && d == 0) a.lse[row] = none ? -INFINITY : (M + __builtin_amdgcn_logf(sum)) * kLn2;
+          if (a.lse && d == 0) a.lse[row] = pg_lse(M, sum, cs);
         }
       }
     };

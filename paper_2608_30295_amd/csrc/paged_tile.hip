@@ -461,8 +461,8 @@ void paged_tile_kernel(PagedAttn a) {
       const int hi = lane >> 5, tok = row / G;
       const size_t qrow = ((size_t)(x.tok0 + tok) * a.hq + (x.view % c.hkv) * G + (row - tok * G)) * kRB;
       const float sum = add_xor32(l);                  // lanes l and l ^ 32 hold the same row
-      const float mc = pg_top(m, sum, cs);
-      const bool none = mc == -INFINITY;
+      const float top = pg_top(m, sum);
+      const bool none = top == -INFINITY;
       if (x.slot >= 0) {
         float* slot = a.slots + (size_t)x.slot * 4;
 #pragma unroll
@@ -472,7 +472,7 @@ void paged_tile_kernel(PagedAttn a) {
             *reinterpret_cast<float4*>(slot + (size_t)at * kD + d * 32 + 8 * i + 4 * hi) =
                 make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
         if (hi == 0) {
-          slot[kTileRows * kD + at] = mc;
+          slot[kTileRows * kD + at] = top;
           slot[kTileRows * (kD + 1) + at] = sum;
         }
       } else {
@@ -494,7 +494,7 @@ void paged_tile_kernel(PagedAttn a) {
             const auto hi2 = __builtin_amdgcn_permlane32_swap(y[0][1], y[1][1], false, false);
             *reinterpret_cast<uint4*>(out + (d * 32 + 8 * (i + hi)) * 2) = make_uint4(lo[0], hi2[0], lo[1], hi2[1]);
           }
-        if (a.lse && hi == 0) a.lse[qrow / kRB] = none ? -INFINITY : (mc + __builtin_amdgcn_logf(sum)) * kLn2;
+        if (a.lse && hi == 0) a.lse[qrow / kRB] = pg_lse(top, sum, cs);
       }
     }
     if (!more) break;

@@ -190,8 +190,8 @@ void paged_tile_f32_kernel(PagedAttn a) {
     }
     if (!mine) continue;
     l = add_xor32(l);                                  // lanes l and l ^ 32 hold the same row
-    const float mc = pg_top(m, l, cs);
-    const bool none = mc == -INFINITY;
+    const float top = pg_top(m, l);
+    const bool none = top == -INFINITY;
     // a partial result is taken as it is, a whole one divided by its sum
     const bool part = pc.slot >= 0;
     const float inv = part ? 1.f : none ? 0.f : 1.f / l;
@@ -209,10 +209,10 @@ void paged_tile_f32_kernel(PagedAttn a) {
     if (hi != 0) continue;
     if (part) {
       float* slot = a.slots + (size_t)pc.slot * 4;
-      slot[kTileRowsF32 * kD + at] = mc;
+      slot[kTileRowsF32 * kD + at] = top;
       slot[kTileRowsF32 * (kD + 1) + at] = l;
     } else if (a.lse) {
-      a.lse[qrow / kRB] = none ? -INFINITY : (mc + __builtin_amdgcn_logf(l)) * kLn2;
+      a.lse[qrow / kRB] = pg_lse(top, l, cs);
     }
   }
 }

@@ -106,3 +106,41 @@ def test_equal_scores_of_any_size_weigh_the_same(dtype, G, n, new):
         z = (host(q).astype(np.float64).sum(-1) * float(c.k[0, 0, 0]) * scale) + np.log(np.arange(n + 1, n + new + 1))[:, None]
         off = np.abs(lse.cpu().numpy() - z)
         assert (off <= 140 * 2.0 ** -24 * np.abs(z) + 2 * (n + new + 200) * 2.0 ** -24).all(), f"{x} {scale}: lse off by {off.max():.3g}"
+
+
+def neighbours(scale):
+    """Scores as far below 0 as fp32 still tells apart by 64 powers of two and more: one, and the
+    next above it, whose products with the scale round to the same number."""
+    c = np.float32(1.4426950408889634) * np.float32(scale)
+    for i in range(1, 4096):
+        x = -np.float32(2.0 ** 34) * np.float32(1 + i / 4096)
+        up = np.nextafter(x, np.float32(0))
+        if x * c == up * c:
+            return float(x), float(up) - float(x)
+    raise AssertionError("no such pair")
+
+
+@pytest.mark.parametrize("at", [0.1, 0.5, 1.0])
+@pytest.mark.parametrize("dtype,G,n,new", FORMS)
+def test_the_larger_of_two_huge_scores_wins(dtype, G, n, new, at):
+    """Scores one step of fp32 apart, far from 0: the row that has the larger one is the result,
+    also where it meets the others only as a part's or a wave's maximum."""
+    scale = 0.125
+    base, step = neighbours(scale)
+    c, plan, put = view(dtype, n, new, G)
+    q = torch.zeros((new, G, 128), dtype=dtype, device=DEV)
+    q[..., :8] = 1
+    hi = np.float32(torch.tensor(base).to(BF16).float().item())   # base in parts that bf16 holds
+    lo = np.float32(base) - hi
+    assert np.float32(torch.tensor(float(lo)).to(BF16).float().item()) == lo and np.float32(hi) + lo == np.float32(base)
+    c.k.zero_()
+    c.k[..., 0], c.k[..., 1] = float(hi), float(lo)
+    win = int(at * (n - 1))
+    put(win, k=step, dim=2)
+    out, lse = ck.attn_paged(plan, c, q, scale=scale)
+    v = host(c.v)[int(c.table[0, 0, win // 32]), win % 32].astype(np.float64)
+    # the others: n + new of them at most, 2^-32 each
+    err = np.abs(host(out).astype(np.float64) - v)
+    assert (err <= torch.finfo(dtype).eps / 2 * np.abs(v) + (n + new) * 2.0 ** -32 * 8 + 2.0 ** -22 * np.abs(v)).all(), f"off by {err.max():.3g}"
+    z = (base + step) * scale
+    assert (np.abs(lse.cpu().numpy() - z) <= 2.0 ** -22 * abs(z)).all()
