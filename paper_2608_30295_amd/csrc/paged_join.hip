@@ -33,10 +33,10 @@ __device__ __forceinline__ void join_rows(const PagedAttn& a, const PagedJoin& j
       const float4 v = *reinterpret_cast<const float4*>(slot + p * step + (size_t)at * kD + lane * 4);
       const float w = pg_share(mp, M, f);              // a part without rows holds zeros
       l += w * lp;
-      x[0] += w * v.x;
-      x[1] += w * v.y;
-      x[2] += w * v.z;
-      x[3] += w * v.w;
+      x[0] = pg_add(x[0], w, v.x);
+      x[1] = pg_add(x[1], w, v.y);
+      x[2] = pg_add(x[2], w, v.z);
+      x[3] = pg_add(x[3], w, v.w);
     }
   }
   if (S > 1) {
@@ -57,10 +57,10 @@ __device__ __forceinline__ void join_rows(const PagedAttn& a, const PagedJoin& j
       const float w = pg_share(s_m[i][row], M, f);
       const float4 v = *reinterpret_cast<const float4*>(&s_x[i][row][lane * 4]);
       l += w * s_l[i][row];
-      x[0] += w * v.x;
-      x[1] += w * v.y;
-      x[2] += w * v.z;
-      x[3] += w * v.w;
+      x[0] = pg_add(x[0], w, v.x);
+      x[1] = pg_add(x[1], w, v.y);
+      x[2] = pg_add(x[2], w, v.z);
+      x[3] = pg_add(x[3], w, v.w);
     }
   }
   if (!mine) return;

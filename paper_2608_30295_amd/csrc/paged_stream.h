@@ -142,6 +142,28 @@ struct StreamLds {
   float (*m)[kStreamWaves][R], (*l)[kStreamWaves][R];
 };
 
+// What a wave wrote of a segment's results, rows 2 wave and 2 wave + 1 (`skip`: bits of those
+// that stay), where V is not finite.  A function of its own, so that the kernel has all
+// registers to itself (inlined, one fp32 token over 65536 rows took 115 to 125 us for 105).
+constexpr int kOwnRows = R / kStreamWaves;
+template <typename T, int G>
+__device__ __attribute__((noinline)) void stream_restore(const char* v, const int32_t* ids, int n_pages, int page_log, int t0, int t1, int see0,
+                                                         int rows, int skip, float* slot, char* out, int q0, int hq) {
+  PagedCache c{};
+  c.v = const_cast<char*>(v);
+  c.n_pages = n_pages;
+  c.page_log = page_log;
+  c.max_pages = INT32_MAX;                    // the rows are the view's
+  const int lane = threadIdx.x & 63, own = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kOwnRows;
+  __builtin_amdgcn_s_waitcnt(0);              // the results lie where they belong
+  pg_restore<T, kOwnRows>(c, ids, t0, t1, min(see0 + (lane & 15) / G, t1), own, [&](int r, float x, float y) {
+    if (r >= rows) return;
+    const int tok = r / G;
+    if (slot) pg_over(slot + r * kD + 2 * lane, x, y);
+    else if (!(skip >> (r - own) & 1)) pg_over(reinterpret_cast<T*>(out) + ((size_t)q0 + (size_t)tok * hq + (r - tok * G)) * kD + 2 * lane, x, y);
+  });
+}
+
 // A workgroup's share: segments [first, last).
 template <typename T, int G, int kBatch>
 __device__ __forceinline__ void stream_share(const PagedAttn& a, const PagedPiece* pieces, int first, int last,
@@ -231,6 +253,7 @@ __device__ __forceinline__ void stream_share(const PagedAttn& a, const PagedPiec
     float m, l;
     float cw;                                         // of the weights: pg_factor()
     bool purged;                                      // a tile of the segment, in the wave
+    int odd = 0, kept = 0;                            // bits of segments: results to be taken from V, and rows that are not
     int cur = 0;
     auto begin = [&]() __attribute__((always_inline)) {
       m = -INFINITY;
@@ -329,7 +352,8 @@ __device__ __forceinline__ void stream_share(const PagedAttn& a, const PagedPiec
       }
       barrier_lds_only();
       const Seg sg = s_seg[cur];
-      for (int t = threadIdx.x; t < sg.rows * (kD / 4); t += kStreamThreads) {
+      bool bad = false, keep = false;
+      for (int t = threadIdx.x; t < sg.rows * (kD / 4); t += kStreamThreads) {   // one turn at most
         const int r = t / (kD / 4), d = (t - r * (kD / 4)) * 4;
         float M = -INFINITY;
 #pragma unroll
@@ -348,6 +372,9 @@ __device__ __forceinline__ void stream_share(const PagedAttn& a, const PagedPiec
           x[2] += f * v.z;
           x[3] += f * v.w;
         }
+        const bool none = M == -INFINITY;
+        bad = sum == sum && pg_unusual(x);
+        keep = none || sum != sum;
         if (sg.slot >= 0) {
           float* slot = a.slots + (size_t)sg.slot * 4;
           *reinterpret_cast<float4*>(slot + r * kD + d) = make_float4(x[0], x[1], x[2], x[3]);
@@ -356,13 +383,17 @@ __device__ __forceinline__ void stream_share(const PagedAttn& a, const PagedPiec
             slot[R * (kD + 1) + r] = sum;
           }
         } else {
-          const bool none = M == -INFINITY;
           const float inv = none ? 0.f : 1.f / sum;
           const int tok = r / G;
           const size_t row = (size_t)sg.q0 + (size_t)tok * a.hq + (r - tok * G);
           pg_put4((T*)nullptr, a.out + (row * kD + d) * sizeof(T), x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
           if (a.lse && d == 0) a.lse[row] = pg_lse(M, sum, cs);
         }
+      }
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(bad) != 0, 0)) {         // half a wave has a row
+        const uint64_t k = __builtin_amdgcn_ballot_w64(keep);
+        odd |= 1 << cur;
+        kept |= (int)((k & 1) | (k >> 31 & 2)) << kOwnRows * cur;
       }
     };
     auto use = [&](auto tag) __attribute__((always_inline)) {
@@ -405,6 +436,13 @@ __device__ __forceinline__ void stream_share(const PagedAttn& a, const PagedPiec
       if (++cur == nseg) break;
       begin();
     }
+
+    for (int i = 0; odd >> i; ++i)                    // results that are not finite
+      if (odd >> i & 1) {
+        const Seg sg = s_seg[i];
+        stream_restore<T, G>(c.v, c.table + (size_t)sg.view * c.max_pages, c.n_pages, c.page_log, sg.t0, sg.t_end, sg.see0, sg.rows,
+                             kept >> kOwnRows * i & 3, sg.slot >= 0 ? a.slots + (size_t)sg.slot * 4 : nullptr, a.out, sg.q0, a.hq);
+      }
   }
 }
 

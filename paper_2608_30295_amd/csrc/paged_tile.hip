@@ -247,7 +247,7 @@ void paged_tile_kernel(PagedAttn a) {
   };
 
   // ---- V that is not finite in masked tiles ------------------------------------------
-  // 0 * NaN is NaN: such values are taken out of the tile, and added to the sums of the new
+  // 0 * NaN is NaN: such values are taken out of the tile, and go into the sums of the new
   // rows that see them at the piece's end.  Every thread looks at its part of the tile; a
   // barrier later all waves know.
   int tag = 0;                                         // of the masked tile
@@ -275,25 +275,6 @@ void paged_tile_kernel(PagedAttn a) {
     }
     barrier_lds_only();
   };
-  // what was taken out of tiles first ... of piece x
-  auto restore = [&](const Piece& x, int first) __attribute__((always_inline)) {
-#pragma unroll 1
-    for (int r = x.t0 + first * kTile; r < x.t0 + x.n_tiles * kTile; ++r) {
-      const int id = pg_entry(c.table + (size_t)x.view * c.max_pages, min(r >> c.page_log, c.max_pages - 1));
-      const char* from = c.v + (pg_page(c, id) + (r & mask)) * kRB + (lane >> 5) * 8;
-      const bool sees = r < see;
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {                  // dims 32 d + 8 i + 4 (l / 32) + [0, 4)
-          const uint2 y = *reinterpret_cast<const uint2*>(from + (32 * d + 8 * i) * 2);
-          const float z[4] = {bf16_lo(y.x), bf16_hi(y.x), bf16_lo(y.y), bf16_hi(y.y)};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[d][4 * i + e] += sees && pg_bad32(z[e]) ? z[e] : 0.f;
-        }
-    }
-  };
-
   Ids next = {}, after = {};                           // pages of the tile after the one whose scores are there, and of the one behind
 
   // ---- turns -----------------------------------------------------------------------
@@ -455,12 +436,15 @@ void paged_tile_kernel(PagedAttn a) {
     }
 
     // ---- results -------------------------------------------------------------------
-    if (purged) restore(x, first);
+    const float sum = add_xor32(l);                    // lanes l and l ^ 32 hold the same row
+    float sums[64];
+#pragma unroll
+    for (int i = 0; i < 64; ++i) sums[i] = o[i >> 4][i & 15];
+    const bool unusual = purged || __builtin_amdgcn_ballot_w64(sum == sum && pg_unusual(sums));
     const int at = wave * 32 + (lane & 31), row = x.row0 + at;
     if (row < x.n_new * G) {
       const int hi = lane >> 5, tok = row / G;
       const size_t qrow = ((size_t)(x.tok0 + tok) * a.hq + (x.view % c.hkv) * G + (row - tok * G)) * kRB;
-      const float sum = add_xor32(l);                  // lanes l and l ^ 32 hold the same row
       const float top = pg_top(m, sum);
       const bool none = top == -INFINITY;
       if (x.slot >= 0) {
@@ -496,6 +480,22 @@ void paged_tile_kernel(PagedAttn a) {
           }
         if (a.lse && hi == 0) a.lse[qrow / kRB] = pg_lse(top, sum, cs);
       }
+    }
+    if (unusual) {
+      const uint64_t fine = __builtin_amdgcn_ballot_w64(m > -INFINITY && sum == sum);
+      __builtin_amdgcn_s_waitcnt(0);                   // the results lie where they belong
+#pragma unroll 1
+      for (int r0 = 0; r0 < 32; r0 += 4)
+        pg_restore<uint16_t, 4>(c, c.table + (size_t)x.view * c.max_pages, x.t0, x.t0 + x.n_tiles * kTile, see, r0, [&](int i, float u, float v) {
+          const int y = wave * 32 + i, r = x.row0 + y, tok = r / G;
+          if (r >= x.n_new * G) return;
+          if (x.slot >= 0) {
+            pg_over(a.slots + (size_t)x.slot * 4 + (size_t)y * kD + 2 * lane, u, v);
+          } else if (fine >> i & 1) {
+            const size_t qr = (size_t)(x.tok0 + tok) * a.hq + (x.view % c.hkv) * G + (r - tok * G);
+            pg_over(reinterpret_cast<uint16_t*>(a.out) + qr * kD + 2 * lane, u, v);
+          }
+        });
     }
     if (!more) break;
     ++w;

@@ -99,7 +99,7 @@ void paged_tile_f32_kernel(PagedAttn a) {
       if (t + 1 < n_tiles) issue(B ? s_k0 : s_k1, B ? s_v0 : s_v1, t + 1);
       const int r0 = pc.t0 + t * kTile;
       if (t >= n_full) {
-        // 0 * NaN is NaN: V that is not finite is taken out of a masked tile, and added to the
+        // 0 * NaN is NaN: V that is not finite is taken out of a masked tile, and goes into the
         // sums of the new rows that see it at the piece's end.  A thread looks at its part.
         ++tag;
         bool bad = false;
@@ -172,47 +172,51 @@ void paged_tile_f32_kernel(PagedAttn a) {
       if (t + 1 < n_tiles) step(S1{}, t + 1);
     }
 
-    if (purged) {
-#pragma unroll 1
-      for (int r = pc.t0 + n_full * kTile; r < pc.t0 + n_tiles * kTile; ++r) {
-        const size_t at = (pg_page(c, pg_entry(ids, min(r >> c.page_log, c.max_pages - 1))) + (r & mask)) * kRB;
-        const bool sees = r < see;
+    l = add_xor32(l);                                  // lanes l and l ^ 32 hold the same row
+    float sums[64];
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+    for (int i = 0; i < 64; ++i) sums[i] = o[i >> 4][i & 15];
+    const bool unusual = purged || __builtin_amdgcn_ballot_w64(l == l && pg_unusual(sums));
+    if (mine) {
+      const float top = pg_top(m, l);
+      const bool none = top == -INFINITY;
+      // a partial result is taken as it is, a whole one divided by its sum
+      const bool part = pc.slot >= 0;
+      const float inv = part ? 1.f : none ? 0.f : 1.f / l;
+      const int at = row - pc.row0;
+      float* out = part ? a.slots + (size_t)pc.slot * 4 + (size_t)at * kD : reinterpret_cast<float*>(a.out + qrow);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {                // dims 32 d + 8 i + 4 hi + [0, 4)
-            const float4 z = *reinterpret_cast<const float4*>(c.v + at + (32 * d + 8 * i + 4 * hi) * 4);
-            const float f[4] = {z.x, z.y, z.z, z.w};
+      for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[d][4 * i + e] += sees && pg_bad32(f[e]) ? f[e] : 0.f;
-          }
+        for (int i = 0; i < 4; ++i) {
+          float f[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f[e] = !part && none ? 0.f : o[d][4 * i + e] * inv;
+          *reinterpret_cast<float4*>(out + d * 32 + 8 * i + 4 * hi) = make_float4(f[0], f[1], f[2], f[3]);
+        }
+      if (hi == 0 && part) {
+        float* slot = a.slots + (size_t)pc.slot * 4;
+        slot[kTileRowsF32 * kD + at] = top;
+        slot[kTileRowsF32 * (kD + 1) + at] = l;
+      } else if (hi == 0 && a.lse) {
+        a.lse[qrow / kRB] = pg_lse(top, l, cs);
       }
     }
-    if (!mine) continue;
-    l = add_xor32(l);                                  // lanes l and l ^ 32 hold the same row
-    const float top = pg_top(m, l);
-    const bool none = top == -INFINITY;
-    // a partial result is taken as it is, a whole one divided by its sum
-    const bool part = pc.slot >= 0;
-    const float inv = part ? 1.f : none ? 0.f : 1.f / l;
-    const int at = row - pc.row0;
-    float* out = part ? a.slots + (size_t)pc.slot * 4 + (size_t)at * kD : reinterpret_cast<float*>(a.out + qrow);
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float f[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = !part && none ? 0.f : o[d][4 * i + e] * inv;
-        *reinterpret_cast<float4*>(out + d * 32 + 8 * i + 4 * hi) = make_float4(f[0], f[1], f[2], f[3]);
-      }
-    if (hi != 0) continue;
-    if (part) {
-      float* slot = a.slots + (size_t)pc.slot * 4;
-      slot[kTileRowsF32 * kD + at] = top;
-      slot[kTileRowsF32 * (kD + 1) + at] = l;
-    } else if (a.lse) {
-      a.lse[qrow / kRB] = pg_lse(top, l, cs);
+    if (unusual) {
+      const uint64_t fine = __builtin_amdgcn_ballot_w64(m > -INFINITY && l == l);
+      __builtin_amdgcn_s_waitcnt(0);                   // the results lie where they belong
+#pragma unroll 1
+      for (int r0 = 0; r0 < 32; r0 += 4)
+        pg_restore<float, 4>(c, ids, pc.t0, pc.t0 + n_tiles * kTile, see, r0, [&](int i, float u, float v) {
+          const int y = wave * 32 + i, r = pc.row0 + y, tk = r / G;
+          if (r >= n_rows) return;
+          if (pc.slot >= 0) {
+            pg_over(a.slots + (size_t)pc.slot * 4 + (size_t)y * kD + 2 * lane, u, v);
+          } else if (fine >> i & 1) {
+            const size_t qr = (size_t)(pc.tok0 + tk) * a.hq + h * G + (r - tk * G);
+            pg_over(reinterpret_cast<float*>(a.out) + qr * kD + 2 * lane, u, v);
+          }
+        });
     }
   }
 }

@@ -144,3 +144,24 @@ def test_the_larger_of_two_huge_scores_wins(dtype, G, n, new, at):
     assert (err <= torch.finfo(dtype).eps / 2 * np.abs(v) + (n + new) * 2.0 ** -32 * 8 + 2.0 ** -22 * np.abs(v)).all(), f"off by {err.max():.3g}"
     z = (base + step) * scale
     assert (np.abs(lse.cpu().numpy() - z) <= 2.0 ** -22 * abs(z)).all()
+
+
+@pytest.mark.parametrize("at", [0.0, 0.5, 1.0])
+@pytest.mark.parametrize("dtype,G,n,new", FORMS)
+def test_infinities_in_rows_of_next_to_no_weight(dtype, G, n, new, at):
+    """Infinite V in rows whose scores lie about 200 powers of two below one row's, in every part
+    of the view: a weight that no fp32 number holds is still one, and its product infinite."""
+    c, plan, put = view(dtype, n, new, G)
+    q = randn((1, G, 128), 5, dtype).expand(new, -1, -1).contiguous()
+    top = int(at * (n - G))
+    for g in range(G):                                            # a row for every head of the group
+        put(top + g, k=(q[0, g].float() * 12.4).to(dtype))
+    rows = sorted({int(x) for x in np.linspace(0, n - 1, 120)} - set(range(top, top + G)))[:120]
+    for i, row in enumerate(rows):
+        put(row, v=inf if i % 2 else -inf, dim=i)
+    put(rows[3], v=-inf, dim=len(rows) + 1)                       # and both in one dim
+    put(rows[-3], v=inf, dim=len(rows) + 1)
+    out, _ = check(c, plan, q, new, G)
+    o = out.float()
+    assert torch.isinf(o[..., :len(rows)]).all() and torch.isnan(o[..., len(rows) + 1]).all()
+    assert torch.isfinite(o[..., len(rows) + 2:]).all()
