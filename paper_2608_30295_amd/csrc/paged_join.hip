@@ -31,7 +31,7 @@ __device__ __forceinline__ void join_rows(const PagedAttn& a, const PagedJoin& j
     for (int p = g; p < j.n_parts; p += S) {
       const float mp = ms[p * step], lp = ms[p * step + j.rows];
       const float4 v = *reinterpret_cast<const float4*>(slot + p * step + (size_t)at * kD + lane * 4);
-      const float w = pg_share(mp, M, f);              // a part without rows holds zeros
+      const float w = pg_share(mp, M, f);              // no finite score: zeros, or what V makes of rows without weight
       l += w * lp;
       x[0] = pg_add(x[0], w, v.x);
       x[1] = pg_add(x[1], w, v.y);
@@ -68,7 +68,8 @@ __device__ __forceinline__ void join_rows(const PagedAttn& a, const PagedJoin& j
   const float inv = none ? 0.f : 1.f / l;
   const int tok = r / G, h = j.view % a.c.hkv;
   const size_t q = (size_t)(j.tok0 + tok) * a.hq + h * G + (r - tok * G);
-  pg_put4((T*)nullptr, a.out + (q * kD + lane * 4) * sizeof(T), x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+  pg_put4((T*)nullptr, a.out + (q * kD + lane * 4) * sizeof(T), none ? 0.f : x[0] * inv, none ? 0.f : x[1] * inv,
+          none ? 0.f : x[2] * inv, none ? 0.f : x[3] * inv);
   if (a.lse && lane == 0) a.lse[q] = pg_lse(M, l, a.log2_scale);
 }
 

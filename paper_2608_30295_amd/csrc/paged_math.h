@@ -95,14 +95,6 @@ __device__ __forceinline__ uint32_t pg_clean16(uint32_t x) { return pg_bad16(x) 
 template <class F>
 __device__ __forceinline__ uint32_t pg_both(uint32_t w, F f) { return f(w & 0xffffu) | (uint32_t)f(w >> 16) << 16; }
 __device__ __forceinline__ bool pg_bad32(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
-__device__ __forceinline__ bool pg_any_bad(const uint16_t*, const uint4& x) {
-  return pg_bad16(x.x) || pg_bad16(x.x >> 16) || pg_bad16(x.y) || pg_bad16(x.y >> 16) || pg_bad16(x.z) || pg_bad16(x.z >> 16) ||
-         pg_bad16(x.w) || pg_bad16(x.w >> 16);
-}
-__device__ __forceinline__ bool pg_any_bad(const float*, const uint4& x) {
-  return pg_bad32(__uint_as_float(x.x)) || pg_bad32(__uint_as_float(x.y)) || pg_bad32(__uint_as_float(x.z)) || pg_bad32(__uint_as_float(x.w));
-}
-
 __device__ __forceinline__ void pg_pair(const uint16_t* p, float& x, float& y) {
   const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
   x = bf16_lo(w);
@@ -113,22 +105,13 @@ __device__ __forceinline__ void pg_pair(const float* p, float& x, float& y) {
   x = w.x;
   y = w.y;
 }
-// x and y into the elements p[0] and p[1], if they are not 0
-__device__ __forceinline__ void pg_over(uint16_t* p, float x, float y) {
-  const uint32_t w = pg_pack2(x, y);
-  if (x != 0.f) p[0] = (uint16_t)w;
-  if (y != 0.f) p[1] = (uint16_t)(w >> 16);
-}
-__device__ __forceinline__ void pg_over(float* p, float x, float y) {
-  if (x != 0.f) p[0] = x;
-  if (y != 0.f) p[1] = y;
-}
+__device__ __forceinline__ void pg_store(uint16_t* p, float x) { *p = (uint16_t)pg_pack2(x, 0.f); }
+__device__ __forceinline__ void pg_store(float* p, float x) { *p = x; }
 
 // An infinite V in a row of finite score is infinite in the result, whatever the row's weight:
 // next to a score 150 powers of two higher its fp32 weight is 0, and 0 inf NaN.  Sums that
 // turned out not to be finite are therefore taken from V itself, once a piece's results are
-// stored, and where parts are joined such a value is not scaled.  (In the results' place, when
-// the sums' registers are free: this is to take none from what runs always.)
+// stored, and where parts are joined such a value is not scaled.
 
 // Whether any of n sums (n even) is not finite (or any two have a product that is not).
 template <int N>
@@ -141,51 +124,99 @@ __device__ __forceinline__ bool pg_unusual(const float (&o)[N]) {
 // sum + w x, where parts are joined
 __device__ __forceinline__ float pg_add(float sum, float w, float x) { return pg_bad32(x) ? sum + x : __builtin_fmaf(w, x, sum); }
 
-// The first cached row of [t, t1) whose V is not finite, or t1.  For all lanes of a wave together.
-template <typename T>
-__device__ __forceinline__ int pg_next_bad(const PagedCache& c, const int32_t* ids, int t, int t1) {
-  constexpr int RB = kD * (int)sizeof(T), LPR = RB / 16, PER = 64 / LPR;   // lanes of a row, rows of a load
-  const int lane = threadIdx.x & 63, mask = (1 << c.page_log) - 1;
-#pragma unroll 1
-  for (; t < t1; t = (t | 15) + 1) {                   // a page holds whole sixteens
-    const char* from = c.v + (pg_page(c, pg_entry(ids, min(t >> c.page_log, c.max_pages - 1))) + (t & mask & ~15)) * RB;
-    uint32_t rows = 0;
-#pragma unroll 2
-    for (int i = 0; i < 16 / PER; ++i) {
-      const uint64_t b = __builtin_amdgcn_ballot_w64(pg_any_bad((const T*)nullptr, ldg16(from + (i * 64 + lane) * 16)));
-#pragma unroll
-      for (int y = 0; y < PER; ++y) rows |= (uint32_t)((b >> y * LPR & ((1ull << LPR) - 1)) != 0) << (i * PER + y);
-    }
-    rows >>= t & 15;
-    if (rows) return min(t + __builtin_ctz(rows), t1);
-  }
-  return t1;
+// Whether the score of a new row (a lane's own) and a cached one (the same for all lanes) is -inf.
+// fp32 queries are scaled first, as they are for the products.
+__device__ __forceinline__ float pg_dot(const uint16_t*, float s, uint32_t q, uint32_t k, float) {
+  return __builtin_fmaf(bf16_hi(q), bf16_hi(k), __builtin_fmaf(bf16_lo(q), bf16_lo(k), s));
 }
-// The elements of the new rows [row0, row0 + ROWS) whose sums of V hold what is not finite, of
-// the cached rows [t0, t1): put(row, x, y) gives dims 2 lane and 2 lane + 1 to where the row's
-// result lies (0: finite).  `see`: cached rows that row number lane sees.
-template <typename T, int ROWS, class F>
-__device__ __forceinline__ void pg_restore(const PagedCache& c, const int32_t* ids, int t0, int t1, int see, int row0, F put) {
-  const int lane = threadIdx.x & 63, mask = (1 << c.page_log) - 1;
-  float z[ROWS][2] = {};
-#pragma unroll 1
-  for (int t = t0; (t = pg_next_bad<T>(c, ids, t, t1)) < t1; ++t) {
-    const size_t row = pg_page(c, pg_entry(ids, min(t >> c.page_log, c.max_pages - 1))) + (t & mask);
-    float x, y;
-    pg_pair(reinterpret_cast<const T*>(c.v) + row * kD + 2 * lane, x, y);
-    x = pg_bad32(x) ? x : 0.f;
-    y = pg_bad32(y) ? y : 0.f;
-    const uint64_t sees = __builtin_amdgcn_ballot_w64(t < see) >> row0;
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r)
-      if (sees >> r & 1) {
-        z[r][0] += x;
-        z[r][1] += y;
-      }
+__device__ __forceinline__ float pg_dot(const float*, float s, uint32_t q, uint32_t k, float scale) {
+  return __builtin_fmaf(__uint_as_float(q) * scale, __uint_as_float(k), s);
+}
+template <typename T>
+__device__ __forceinline__ bool pg_struck(const T* q, const T* k, float scale) {
+  float s = 0.f;
+#pragma unroll 4
+  for (int i = 0; i < kD * (int)sizeof(T) / 16; ++i) {
+    const uint4 x = ld16(q + i * 16 / sizeof(T)), y = ld16(k + i * 16 / sizeof(T));
+    s = pg_dot((const T*)nullptr, s, x.x, y.x, scale);
+    s = pg_dot((const T*)nullptr, s, x.y, y.y, scale);
+    s = pg_dot((const T*)nullptr, s, x.z, y.z, scale);
+    s = pg_dot((const T*)nullptr, s, x.w, y.w, scale);
   }
+  return s == -INFINITY;
+}
+
+// What V holds of a dim that is not finite, as bits of new rows.
+struct OddDim {
+  uint32_t up = 0, down = 0, nan = 0;                  // inf, -inf, NaN
+  __device__ __forceinline__ void add(float x, uint32_t sees, uint32_t struck) {
+    const uint32_t n = x != x ? sees : x == INFINITY || x == -INFINITY ? sees & struck : 0;
+    nan |= n;
+    up |= x == INFINITY ? sees & ~struck : 0;
+    down |= x == -INFINITY ? sees & ~struck : 0;
+  }
+  template <typename E>
+  __device__ __forceinline__ void put(E* p, int r) const {
+    const bool u = up >> r & 1, d = down >> r & 1, n = nan >> r & 1;
+    if (u || d || n) pg_store(p, n || (u && d) ? __builtin_nanf("") : u ? INFINITY : -INFINITY);
+  }
+};
+
+// The results of up to 32 new rows of a wave, where V of the cached rows [t0, t1) that they see
+// is not finite: the infinity that there is alone, or NaN.  A row without weight, of a score of
+// -inf, makes NaN of an infinity.  New row row0 + r, r < n, of a sequence's n_rows in a view sees
+// see0 + (row0 + r) / G rows; its query is row q_row(row0 + r) of q, its result lies at slot + r *
+// 128 or, without slots, at that row of out, where it stays if bit r of `skip` is set.
+// Once the results are stored, in their place: the kernels' registers are all in use before.
+struct RestoreAt {
+  int32_t t0, t1, see0, row0, n, n_rows, skip, hq;
+  size_t q0;                                           // of the sequence's first token and the group's first head
+  float* slot;
+};
+template <typename T, int G>
+__device__ __forceinline__ void pg_restore(const PagedCache& c, int view, const char* q, float scale, char* out, const RestoreAt& at) {
+  constexpr int AHEAD = 8;                             // cached rows at a time; a page holds whole sixteens
+  const int32_t* ids = c.table + (size_t)view * c.max_pages;
+  const int lane = __lane_id(), mask = (1 << c.page_log) - 1;
+  const int own = min(at.row0 + min(lane & 31, at.n - 1), at.n_rows - 1), see = at.see0 + own / G;
+  auto q_row = [&](int r) { return at.q0 + (size_t)(r / G) * at.hq + r % G; };
+  const T* mine = reinterpret_cast<const T*>(q) + q_row(own) * kD;
+  OddDim a, b;                                         // dims 2 lane and 2 lane + 1
+#pragma unroll 1
+  for (int t = at.t0; t < at.t1; t += AHEAD) {
+    const size_t row = pg_page(c, pg_entry(ids, min(t >> c.page_log, c.max_pages - 1))) + (t & mask);
+    const T* from = reinterpret_cast<const T*>(c.v) + row * kD + 2 * lane;
+    float x[AHEAD], y[AHEAD];
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r)
-    if (__builtin_amdgcn_ballot_w64(z[r][0] != 0.f || z[r][1] != 0.f)) put(row0 + r, z[r][0], z[r][1]);
+    for (int i = 0; i < AHEAD; ++i) pg_pair(from + i * kD, x[i], y[i]);
+    bool odd = false;                                  // where NaN is known for all rows, nothing changes
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) odd = odd || (pg_bad32(x[i]) && ~a.nan) || (pg_bad32(y[i]) && ~b.nan);
+    if (!__builtin_amdgcn_ballot_w64(odd)) continue;
+#pragma unroll 1
+    for (int i = 0; i < min(AHEAD, at.t1 - t); ++i) {
+      float u, v;
+      pg_pair(from + i * kD, u, v);
+      const uint32_t sees = (uint32_t)__builtin_amdgcn_ballot_w64(t + i < see);
+      uint32_t struck = 0;
+      if (__builtin_amdgcn_ballot_w64(u == INFINITY || u == -INFINITY || v == INFINITY || v == -INFINITY))
+        struck = (uint32_t)__builtin_amdgcn_ballot_w64(pg_struck(mine, reinterpret_cast<const T*>(c.k) + (row + i) * kD, scale));
+      a.add(u, sees, struck);
+      b.add(v, sees, struck);
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0);                       // the results lie where they belong
+#pragma unroll 1
+  for (int r = 0; r < at.n && at.row0 + r < at.n_rows; ++r) {
+    if (at.slot) {
+      a.put(at.slot + r * kD + 2 * lane, r);
+      b.put(at.slot + r * kD + 2 * lane + 1, r);
+    } else if (!(at.skip >> r & 1)) {
+      T* to = reinterpret_cast<T*>(out) + q_row(at.row0 + r) * kD + 2 * lane;
+      a.put(to, r);
+      b.put(to + 1, r);
+    }
+  }
 }
 
 }  // namespace catekv

@@ -142,26 +142,21 @@ struct StreamLds {
   float (*m)[kStreamWaves][R], (*l)[kStreamWaves][R];
 };
 
-// What a wave wrote of a segment's results, rows 2 wave and 2 wave + 1 (`skip`: bits of those
-// that stay), where V is not finite.  A function of its own, so that the kernel has all
-// registers to itself (inlined, one fp32 token over 65536 rows took 115 to 125 us for 105).
-constexpr int kOwnRows = R / kStreamWaves;
+constexpr int kOwnRows = R / kStreamWaves;    // of a segment's results, that a wave writes
+// pg_restore() as a function by itself: inlined here, one fp32 token over 65536 rows took 115 to
+// 125 us for 105, with registers that the kernel then has to spill.
 template <typename T, int G>
-__device__ __attribute__((noinline)) void stream_restore(const char* v, const int32_t* ids, int n_pages, int page_log, int t0, int t1, int see0,
-                                                         int rows, int skip, float* slot, char* out, int q0, int hq) {
+__device__ __attribute__((noinline)) void stream_restore(char* k, char* v, int32_t* ids, int n_pages, int page_log, const char* q, float scale,
+                                                         char* out, int t0, int t1, int see0, int row0, int n_rows, int skip, int hq, int q0,
+                                                         float* slot) {
   PagedCache c{};
-  c.v = const_cast<char*>(v);
+  c.k = k;
+  c.v = v;
+  c.table = ids;
   c.n_pages = n_pages;
   c.page_log = page_log;
   c.max_pages = INT32_MAX;                    // the rows are the view's
-  const int lane = threadIdx.x & 63, own = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kOwnRows;
-  __builtin_amdgcn_s_waitcnt(0);              // the results lie where they belong
-  pg_restore<T, kOwnRows>(c, ids, t0, t1, min(see0 + (lane & 15) / G, t1), own, [&](int r, float x, float y) {
-    if (r >= rows) return;
-    const int tok = r / G;
-    if (slot) pg_over(slot + r * kD + 2 * lane, x, y);
-    else if (!(skip >> (r - own) & 1)) pg_over(reinterpret_cast<T*>(out) + ((size_t)q0 + (size_t)tok * hq + (r - tok * G)) * kD + 2 * lane, x, y);
-  });
+  pg_restore<T, G>(c, 0, q, scale, out, {t0, t1, see0, row0, kOwnRows, n_rows, skip, hq, (size_t)q0, slot});
 }
 
 // A workgroup's share: segments [first, last).
@@ -365,7 +360,6 @@ __device__ __forceinline__ void stream_share(const PagedAttn& a, const PagedPiec
           const float mw = s_m[w][r];
           const float f = pg_share(mw, M, fM);
           const float4 v = *reinterpret_cast<const float4*>(&s_o[w][r][d]);
-          if (mw == -INFINITY) continue;
           sum += f * s_l[w][r];
           x[0] += f * v.x;
           x[1] += f * v.y;
@@ -386,7 +380,8 @@ __device__ __forceinline__ void stream_share(const PagedAttn& a, const PagedPiec
           const float inv = none ? 0.f : 1.f / sum;
           const int tok = r / G;
           const size_t row = (size_t)sg.q0 + (size_t)tok * a.hq + (r - tok * G);
-          pg_put4((T*)nullptr, a.out + (row * kD + d) * sizeof(T), x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+          pg_put4((T*)nullptr, a.out + (row * kD + d) * sizeof(T), none ? 0.f : x[0] * inv, none ? 0.f : x[1] * inv,
+                  none ? 0.f : x[2] * inv, none ? 0.f : x[3] * inv);
           if (a.lse && d == 0) a.lse[row] = pg_lse(M, sum, cs);
         }
       }
@@ -440,8 +435,9 @@ __device__ __forceinline__ void stream_share(const PagedAttn& a, const PagedPiec
     for (int i = 0; odd >> i; ++i)                    // results that are not finite
       if (odd >> i & 1) {
         const Seg sg = s_seg[i];
-        stream_restore<T, G>(c.v, c.table + (size_t)sg.view * c.max_pages, c.n_pages, c.page_log, sg.t0, sg.t_end, sg.see0, sg.rows,
-                             kept >> kOwnRows * i & 3, sg.slot >= 0 ? a.slots + (size_t)sg.slot * 4 : nullptr, a.out, sg.q0, a.hq);
+        stream_restore<T, G>(c.k, c.v, c.table + (size_t)sg.view * c.max_pages, c.n_pages, c.page_log, a.q, a.scale, a.out,
+                             sg.t0, sg.t_end, sg.see0, wave * kOwnRows, sg.rows, kept >> kOwnRows * i & 3, a.hq, sg.q0,
+                             sg.slot >= 0 ? a.slots + (size_t)sg.slot * 4 + wave * kOwnRows * kD : nullptr);
       }
   }
 }

@@ -483,19 +483,10 @@ void paged_tile_kernel(PagedAttn a) {
     }
     if (unusual) {
       const uint64_t fine = __builtin_amdgcn_ballot_w64(m > -INFINITY && sum == sum);
-      __builtin_amdgcn_s_waitcnt(0);                   // the results lie where they belong
-#pragma unroll 1
-      for (int r0 = 0; r0 < 32; r0 += 4)
-        pg_restore<uint16_t, 4>(c, c.table + (size_t)x.view * c.max_pages, x.t0, x.t0 + x.n_tiles * kTile, see, r0, [&](int i, float u, float v) {
-          const int y = wave * 32 + i, r = x.row0 + y, tok = r / G;
-          if (r >= x.n_new * G) return;
-          if (x.slot >= 0) {
-            pg_over(a.slots + (size_t)x.slot * 4 + (size_t)y * kD + 2 * lane, u, v);
-          } else if (fine >> i & 1) {
-            const size_t qr = (size_t)(x.tok0 + tok) * a.hq + (x.view % c.hkv) * G + (r - tok * G);
-            pg_over(reinterpret_cast<uint16_t*>(a.out) + qr * kD + 2 * lane, u, v);
-          }
-        });
+      const RestoreAt to = {x.t0, x.t0 + x.n_tiles * kTile, x.see0, x.row0 + wave * 32, 32, x.n_new * G, (int)~fine, a.hq,
+                            (size_t)x.tok0 * a.hq + (x.view % c.hkv) * G,
+                            x.slot >= 0 ? a.slots + (size_t)x.slot * 4 + (size_t)wave * 32 * kD : nullptr};
+      pg_restore<uint16_t, G>(c, x.view, a.q, a.scale, a.out, to);
     }
     if (!more) break;
     ++w;

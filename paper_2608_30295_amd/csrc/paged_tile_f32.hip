@@ -204,19 +204,9 @@ void paged_tile_f32_kernel(PagedAttn a) {
     }
     if (unusual) {
       const uint64_t fine = __builtin_amdgcn_ballot_w64(m > -INFINITY && l == l);
-      __builtin_amdgcn_s_waitcnt(0);                   // the results lie where they belong
-#pragma unroll 1
-      for (int r0 = 0; r0 < 32; r0 += 4)
-        pg_restore<float, 4>(c, ids, pc.t0, pc.t0 + n_tiles * kTile, see, r0, [&](int i, float u, float v) {
-          const int y = wave * 32 + i, r = pc.row0 + y, tk = r / G;
-          if (r >= n_rows) return;
-          if (pc.slot >= 0) {
-            pg_over(a.slots + (size_t)pc.slot * 4 + (size_t)y * kD + 2 * lane, u, v);
-          } else if (fine >> i & 1) {
-            const size_t qr = (size_t)(pc.tok0 + tk) * a.hq + h * G + (r - tk * G);
-            pg_over(reinterpret_cast<float*>(a.out) + qr * kD + 2 * lane, u, v);
-          }
-        });
+      const RestoreAt to = {pc.t0, pc.t0 + n_tiles * kTile, see0, pc.row0 + wave * 32, 32, n_rows, (int)~fine, a.hq, (size_t)pc.tok0 * a.hq + h * G,
+                            pc.slot >= 0 ? a.slots + (size_t)pc.slot * 4 + (size_t)wave * 32 * kD : nullptr};
+      pg_restore<float, G>(c, pc.view, a.q, a.scale, a.out, to);
     }
   }
 }

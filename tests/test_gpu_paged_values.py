@@ -165,3 +165,26 @@ def test_infinities_in_rows_of_next_to_no_weight(dtype, G, n, new, at):
     o = out.float()
     assert torch.isinf(o[..., :len(rows)]).all() and torch.isnan(o[..., len(rows) + 1]).all()
     assert torch.isfinite(o[..., len(rows) + 2:]).all()
+
+
+@pytest.mark.parametrize("dtype,G,n,new", FORMS)
+def test_infinities_in_rows_without_weight(dtype, G, n, new):
+    """A score of -inf is a weight of 0, and 0 times an infinity NaN, wherever the row lies: in
+    single rows, and in a stretch of them that fills tiles and parts.  Where every score is
+    -inf the result is 0."""
+    c, plan, put = view(dtype, n, new, G, hkv=2)
+    q = randn((new, 2 * G, 128), 5, dtype)
+    q[..., 0] = q[..., 0].abs() + 0.5
+    rows = sorted(({int(x) for x in np.linspace(0, n - 1, 60)} | {n, n + new - 1}) - {5})
+    for i, row in enumerate(rows):
+        put(row, k=-inf, dim=0)
+        put(row, v=inf if i % 2 else -inf, dim=i)
+    put(5, v=inf, dim=80)                                         # a row of ordinary weight
+    for row in range(n // 4, n // 4 + min(n // 2, 400)):
+        put(row, k=-inf, dim=0)
+    put(n // 4 + 3, v=inf, dim=81)
+    check(c, plan, q, new, G)
+    for p in c.table[0, 0].tolist():
+        c.k[p, :, 0] = -inf
+    out, lse = check(c, plan, q, new, G)
+    assert (out[:, :G] == 0).all() and (lse[:, :G] == -inf).all()
