@@ -149,8 +149,10 @@ def append_kv_paged(plan: PagedPlan, cache: PagedCache, k_new: torch.Tensor, v_n
                          f"{tuple(v_new.shape)}")
     if k_new.dtype != cache.dtype or v_new.dtype != cache.dtype:
         raise TypeError(f"k_new and v_new must be {cache.dtype}, not {k_new.dtype}, {v_new.dtype}")
-    tok, head, one = k_new.stride()
-    if one != 1 or v_new.stride() != (tok, head, one):
+    # (what a dimension of size 1 has for a stride leads nowhere)
+    strides = [tuple(x if n > 1 else 0 for x, n in zip(t.stride(), t.shape)) for t in (k_new, v_new)]
+    tok, head, one = strides[0]
+    if one != 1 or strides[1] != strides[0]:
         raise ValueError("k_new and v_new need the same strides and contiguous rows")
     index = _device_of(cache.table, plan.ws, overflow)
     if k_new.get_device() != index or v_new.get_device() != index:

@@ -36,3 +36,30 @@ def test_lengths_of_any_size_are_checked(L):
         assert over.item() == 1
         ck.drop_paged(c, torch.tensor([0, 0, 0], device=DEV))
         before.same(c)
+
+
+@pytest.mark.parametrize("new,hkv", [(1, 4), (3, 1), (1, 1), (0, 4)])
+def test_strides_of_dimensions_of_size_one_do_not_matter(new, hkv):
+    """One token, or one head: k by itself and v a part of a projection of all, whose strides
+    differ where they lead nowhere; one that is no multiple of 16 bytes, too."""
+    c, s = cache_of(40, 16, 2, hkv, 4, BF16)
+    append(c, s, [1], [5], hkv, 1)
+    plan = ck.paged_plan(c, [1], [new], [[20] * hkv], hkv)
+    k = randn((new, hkv, 128), 3, BF16)
+    if hkv > 1:                                                  # [token][3 hkv d + 8]: q, k and v side by side
+        v = randn((max(new, 1), 3 * hkv * 128 + 8), 4, BF16).as_strided((new, hkv, 128), (3 * hkv * 128 + 8, 128, 1), 2 * hkv * 128)
+    else:                                                        # [token][d], any stride of the one head
+        v = randn((new, 128), 4, BF16).as_strided((new, 1, 128), (128, 77, 1))
+    ck.append_kv_paged(plan, c, k, v)
+    ck.attn_paged(plan, c, randn((new, hkv, 128), 5, BF16))
+    s.append([1], [new], host(k), host(v))
+    s.same(c)
+
+
+def test_strides_that_differ_are_refused():
+    c, _ = cache_of(40, 16, 2, 4, 4, BF16)
+    plan = ck.paged_plan(c, [1], [2], [[20] * 4], 4)
+    k, v = randn((2, 4, 128), 3, BF16), randn((2, 3, 4, 128), 4, BF16)[:, 2]
+    with pytest.raises(ValueError):
+        ck.append_kv_paged(plan, c, k, v)
+    assert c.lens.sum().item() == 0
