@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import operator
 from array import array
 from dataclasses import dataclass, field
 from typing import Optional, Sequence, Tuple
@@ -106,10 +107,22 @@ class PagedPlan:
         self.ref = ctypes.byref(self.plan)
 
 
+def _whole(x, dtype, name: str) -> np.ndarray:
+    """The whole numbers of x, flat; what the type does not hold is refused, not cut."""
+    a = np.asarray(x)
+    if a.dtype.kind == "O":                          # single tensors, or Python's long numbers
+        a = np.array([operator.index(i) for i in a.ravel()], dtype=object)
+    elif a.size and a.dtype.kind not in "iu":
+        raise TypeError(f"{name} must be whole numbers, not {a.dtype}")
+    if a.size and not np.can_cast(a.dtype, dtype) and not (np.iinfo(dtype).min <= a.min() and a.max() <= np.iinfo(dtype).max):
+        raise ValueError(f"{name} holds a number that {np.dtype(dtype)} does not")
+    return np.ascontiguousarray(a, dtype=dtype).ravel()
+
+
 def _plan_args(cache: PagedCache, slots, new, max_rows):
-    s = np.ascontiguousarray(slots, dtype=np.int32).ravel()
-    m = np.ascontiguousarray(new, dtype=np.int32).ravel()
-    r = np.ascontiguousarray(max_rows, dtype=np.int64).ravel()
+    s = _whole(slots, np.int32, "slots")
+    m = _whole(new, np.int32, "new")
+    r = _whole(max_rows, np.int64, "max_rows")
     if m.size != s.size or r.size != s.size * cache.hkv:
         raise ValueError(f"{s.size} slots, {m.size} counts of new tokens and {r.size} bounds for {cache.hkv} heads each")
     return (s.ctypes.data_as(_lib.P_i32), m.ctypes.data_as(_lib.P_i32), r.ctypes.data_as(_lib.P_i64), s.size), m, (s, r)

@@ -5,6 +5,7 @@ import ctypes
 import math
 import os
 import re
+from types import SimpleNamespace
 
 import numpy as np
 import pytest
@@ -317,3 +318,22 @@ def test_bounds_count_the_roundings():
         p = np.exp(s - s.max())
         o = bf(bf(p) @ v[:261 + j] / p.sum())
         assert (np.abs(o - out[j]) <= eo[j]).all() and np.abs(o - out[j]).max() > 0
+
+
+@needs_lib
+@pytest.mark.parametrize("slots,new,rows,error", [
+    (np.array([2 ** 32, 1]), [1, 1], [[9, 9]] * 2, ValueError), ([0, 1], np.array([2 ** 32 + 1, 1]), [[9, 9]] * 2, ValueError),
+    ([0, 1], torch.tensor([1, -2 ** 32 + 1]), [[9, 9]] * 2, ValueError), ([0, 1], [1, 1], np.array([[9, 9], [9, 2 ** 64 - 9]], np.uint64), ValueError),
+    ([0, 1], [1.5, 1], [[9, 9]] * 2, TypeError), ([0, 1], [1, 1], torch.tensor([[9.0, 9], [9, math.nan]]), TypeError),
+    ([0, 1], [1, 2 ** 70], [[9, 9]] * 2, ValueError), ([0, 1], [1, 1], [[9, 9], [9, None]], TypeError), ([[0], [1]], [1, 1], [9] * 4, None),
+    (range(2), torch.tensor([1, 1]), np.full((2, 2), 9, np.uint8), None), ([torch.tensor(0), 1], [1, np.int64(1)], [[9, 9]] * 2, None), ([], [], [], None),
+])
+def test_the_binding_takes_whole_numbers_as_they_are(slots, new, rows, error):
+    """Numbers that 32 bits do not hold, or that are none, are refused, and not cut to others."""
+    c = SimpleNamespace(hkv=2, ref=ctypes.byref(cache()))
+    if error:
+        with pytest.raises(error):
+            ck.paged_workspace(c, slots, new, rows, 8)
+    else:
+        want = ck.lib().catekv_paged_workspace(c.ref, i32(0, 1), i32(1, 1), i64(9, 9, 9, 9), len(slots), 8)
+        assert ck.paged_workspace(c, slots, new, rows, 8) == want
