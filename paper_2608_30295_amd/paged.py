@@ -114,9 +114,13 @@ def _whole(x, dtype, name: str) -> np.ndarray:
         a = np.array([operator.index(i) for i in a.ravel()], dtype=object)
     elif a.size and a.dtype.kind not in "iu":
         raise TypeError(f"{name} must be whole numbers, not {a.dtype}")
-    if a.size and not np.can_cast(a.dtype, dtype) and not (np.iinfo(dtype).min <= a.min() and a.max() <= np.iinfo(dtype).max):
+    try:
+        b = a.astype(dtype, copy=False)
+    except OverflowError:
+        b = None
+    if b is None or b is not a and (a != b).any():
         raise ValueError(f"{name} holds a number that {np.dtype(dtype)} does not")
-    return np.ascontiguousarray(a, dtype=dtype).ravel()
+    return np.ascontiguousarray(b).ravel()
 
 
 def _plan_args(cache: PagedCache, slots, new, max_rows):
