@@ -1,7 +1,9 @@
 """What the calls of include/catekv_paged.h refuse, on the host: arguments are checked
 before the GPU is touched.  The plain forms that the GPU tests compare with are pinned
 by facts other than their own formulas."""
+import ast
 import ctypes
+import inspect
 import math
 import os
 import re
@@ -337,3 +339,13 @@ def test_the_binding_takes_whole_numbers_as_they_are(slots, new, rows, error):
     else:
         want = ck.lib().catekv_paged_workspace(c.ref, i32(0, 1), i32(1, 1), i64(9, 9, 9, 9), len(slots), 8)
         assert ck.paged_workspace(c, slots, new, rows, 8) == want
+
+
+@pytest.mark.skipif(not os.path.exists(os.path.join(ROOT, "README.md")), reason="a tree without its README")
+def test_the_examples_of_the_readme_are_calls_that_exist():
+    blocks = re.findall(r"```python\n(.*?)```", open(os.path.join(ROOT, "README.md")).read(), flags=re.S)
+    calls = [x for b in blocks for x in ast.walk(ast.parse(b)) if isinstance(x, ast.Call) and isinstance(x.func, ast.Attribute)
+             and getattr(x.func.value, "id", None) == "ck"]
+    assert len(calls) > 15
+    for x in calls:
+        inspect.signature(getattr(ck, x.func.attr)).bind(*x.args, **{k.arg: k.value for k in x.keywords})
