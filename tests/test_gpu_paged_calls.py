@@ -63,3 +63,44 @@ def test_strides_that_differ_are_refused():
     with pytest.raises(ValueError):
         ck.append_kv_paged(plan, c, k, v)
     assert c.lens.sum().item() == 0
+
+
+def test_decoding_over_pages_gives_what_decode_attn_gives():
+    """A prompt's cache with two of four heads cut back, in pages and dense: three more tokens,
+    each attended for by both, and both held to the same 64-bit results."""
+    n, hkv, G, cs, tail, b = 900, 4, 4, 8, 32, 20
+    hq = hkv * G
+    k, v = (randn((hkv, n + 3, 128), i, BF16) for i in (1, 2))
+    idx = ck.select_critical(randn((hq, tail, 128), 7, BF16), k[:, :n].contiguous(), [1, 3], cs, b)
+    lens = torch.full((hkv,), n, dtype=torch.int64, device=DEV)
+    kc, vc = ck.compact_kv(k[:, :n].contiguous(), v[:, :n].contiguous(), [1, 3], idx, cs, tail, lens)
+    dense = [[torch.zeros((n + 3, 128), dtype=BF16, device=DEV) for _ in "kv"] for _ in range(hkv)]
+    for h in range(hkv):
+        for to, full, cut in zip(dense[h], (k, v), (kc, vc)):
+            rows = cut[(1, 3).index(h)] if h in (1, 3) else full[h, :n]
+            to[:int(lens[h])] = rows[:int(lens[h])]
+    c, _ = cache_of(80, 64, 2, hkv, 16, BF16)
+    plan = ck.paged_plan(c, [1], [n], [[n] * hkv], hq)
+    ck.append_kv_paged(plan, c, k[:, :n].transpose(0, 1), v[:, :n].transpose(0, 1))
+    ck.compact_kv_paged(c, 1, [1, 3], idx, cs, tail)
+    assert torch.equal(c.lens[1], lens)
+    plan, dense_plan = ck.paged_plan(c, [1], [1], [[n + 3] * hkv], hq), ck.decode_plan([n + 3] * hkv, hq, hkv, DEV)
+    table = ck.kv_table([(a.data_ptr(), w.data_ptr()) for a, w in dense], DEV)
+    for t in range(3):
+        k1, v1 = (x[:, n + t].unsqueeze(0).contiguous() for x in (k, v))
+        ck.append_kv_paged(plan, c, k1, v1)
+        for h in range(hkv):
+            dense[h][0][int(lens[h])], dense[h][1][int(lens[h])] = k1[0, h], v1[0, h]
+        lens += 1
+        q = randn((1, hq, 128), 20 + t, BF16)
+        out, lse = ck.attn_paged(plan, c, q)
+        want, want_lse = ck.decode_attn(dense_plan, q, table, lens.view(1, hkv))
+        s = R.Pages.of(c)
+        for h in range(hkv):
+            g = slice(h * G, (h + 1) * G)
+            kk, vv = s.rows(1, h)
+            assert np.array_equal(kk, host(dense[h][0])[:len(kk)]) and np.array_equal(vv, host(dense[h][1])[:len(kk)])
+            o, z, A, B = R.attention(host(q)[:, g], kk, vv, 1, 128 ** -0.5)
+            for a, l, dtype in ((out, lse, BF16), (want, want_lse, F32)):        # decode_attn: fp32 weights and results
+                eo, ez = R.bounds(o, z, A, B, len(kk), dtype, G)
+                assert (np.abs(host(a)[:, g] - o) <= eo).all() and (np.abs(host(l)[:, g] - z) <= ez).all()
