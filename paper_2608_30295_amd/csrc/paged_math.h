@@ -121,8 +121,6 @@ __device__ __forceinline__ bool pg_unusual(const float (&o)[N]) {
   for (int i = 0; i < N; i += 2) t = __builtin_fmaf(o[i], o[i + 1], t);
   return pg_bad32(t);
 }
-// sum + w x, where parts are joined
-__device__ __forceinline__ float pg_add(float sum, float w, float x) { return pg_bad32(x) ? sum + x : __builtin_fmaf(w, x, sum); }
 
 // Whether the score of a new row (a lane's own) and a cached one (the same for all lanes) is -inf.
 // fp32 queries are scaled first, as they are for the products.
