@@ -188,3 +188,39 @@ def test_infinities_in_rows_without_weight(dtype, G, n, new):
         c.k[p, :, 0] = -inf
     out, lse = check(c, plan, q, new, G)
     assert (out[:, :G] == 0).all() and (lse[:, :G] == -inf).all()
+
+
+@pytest.mark.parametrize("dtype,G,singles,long,chunk", [(BF16, 1, 60, 40, 600), (BF16, 2, 9, 900, 300), (BF16, 4, 60, 500, 150), (BF16, 8, 300, 40, 3),
+                                                        (BF16, 4, 400, 300, 2), (F32, 4, 60, 300, 100), (F32, 2, 300, 200, 3)])
+def test_values_that_are_not_finite_all_over_a_batch(dtype, G, singles, long, chunk):
+    """Sequences of all lengths in one batch, chunks beside few tokens, where one row in twenty has
+    an infinity or NaN in V and one in forty scores of -inf, rows behind the views' ends among them."""
+    hkv, r, page = 2, np.random.RandomState(singles), 32
+    new = [chunk] + [int(x) for x in r.randint(1, 3 if 2 * G <= 16 else 2, size=singles)] + [chunk // 2 + 1]
+    ctx = [1500] + [int(x) for x in r.randint(0, long, size=singles)] + [700]
+    slots = [int(x) for x in r.permutation(singles + 4)[:singles + 2]]
+    need = sum(hkv * R.pages_of(a + b, page) for a, b in zip(ctx, new))
+    c, s = cache_of(need + 9, page, singles + 4, hkv, max(R.pages_of(a + b, page) for a, b in zip(ctx, new)) + 1, dtype)
+    append(c, s, slots, ctx, hkv * G, 31)
+    plan = append(c, s, slots, new, hkv * G, 33)
+    k, v = c.k.view(-1, 128), c.v.view(-1, 128)
+    rows = r.permutation(len(v))
+    for i, x in enumerate((inf, -inf, math.nan, inf, inf, -inf)):
+        at = torch.from_numpy(rows[i::120].copy()).to(DEV)
+        v[at, torch.from_numpy(r.randint(0, 100, size=len(at))).to(DEV)] = x
+    k[torch.from_numpy(rows[::40].copy()).to(DEV), 0] = -inf
+    q = randn((sum(new), hkv * G, 128), 35, dtype)
+    q[..., 0] = q[..., 0].abs() + 0.5
+    out, lse = ck.attn_paged(plan, c, q)
+    s, at = R.Pages.of(c), 0
+    got, got_lse, qh = host(out).astype(np.float64), lse.cpu().numpy().astype(np.float64), host(q)
+    for i, (slot, m) in enumerate(zip(slots, new)):
+        for h in range(hkv):
+            g = slice(h * G, (h + 1) * G)
+            o, z, eo, ez = reference(qh[at:at + m, g], *s.rows(slot, h), m, 128 ** -0.5, dtype)
+            x, y, fin = got[at:at + m, g], got_lse[at:at + m, g], np.isfinite(o)
+            assert ((x == o) | (np.isnan(x) & np.isnan(o)))[~fin].all(), f"sequence {i} of {ctx[i]} + {m} head {h}: {np.argwhere(~fin & (x != o))[:4].tolist()}"
+            assert (np.abs(x - o)[fin] <= eo[fin]).all(), f"sequence {i} of {ctx[i]} + {m} head {h}"
+            fin = np.isfinite(z)
+            assert np.array_equal(z[~fin], y[~fin], equal_nan=True) and (np.abs(y - z)[fin] <= ez[fin]).all(), f"sequence {i} head {h}: lse"
+        at += m
