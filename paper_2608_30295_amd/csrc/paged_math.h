@@ -173,7 +173,7 @@ struct RestoreAt {
 };
 template <typename T, int G>
 __device__ __forceinline__ void pg_restore(const PagedCache& c, int view, const char* q, float scale, char* out, const RestoreAt& at) {
-  constexpr int AHEAD = 8;                             // cached rows at a time; a page holds whole sixteens
+  constexpr int AHEAD = 8;                             // cached rows at a time (a page holds whole sixteens); 16: the same
   const int32_t* ids = c.table + (size_t)view * c.max_pages;
   const int lane = __lane_id(), mask = (1 << c.page_log) - 1;
   const int own = min(at.row0 + min(lane & 31, at.n - 1), at.n_rows - 1), see = at.see0 + own / G;

@@ -440,7 +440,7 @@ void paged_tile_kernel(PagedAttn a) {
     float sums[64];
 #pragma unroll
     for (int i = 0; i < 64; ++i) sums[i] = o[i >> 4][i & 15];
-    const bool unusual = purged || __builtin_amdgcn_ballot_w64(sum == sum && pg_unusual(sums));
+    const bool unusual = __builtin_amdgcn_ballot_w64(sum == sum && pg_unusual(sums));
     const int at = wave * 32 + (lane & 31), row = x.row0 + at;
     if (row < x.n_new * G) {
       const int hi = lane >> 5, tok = row / G;
@@ -481,9 +481,10 @@ void paged_tile_kernel(PagedAttn a) {
         if (a.lse && hi == 0) a.lse[qrow / kRB] = pg_lse(top, sum, cs);
       }
     }
-    if (unusual) {
+    if (unusual || purged) {                           // only tiles that were looked at have V left out of finite sums
       const uint64_t fine = __builtin_amdgcn_ballot_w64(m > -INFINITY && sum == sum);
-      const RestoreAt to = {x.t0, x.t0 + x.n_tiles * kTile, x.see0, x.row0 + wave * 32, 32, x.n_new * G, (int)~fine, a.hq,
+      const int n = x.n_new * G, end = min(x.t0 + x.n_tiles * kTile, x.see0 + (min(x.row0 + wave * 32 + 32, n) - 1) / G);
+      const RestoreAt to = {unusual ? x.t0 : x.t0 + first * kTile, end, x.see0, x.row0 + wave * 32, 32, n, (int)~fine, a.hq,
                             (size_t)x.tok0 * a.hq + (x.view % c.hkv) * G,
                             x.slot >= 0 ? a.slots + (size_t)x.slot * 4 + (size_t)wave * 32 * kD : nullptr};
       pg_restore<uint16_t, G>(c, x.view, a.q, a.scale, a.out, to);

@@ -176,7 +176,7 @@ void paged_tile_f32_kernel(PagedAttn a) {
     float sums[64];
 #pragma unroll
     for (int i = 0; i < 64; ++i) sums[i] = o[i >> 4][i & 15];
-    const bool unusual = purged || __builtin_amdgcn_ballot_w64(l == l && pg_unusual(sums));
+    const bool unusual = __builtin_amdgcn_ballot_w64(l == l && pg_unusual(sums));
     if (mine) {
       const float top = pg_top(m, l);
       const bool none = top == -INFINITY;
@@ -202,9 +202,10 @@ void paged_tile_f32_kernel(PagedAttn a) {
         a.lse[qrow / kRB] = pg_lse(top, l, cs);
       }
     }
-    if (unusual) {
+    if (unusual || purged) {                           // only masked tiles have V left out of finite sums
       const uint64_t fine = __builtin_amdgcn_ballot_w64(m > -INFINITY && l == l);
-      const RestoreAt to = {pc.t0, pc.t0 + n_tiles * kTile, see0, pc.row0 + wave * 32, 32, n_rows, (int)~fine, a.hq, (size_t)pc.tok0 * a.hq + h * G,
+      const int end = min(pc.t0 + n_tiles * kTile, see0 + (min(pc.row0 + wave * 32 + 32, n_rows) - 1) / G);
+      const RestoreAt to = {unusual ? pc.t0 : pc.t0 + n_full * kTile, end, see0, pc.row0 + wave * 32, 32, n_rows, (int)~fine, a.hq, (size_t)pc.tok0 * a.hq + h * G,
                             pc.slot >= 0 ? a.slots + (size_t)pc.slot * 4 + (size_t)wave * 32 * kD : nullptr};
       pg_restore<float, G>(c, pc.view, a.q, a.scale, a.out, to);
     }
