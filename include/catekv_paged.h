@@ -120,7 +120,8 @@ int catekv_paged_append(const catekv_paged_cache* cache, const catekv_paged_plan
  * A token whose scores are all NaN has NaN results.  What a token sees of V reaches its result
  * as the formula says: an infinity is the result, however small its row's weight (the row's
  * score finite), both of them in a dim or one in a row of score -inf (0 times it) are NaN.
- * Such results take longer: 1 us for 8 of the view's rows, 5 for each that holds an infinity.
+ * Such results take longer: 2 to 5 us for 8 of a view's rows, and 5 for each that holds an
+ * infinity, in the kernel's longest piece.
  * bf16: for a sequence of up to 16 new rows (its new tokens times hq / hkv) the weights
  * exp(s - max) are kept to 16 bits for their product with V, for longer ones they are
  * rounded to bf16; their sum is of the unrounded ones.

@@ -12,7 +12,9 @@
 // loaded of each cached row, one product per dim.
 //
 // bf16, 3 views of 131072 rows and 5 of 2112, 4 heads a group: 207 MB in 37 us, 5.6 TB/s with
-// the start; 64 sequences: 553 MB in 95 us, 5.8 TB/s.  fp32, 65536 rows: 4.9 TB/s.  A
+// the start; 64 sequences: 553 MB in 95 us, 5.8 TB/s.  fp32, 8 views of 65536 rows: 537 MB in 102 us,
+// 5.3 TB/s; 64 sequences 1108 MB in 210, the same: with 256 registers in use, 15 to 27 spilled, most in
+// the last tiles of a segment, and a quarter of the cycles in its fp32 products.  A
 // compute unit takes 22 GB/s with all of them at work and 23 to 28 with a third: all are given a share, but for those
 // that a batch's chunks keep.
 #pragma once

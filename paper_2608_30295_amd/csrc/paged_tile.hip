@@ -11,13 +11,18 @@
 // registers are in place as the operand P^T of O^T = V^T P^T: a product does not ask in
 // which order its terms come, and V is read in the same order.
 //
+// Weights are rounded to bf16 for their product with V (2^-8 of each; their sum is of the
+// unrounded ones): against 64 bits 0.0020, as a root mean square over the values', instead of
+// the 0.0017 of the result's own rounding.  In two parts, as the few-token kernel has them, they would take three
+// products where two bound the kernel now.
+//
 // The softmax runs online, one tile behind: between the products of tile t + 1's scores
 // the vector unit forms the weights of tile t, and while these meet V it takes the
 // maxima of tile t + 1.  A wave issues in order, so the two are laid between each other
 // in the program, and scheduling barriers keep them there.
 //
-// 2048 new tokens, the last of 32768 rows, 32 heads over 8: 1065 GFLOP in 990 to 1055 us, 1.01 to
-// 1.07 PFLOP/s where a large library product reaches 1.10 (products beside each other
+// 2048 new tokens, the last of 32768 rows, 32 heads over 8: 1065 GFLOP in 940 to 1030 us, 1.03 to
+// 1.13 PFLOP/s where a large library product reaches 1.10 (products beside each other
 // without softmax: 1.6 to 1.9).  The matrix cores are busy for 52% of the cycles, the vector
 // unit issues in 45%; no LDS bank conflicts.  Larger tiles of new rows do not fit the
 // registers; 128 to a workgroup would read K and V from LDS twice as often.

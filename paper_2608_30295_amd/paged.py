@@ -142,6 +142,8 @@ def paged_plan(cache: PagedCache, slots: Sequence[int], new: Sequence[int], max_
                ws: Optional[torch.Tensor] = None) -> PagedPlan:
     """Work list of a batch: sequence i lies in slots[i] and has new[i] new tokens;
     max_rows [n_seqs][hkv]: upper bounds of its views' rows with them (blocking).
+    Attention looks no further: a view that outgrows its bound needs another plan, and
+    nothing says so at the call.
     Serves the append and the attention of every layer and later step of a batch of
     this shape, on caches of this geometry."""
     args, m, _hold = _plan_args(cache, slots, new, max_rows)
