@@ -224,3 +224,19 @@ def test_values_that_are_not_finite_all_over_a_batch(dtype, G, singles, long, ch
             fin = np.isfinite(z)
             assert np.array_equal(z[~fin], y[~fin], equal_nan=True) and (np.abs(y - z)[fin] <= ez[fin]).all(), f"sequence {i} head {h}: lse"
         at += m
+
+
+@pytest.mark.parametrize("dtype,G,n,new", FORMS)
+def test_a_score_of_plus_infinity_is_nan(dtype, G, n, new):
+    """inf - inf in the softmax: NaN for the tokens that see the row, wherever it lies, and nothing
+    for those that do not; finite scores as large as fp32 holds are none."""
+    for row in (n // 2, n + new - 1):
+        c, plan, put = view(dtype, n, new, G, hkv=2)
+        q = randn((new, 2 * G, 128), 5, dtype)
+        q[..., 0] = q[..., 0].abs() + 0.5
+        put(row, k=inf, dim=0)
+        put(3, k=-inf, dim=0, head=1)
+        out, lse = check(c, plan, q, new, G)
+        sees = torch.arange(n, n + new, device=DEV) >= row
+        assert torch.isnan(out[sees, :G].float()).all() and torch.isnan(lse[sees, :G]).all()
+        assert torch.isfinite(out[~sees].float()).all() and torch.isfinite(out[:, G:].float()).all()
