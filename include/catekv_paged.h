@@ -115,7 +115,7 @@ int catekv_paged_append(const catekv_paged_cache* cache, const catekv_paged_plan
  * and out = 0, lse = -inf where see <= 0 or every score is -inf.  What lies in rows
  * that a token does not see (NaN and infinities among it) does not reach its result.
  * q     [n_tokens][hq][d] (dtype)
- * out   [n_tokens][hq][d] (dtype: fp32 sums, rounded once)
+ * out   [n_tokens][hq][d] (dtype: fp32 sums, rounded once); q, which is read until the end, is not it
  * lse   [n_tokens][hq] fp32 or NULL
  * A token whose scores are all NaN has NaN results.  What a token sees of V reaches its result
  * as the formula says: an infinity is the result, however small its row's weight (the row's

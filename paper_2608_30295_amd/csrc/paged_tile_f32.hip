@@ -205,7 +205,8 @@ void paged_tile_f32_kernel(PagedAttn a) {
     if (unusual || purged) {                           // only masked tiles have V left out of finite sums
       const uint64_t fine = __builtin_amdgcn_ballot_w64(m > -INFINITY && l == l);
       const int end = min(pc.t0 + n_tiles * kTile, see0 + (min(pc.row0 + wave * 32 + 32, n_rows) - 1) / G);
-      const RestoreAt to = {unusual ? pc.t0 : pc.t0 + n_full * kTile, end, see0, pc.row0 + wave * 32, 32, n_rows, (int)~fine, a.hq, (size_t)pc.tok0 * a.hq + h * G,
+      const RestoreAt to = {unusual ? pc.t0 : pc.t0 + n_full * kTile, end, see0, pc.row0 + wave * 32, 32, n_rows, (int)~fine, a.hq,
+                            (size_t)pc.tok0 * a.hq + h * G,
                             pc.slot >= 0 ? a.slots + (size_t)pc.slot * 4 + (size_t)wave * 32 * kD : nullptr};
       pg_restore<float, G>(c, pc.view, a.q, a.scale, a.out, to);
     }
