@@ -133,8 +133,9 @@ int catekv_paged_attn(const catekv_paged_cache* cache, const catekv_paged_plan_t
 /* Slot dst_host[i] becomes a copy of slot src_host[i] that shares its pages.  Every
  * view of dst must be empty: one that is not is left unchanged, and *refused = 1
  * when refused is not NULL (int32, device, never cleared here).
- * Errors: INVALID_ARG for null pointers, n outside [1, 256], a slot out of range, a
- * dst listed twice or also as a src. */
+ * Any number of pairs (a launch for every 256).
+ * Errors: INVALID_ARG for null pointers, n < 1, a slot out of range, a dst listed
+ * twice or also as a src. */
 int catekv_paged_fork(const catekv_paged_cache* cache, const int32_t* src_host, const int32_t* dst_host, int n,
                       int32_t* refused, void* stream);
 

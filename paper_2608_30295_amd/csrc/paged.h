@@ -8,7 +8,7 @@
 namespace catekv {
 
 constexpr int64_t kPagedMaxRows = (int64_t)1 << 26;   // of a view
-constexpr int kPagedMaxList = 256;                    // slots of a fork or a gather
+constexpr int kPagedMaxList = 256;                    // slots of a gather, pairs of one of a fork's launches
 constexpr int kPagedMaxHeads = 128;                   // heads of a compaction
 constexpr int kPagedMaxHkv = 1024;                    // views of a slot (threads of the taking workgroup)
 

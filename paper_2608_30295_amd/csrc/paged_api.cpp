@@ -671,22 +671,25 @@ int catekv_paged_fork(const catekv_paged_cache* cache, const int32_t* src_host, 
     int rc = check_cache(cache);
     if (rc) return rc;
     if (!src_host || !dst_host) return fail(CATEKV_ERR_INVALID_ARG, "null pointer");
-    if (n < 1 || n > kPagedMaxList) return fail(CATEKV_ERR_INVALID_ARG, "n=%d outside [1, %d]", n, kPagedMaxList);
+    if (n < 1) return fail(CATEKV_ERR_INVALID_ARG, "n=%d must be >= 1", n);
     rc = check_slots(cache, src_host, n, false, "source");
     if (!rc) rc = check_slots(cache, dst_host, n, true, "destination");
     if (rc) return rc;
-    PagedFork a{};
-    a.c = kernel_cache(cache);
-    a.refused = refused;
-    a.n = n;
-    std::copy(src_host, src_host + n, a.src);
-    std::copy(dst_host, dst_host + n, a.dst);
     std::vector<char> is_src(cache->n_slots);
     for (int i = 0; i < n; ++i) is_src[src_host[i]] = 1;
     for (int i = 0; i < n; ++i)
       if (is_src[dst_host[i]]) return fail(CATEKV_ERR_INVALID_ARG, "slot %d is a source and a destination", dst_host[i]);
-    const hipError_t e = launch_paged_fork(a, reinterpret_cast<hipStream_t>(stream));
-    return e == hipSuccess ? host_ok() : hip_fail(e, "paged_fork launch");
+    PagedFork a{};
+    a.c = kernel_cache(cache);
+    a.refused = refused;
+    for (int i = 0; i < n; i += a.n) {             // no pair depends on another
+      a.n = std::min(n - i, kPagedMaxList);
+      std::copy(src_host + i, src_host + i + a.n, a.src);
+      std::copy(dst_host + i, dst_host + i + a.n, a.dst);
+      const hipError_t e = launch_paged_fork(a, reinterpret_cast<hipStream_t>(stream));
+      if (e != hipSuccess) return hip_fail(e, "paged_fork launch");
+    }
+    return host_ok();
   });
 }
 

@@ -210,8 +210,8 @@ def attn_paged(plan: PagedPlan, cache: PagedCache, q: torch.Tensor, scale: Optio
 def fork_paged(cache: PagedCache, src: Sequence[int], dst: Sequence[int], refused: Optional[torch.Tensor] = None) -> None:
     """Slot dst[i] (empty) becomes a copy of slot src[i] that shares its pages; an
     append to either copies the page that it writes first.  refused: int32 [1] on
-    the GPU (set to 1 when a view of a dst was not empty, and left) or None.  Up to
-    256 pairs go in one call; longer lists are refused."""
+    the GPU (set to 1 when a view of a dst was not empty, and left) or None.  Lists of
+    any length, checked as a whole before the first is forked."""
     if len(src) != len(dst):
         raise ValueError(f"{len(src)} sources for {len(dst)} destinations")
     index = _device_of(cache.table, refused)

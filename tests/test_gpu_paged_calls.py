@@ -65,6 +65,22 @@ def test_strides_that_differ_are_refused():
     assert c.lens.sum().item() == 0
 
 
+@pytest.mark.parametrize("n", [256, 257, 600])
+def test_forks_of_any_number(n):
+    """More pairs than one launch takes, one of them to a slot that is not empty, in the last launch;
+    a list with a bad slot at its end forks none."""
+    c, s = cache_of(80, 16, n + 5, 2, 4, BF16)
+    append(c, s, [0, 1, n + 2], [37, 16, 3], 2, 1)
+    src, dst = [i % 3 for i in range(n)], list(range(3, n + 3))       # (slot 2 is empty; n + 2 holds rows)
+    ref = torch.zeros(1, dtype=torch.int32, device=DEV)
+    with pytest.raises(Exception, match="slot"):
+        ck.fork_paged(c, src + [0], dst + [n + 5], ref)
+    s.same(c)
+    ck.fork_paged(c, src, dst, ref)
+    assert s.fork(src, dst) is True and ref.item() == 1
+    s.same(c)
+
+
 def test_decoding_over_pages_gives_what_decode_attn_gives():
     """A prompt's cache with two of four heads cut back, in pages and dense: three more tokens,
     each attended for by both, and both held to the same 64-bit results."""
